@@ -1,0 +1,447 @@
+"""The measured work of the serving operators: what one tensor-parallel shard
+of a quantised decoder does in a step, at the shard sizes of TP degrees 1, 2,
+4 and 8 of a 31B-parameter decoder (hidden size 5120, 40 query and 8 key/value
+heads of 128, feed-forward size 20480) and at generic odd sizes.
+
+* ``linear``     a projection in 8-bit integers: the activations are quantised
+                 with a scale for each token, multiplied by weights that have a
+                 scale for each output channel, and scaled back;
+* ``append``     a step's queries and keys are rotated to their positions, keys
+                 and values enter the paged 8-bit cache, and the sequences'
+                 cache is read back as the values it stands for;
+* ``attention``  attention of packed queries over the paged 8-bit cache, with a
+                 scale for each page and head.
+
+With ``own`` false every operator is computed in its plain form (elementary
+torch operations in 32 bits, rounded once at the end); with ``own`` true by the
+public calls of ``paper_2608_19659_amd.fleetsieve``.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SIZE = {"f32": 4, "f16": 2, "bf16": 2}
+TINY = 2.0 ** -100  # a row or block whose largest magnitude is below this counts as zero
+LARGEST_LINEAR = 8192 * 20480 * 5120
+LARGEST_PAIRS = 2 * 2048 * 40 * 8192 * 128
+LARGEST_CACHE = 64 * 8192 * 8 * 128
+LARGEST_APPEND = 8192 * 56 * 128
+
+
+def listed():
+    return [
+        # One user's token through the fused query/key/value projection, whole model on one GPU: latency.
+        dict(name="linear-1token-qkv", kind="linear", M=1, N=7168, K=5120, dtype="bf16", out="bf16", bias=False),
+        # A batch of 64 decoding users through a feed-forward matrix of the TP4 shard: the weights' bytes.
+        dict(name="linear-64tokens-TP4", kind="linear", M=64, N=5120, K=5120, dtype="bf16", out="bf16", bias=False),
+        # A ragged chunk with sizes that are a multiple of nothing, 32-bit outputs and a bias.
+        dict(name="linear-odd", kind="linear", M=333, N=1001, K=1999, dtype="f16", out="f32", bias=True),
+        # A prefill of 8192 tokens through the first feed-forward matrix: the largest product.
+        dict(name="linear-prefill", kind="linear", M=8192, N=20480, K=5120, dtype="bf16", out="bf16", bias=False),
+        # A decode step of 64 users on the TP4 shard: one new token each, into pages that are partly full.
+        dict(name="append-64users-TP4", kind="append", S=64, new=1, old=100, spread="ragged", Hq=10, Hkv=2, D=128,
+             R=128, page=64, dtype="bf16"),
+        # Four prompts of 2048 tokens enter the cache at once, whole model on one GPU.
+        dict(name="append-prefill", kind="append", S=4, new=2048, old=0, spread="equal", Hq=40, Hkv=8, D=128, R=128,
+             page=64, dtype="bf16"),
+        # A mixed step: one prompt chunk beside decoding users, small heads, pages of 16, a half of each head rotated.
+        dict(name="append-mixed", kind="append", S=17, new=301, old=75, spread="mixed", Hq=15, Hkv=5, D=64, R=32,
+             page=16, dtype="f16"),
+        # One user on the TP8 shard (5 query heads over 1): the shortest call.
+        dict(name="attention-1user-TP8", kind="attention", S=1, q=1, ctx=1000, spread="equal", Hq=5, Hkv=1, D=128,
+             page=64, window=0, dtype="bf16"),
+        # 64 decoding users with contexts of 512 to 8192 tokens, whole model on one GPU.
+        dict(name="attention-64users", kind="attention", S=64, q=1, ctx=8192, spread="ragged", Hq=40, Hkv=8, D=128,
+             page=64, window=0, dtype="bf16"),
+        # Four users with 131072 tokens each on the TP4 shard: few rows, a long axis.
+        dict(name="attention-long-TP4", kind="attention", S=4, q=1, ctx=131072, spread="equal", Hq=10, Hkv=2, D=128,
+             page=64, window=0, dtype="bf16"),
+        # Two prompts' chunks of 2048 tokens over 8192 tokens of context: the matrix products.
+        dict(name="attention-chunk", kind="attention", S=2, q=2048, ctx=8192, spread="equal", Hq=40, Hkv=8, D=128,
+             page=64, window=0, dtype="bf16"),
+        # A mixed step: a chunk beside decoding users and places of a graph that hold none, no shared heads,
+        # pages of 16, a window of 1000 tokens.
+        dict(name="attention-mixed-window", kind="attention", S=11, q=389, ctx=4001, spread="mixed", Hq=12, Hkv=12,
+             D=64, page=16, window=1000, dtype="f16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    """One more case: projections of 1 to 8192 tokens and 64 to 20480 channels,
+    appends of 1 to 256 sequences with 1 to 2048 new tokens, attention of 1 to
+    256 sequences over 1 to 131072 tokens; cut to the listed cases' work."""
+    kind = rng.choice(["linear", "linear", "append", "attention", "attention", "attention"])
+    dtype = rng.choice(["bf16", "bf16", "f16"])
+    if kind == "linear":
+        M, N, K = _log(rng, 1, 8192), _log(rng, 64, 20480), _log(rng, 64, 20480)
+        if rng.random() < 0.6:  # shard sizes are multiples of 64, others of nothing
+            N, K = -(-N // 64) * 64, -(-K // 64) * 64
+        M = max(1, min(M, LARGEST_LINEAR // (N * K)))
+        return dict(kind=kind, M=M, N=N, K=K, dtype=dtype, out=rng.choice([dtype, dtype, "f32"]),
+                    bias=rng.random() < 0.3)
+    Hkv, group = rng.choice([1, 2, 4, 5, 8, 12]), rng.choice([1, 3, 4, 5, 8])
+    D, page = rng.choice([64, 128, 128]), rng.choice([16, 32, 64, 64])
+    c = dict(kind=kind, S=_log(rng, 1, 256), Hq=Hkv * group, Hkv=Hkv, D=D, page=page, dtype=dtype)
+    c["spread"] = rng.choice(["equal", "ragged", "mixed"])
+    decode = rng.random() < 0.6
+    if kind == "append":
+        c["new"] = 1 if decode else _log(rng, 1, 2048)
+        c["old"] = rng.randint(0, 200)
+        c["R"] = rng.choice([D, D, D // 2, 0])
+        full = c["S"] * (c["new"] + c["old"]) * (c["Hq"] + 2 * Hkv) * D
+        if full > LARGEST_APPEND:
+            c["S"] = max(1, c["S"] * LARGEST_APPEND // full)
+        return c
+    c["q"] = 1 if decode else _log(rng, 2, 2048)
+    c["ctx"] = max(c["q"], _log(rng, 1, 131072 if decode else 16384))
+    c["window"] = 0 if rng.random() < 0.7 else _log(rng, 16, 4096)
+    full = c["S"] * c["ctx"] * Hkv * D
+    if full > LARGEST_CACHE:
+        c["S"] = max(1, c["S"] * LARGEST_CACHE // full)
+    full = c["S"] * c["ctx"] * c["q"] * c["Hq"] * D
+    if full > LARGEST_PAIRS:
+        c["S"] = max(1, c["S"] * LARGEST_PAIRS // full)
+        c["q"] = max(1, min(c["q"], LARGEST_PAIRS // (c["S"] * c["ctx"] * c["Hq"] * D)))
+    return c
+
+
+def _lengths(c):
+    """Each sequence's (new tokens, tokens in the cache with the new ones): a
+    function of the case alone.  ``mixed``: one sequence with all the new
+    tokens beside sequences with one, and every fifth place empty (its cache
+    length 0, its token a filler)."""
+    new_max, whole = (c["new"], c["old"] + c["new"]) if c["kind"] == "append" else (c["q"], c["ctx"])
+    rng = random.Random(1000 * c["S"] + whole)
+    got = []
+    for s in range(c["S"]):
+        if c["spread"] == "equal":
+            got.append((new_max, whole))
+            continue
+        if c["kind"] == "append":
+            n = new_max if s == 0 or c["spread"] == "ragged" else 1
+            got.append((n, n + rng.randint(0, c["old"])))
+            continue
+        length = whole if s == 0 else _log(rng, max(1, whole // 16), whole)
+        n = min(new_max, length) if s == 0 or c["spread"] == "ragged" else 1
+        got.append((n, 0) if c["spread"] == "mixed" and s % 5 == 4 else (n, length))
+    return got
+
+
+# ------------------------------------------------------------------ inputs --
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed) * 7919 + 17)
+    return g
+
+
+def _normal(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def _int32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _codes(g, shape):
+    """8-bit codes of about normal values, and their block scales' spread."""
+    out = torch.empty(shape, dtype=torch.int8, device="cuda")
+    for part in out.view(-1).split(1 << 28):
+        part.copy_((_normal(g, part.numel()) * 36.0).round_().clamp_(-127, 127))
+    return out
+
+
+def _cache(c, g, seed, lengths):
+    """A paged cache that holds the sequences' tokens in pages of a random
+    order, with unused pages between, and the table of each sequence's pages."""
+    page = c["page"]
+    need = [-(-total // page) for _, total in lengths]
+    n_pages = sum(need) + 3
+    order = list(range(n_pages))
+    random.Random(seed).shuffle(order)
+    table, at = [], 0
+    for n in need:
+        table.append(order[at:at + n] + [-1] * (max(need) - n if max(need) else 1))
+        at += n
+    shape = (n_pages, c["Hkv"])
+    scale = lambda lo, hi: (torch.rand(shape, generator=g, device="cuda") * (hi - lo) + lo) / 127.0  # noqa: E731
+    return dict(k=_codes(g, (*shape, page, c["D"])), v=_codes(g, (*shape, c["D"], page)), k_scale=scale(2.0, 4.5),
+                v_scale=scale(2.0, 4.5), table=table, n_pages=n_pages)
+
+
+def _context():
+    from paper_2608_19659_amd import fleetsieve as fs
+    if "ctx" not in _context.__dict__:
+        _context.ctx = fs.Context(torch.cuda.current_device())
+    return fs, _context.ctx
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    c, dt = case, DTYPES[case["dtype"]]
+    s = dict(case=case)
+    if c["kind"] == "linear":
+        # activations with a few large channels, as a decoder's residual stream has
+        channel = torch.where(torch.rand(c["K"], generator=g, device="cuda") < 0.01, 8.0, 1.0)
+        s["x"] = (_normal(g, c["M"], c["K"]) * channel).to(dt)
+        s["w"] = _codes(g, (c["N"], c["K"]))
+        s["w_scale"] = (torch.rand(c["N"], generator=g, device="cuda") + 0.5) / (36.0 * math.sqrt(c["K"]))
+        s["bias"] = _normal(g, c["N"]) if c["bias"] else None
+        if own:
+            fs, ctx = _context()
+            s["plan"] = fs.LinearPlan(ctx, s["x"], s["w"], s["w_scale"], bias=s["bias"], out_dtype=DTYPES[c["out"]])
+        return s
+    lengths = _lengths(c)
+    cache = _cache(c, g, seed, lengths)
+    s.update(cache)
+    new = [n for n, _ in lengths]
+    starts = [0]
+    for n in new:
+        starts.append(starts[-1] + n)
+    T = starts[-1]
+    s["cu_q"], s["max_q"] = _int32(starts), max(new)
+    # a fused projection's rows hold q, k and v side by side
+    Hq, Hkv, D = c["Hq"], c["Hkv"], c["D"]
+    rows = (_normal(g, T, Hq + 2 * Hkv, D) * 1.2).to(dt)
+    s["q"], s["k_new"], s["v_new"] = rows[:, :Hq], rows[:, Hq:Hq + Hkv], rows[:, Hq + Hkv:]
+    if c["kind"] == "append":
+        positions = [p for n, total in lengths for p in range(total - n, total)]
+        place = lambda q, p: cache["table"][q][p // c["page"]] * c["page"] + p % c["page"]  # noqa: E731
+        s["positions"] = _int32(positions)
+        s["slots"] = _int32([place(i, p) for i, (n, total) in enumerate(lengths) for p in range(total - n, total)])
+        s["all_slots"] = _int32([place(i, p) for i, (n, total) in enumerate(lengths) for p in range(total)])
+        reach, half = max(total for _, total in lengths), max(1, c["R"] // 2)
+        angle = torch.arange(reach, device="cuda", dtype=torch.float64)[:, None] * 10000.0 ** (
+            -torch.arange(half, device="cuda", dtype=torch.float64) / half)
+        s["cos"], s["sin"] = (angle.cos().float(), angle.sin().float()) if c["R"] else (None, None)
+    else:
+        s["block_table"], s["ctx_lens"] = _int32(cache["table"]), _int32([total for _, total in lengths])
+        s["scale"] = 1.0 / math.sqrt(D)
+    del s["table"]
+    if own:
+        fs, ctx = _context()
+        kv = fs.KVCache(s["k"], s["v"], s["k_scale"], s["v_scale"])
+        if c["kind"] == "append":
+            s["plan"] = fs.AppendPlan(ctx, kv, s["k_new"], s["v_new"], s["slots"], q=s["q"], positions=s["positions"],
+                                      cos=s["cos"], sin=s["sin"])
+            s["read"] = fs.ReadPlan(ctx, kv, s["all_slots"])
+        else:
+            s["plan"] = fs.AttentionPlan(ctx, kv, s["q"], s["block_table"], s["ctx_lens"], s["cu_q"], s["max_q"],
+                                         scale=s["scale"], window=c["window"])
+    return s
+
+
+# -------------------------------------------------------------- plain forms --
+def _plain_linear(s):
+    x = s["x"].float()
+    most = x.abs().amax(dim=1, keepdim=True)
+    live = ~(most < TINY)
+    codes = torch.where(live, torch.round(x * (127.0 / most)), torch.zeros_like(x))
+    scale = torch.where(live, most / 127.0, torch.zeros_like(most))
+    y = (codes @ s["w"].float().t()) * scale * s["w_scale"]
+    if s["bias"] is not None:
+        y = y + s["bias"]
+    return y.to(DTYPES[s["case"]["out"]])
+
+
+def _rotated(x, cos, sin, positions):
+    x = x.float()
+    if cos is None:
+        return x
+    at = positions.long()
+    co, si, h = cos[at][:, None, :], sin[at][:, None, :], cos.shape[1]
+    a, b = x[..., :h], x[..., h:2 * h]
+    return torch.cat([a * co - b * si, b * co + a * si, x[..., 2 * h:]], dim=-1)
+
+
+def _plain_enter(codes, scales, x, slots):
+    """`x` [T, H, D] enters codes [pages, H, page, D] at `slots`, in place."""
+    page = codes.shape[2]
+    at, slot = slots.long() // page, slots.long() % page
+    n, H = codes.shape[0], codes.shape[1]
+    most = torch.zeros(n, H, device=x.device).index_reduce_(0, at, x.abs().amax(dim=2), "amax")
+    first = torch.full((n,), page, device=x.device).index_reduce_(0, at, slot, "amin")
+    touched = first < page
+    old = torch.where((first == 0)[:, None], torch.zeros_like(scales), scales)
+    made = torch.where(most < TINY, torch.zeros_like(most), most / 127.0)
+    new = torch.where(touched[:, None], torch.maximum(old, made), scales)
+    ratio = torch.where(new > 0, old / new, torch.zeros_like(new))
+    kept = torch.round(codes.float() * ratio[:, :, None, None]).to(torch.int8)
+    codes.copy_(torch.where((touched[:, None] & (new != scales))[:, :, None, None], kept, codes))
+    inverse = torch.where(new > 0, 1.0 / new, torch.zeros_like(new))
+    codes[at, :, slot] = torch.round(x * inverse[at][:, :, None]).clamp(-127, 127).to(torch.int8)
+    scales.copy_(new)
+
+
+def _plain_append(s):
+    c = s["case"]
+    q = _rotated(s["q"], s["cos"], s["sin"], s["positions"]).to(DTYPES[c["dtype"]])
+    _plain_enter(s["k"], s["k_scale"], _rotated(s["k_new"], s["cos"], s["sin"], s["positions"]), s["slots"])
+    v = s["v"].transpose(2, 3).contiguous()
+    _plain_enter(v, s["v_scale"], s["v_new"].float(), s["slots"])
+    s["v"].copy_(v.transpose(2, 3))
+    at, slot = s["all_slots"].long() // c["page"], s["all_slots"].long() % c["page"]
+    k = s["k"][at, :, slot].float() * s["k_scale"][at][:, :, None]
+    v = s["v"][at, :, :, slot].float() * s["v_scale"][at][:, :, None]
+    return dict(q=q, k=k, v=v)
+
+
+def _plain_attention(s):
+    c = s["case"]
+    S, Hkv, D, page = c["S"], c["Hkv"], c["D"], c["page"]
+    group, longest = c["Hq"] // Hkv, s["block_table"].shape[1] * page
+    starts, ctx = s["cu_q"].long(), s["ctx_lens"].long()
+    n_new = starts[1:] - starts[:-1]
+    token = torch.arange(longest, device="cuda")
+    at = s["block_table"].long().clamp(min=0)[:, token // page]  # [S, N]
+    slot = (token % page).expand_as(at)
+    k = (s["k"][at, :, slot].float() * s["k_scale"][at][..., None]).transpose(1, 2).contiguous()  # [S, Hkv, N, D]
+    v = (s["v"][at, :, :, slot].float() * s["v_scale"][at][..., None]).transpose(1, 2).contiguous()
+    j = torch.arange(s["max_q"], device="cuda")
+    rows = (starts[:-1, None] + j).clamp(max=s["q"].shape[0] - 1)
+    q = s["q"].float()[rows]  # [S, J, Hq, D]
+    q = q.view(S, -1, Hkv, group, D).permute(0, 2, 1, 3, 4).reshape(S, Hkv, -1, D)
+    score = torch.matmul(q, k.transpose(2, 3)).view(S, Hkv, -1, group, longest).mul_(s["scale"])
+    position = (ctx - n_new)[:, None] + j  # [S, J]
+    seen = (token <= position[..., None]) & (token < ctx[:, None, None])
+    if c["window"]:
+        seen &= token > position[..., None] - c["window"]
+    seen = seen[:, None, :, None, :]
+    score.masked_fill_(~seen, -math.inf)
+    most = score.amax(dim=-1, keepdim=True)
+    p = score.sub_(torch.where(torch.isinf(most), torch.zeros_like(most), most)).exp_()
+    total = p.sum(dim=-1, keepdim=True)
+    o = torch.matmul(p.view(S, Hkv, -1, longest), v).view(S, Hkv, -1, group, D)
+    o = o / torch.where(total > 0, total, torch.ones_like(total))
+    o = o.permute(0, 2, 1, 3, 4).reshape(S, -1, c["Hq"], D)
+    of = torch.repeat_interleave(torch.arange(S, device="cuda"), n_new)
+    return o[of, torch.arange(s["q"].shape[0], device="cuda") - starts[of]].to(DTYPES[c["dtype"]])
+
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        out = state["plan"].run()
+        if kind == "append":
+            k, v = state["read"].run()
+            return dict(q=out, k=k, v=v)
+        return out
+    return {"linear": _plain_linear, "append": _plain_append, "attention": _plain_attention}[kind](state)
+
+
+# ---------------------------------------------------------------- the floor --
+def _visible(c):
+    """(tokens that some query of each sequence sees, pairs of a query token
+    and a token that it sees), summed over the sequences."""
+    tokens = pairs = 0
+    w = c["window"] or 1 << 60
+    for n, total in _lengths(c):
+        first = total - n
+        if total <= 0:
+            continue
+        tokens += total - max(0, first - w + 1)
+        full = min(max(w - 1 - first, 0), n)  # queries that see fewer than w tokens
+        pairs += full * first + full * (full + 1) // 2 + (n - full) * (w if n > full else 0)
+    return tokens, pairs
+
+
+def work(case):
+    c, b = case, SIZE[case["dtype"]]
+    if c["kind"] == "linear":
+        M, N, K = c["M"], c["N"], c["K"]
+        return dict(bytes=M * K * b + N * K + 4 * N + M * N * SIZE[c["out"]] + (4 * N if c["bias"] else 0),
+                    flops=2 * M * N * K)
+    lengths = _lengths(c)
+    T = sum(n for n, _ in lengths)
+    if c["kind"] == "append":
+        held = sum(total for _, total in lengths)
+        rows = T * c["D"] * ((2 * c["Hq"] + 2 * c["Hkv"]) * b + 2 * c["Hkv"])
+        table = 4 * c["R"] * max(total for _, total in lengths)
+        return dict(bytes=rows + table + 8 * T + 2 * held * c["Hkv"] * c["D"] * (1 + 4), flops=3 * T * c["R"] * (
+            c["Hq"] + c["Hkv"]) + 4 * T * c["Hkv"] * c["D"])
+    tokens, pairs = _visible(c)
+    pages = tokens // c["page"] + 1
+    return dict(bytes=2 * T * c["Hq"] * c["D"] * b + 2 * tokens * c["Hkv"] * c["D"] + pages * (4 + 8 * c["Hkv"]),
+                flops=4 * pairs * c["Hq"] * c["D"])
+
+
+# ---------------------------------------------------- definitions, 64 bits --
+def exact(case, seed):
+    s = prepare(case, seed)
+    c = case
+    if c["kind"] == "linear":
+        x = s["x"].double()
+        out = torch.empty(c["M"], c["N"], dtype=torch.float64, device="cuda")
+        w = s["w"].double() * s["w_scale"].double()[:, None]
+        for r in range(0, c["M"], 2048):
+            part = x[r:r + 2048]
+            step = part.abs().max(dim=1, keepdim=True).values / 127.0
+            step[step * 127.0 < TINY] = math.inf
+            held = (part / step).round()
+            out[r:r + 2048] = held.mul(torch.where(step.isinf(), 0.0, step)).matmul(w.T)
+        return out if s["bias"] is None else out + s["bias"].double()
+    if c["kind"] == "append":
+        page = c["page"]
+        turned = {}
+        for name in ("q", "k_new"):
+            x = s[name].double().clone()
+            if c["R"]:
+                h = c["R"] // 2
+                z = torch.complex(x[:, :, :h], x[:, :, h:2 * h])
+                turn = torch.complex(s["cos"].double(), s["sin"].double())[s["positions"].long()]
+                z = z * turn[:, None, :]
+                x[:, :, :h], x[:, :, h:2 * h] = z.real, z.imag
+            turned[name] = x
+        whole = []
+        for codes, scales, x in ((s["k"], s["k_scale"], turned["k_new"]), (s["v"].transpose(2, 3), s["v_scale"],
+                                                                           s["v_new"].double())):
+            parts, at, row = [], 0, 0
+            every = s["all_slots"].tolist()
+            for n, total in _lengths(c):
+                mine = every[row:row + total]
+                got = torch.empty(total, c["Hkv"], c["D"], dtype=torch.float64, device="cuda")
+                for p in range(0, total, page):
+                    q, end = mine[p] // page, min(total, p + page)
+                    first = max(p, total - n)  # the page's first new token
+                    old = codes[q, :, :first - p].double().transpose(0, 1)
+                    step = scales[q].double()
+                    if first < end:
+                        new = x[at + first - (total - n):at + end - (total - n)]
+                        step = step if first > p else torch.zeros_like(step)
+                        grown = torch.maximum(step, new.abs().amax(dim=(0, 2)) / 127.0)
+                        safe = torch.where(grown > 0, grown, 1.0)[None, :, None]
+                        if first > p:
+                            old = torch.where((grown > step)[None, :, None], (old * step[None, :, None] / safe).round(), old)
+                        got[first:end] = (new / safe).round().clamp(-127, 127) * grown[None, :, None]
+                        step = grown
+                    got[p:first if first < end else end] = old[:end - p] * step[None, :, None]
+                parts.append(got)
+                at, row = at + n, row + total
+            whole.append(torch.cat(parts))
+        return dict(q=turned["q"], k=whole[0], v=whole[1])
+    T, group, page = s["q"].shape[0], c["Hq"] // c["Hkv"], c["page"]
+    out = torch.zeros(T, c["Hq"], c["D"], dtype=torch.float64, device="cuda")
+    row = 0
+    for i, (n, total) in enumerate(_lengths(c)):
+        ids = s["block_table"][i, :-(-total // page)].long()
+        for h in range(c["Hkv"] if total else 0):
+            k = (s["k"][ids, h].double() * s["k_scale"][ids, h].double()[:, None, None]).reshape(-1, c["D"])[:total]
+            v = (s["v"][ids, h].double() * s["v_scale"][ids, h].double()[:, None, None]).transpose(1, 2).reshape(
+                -1, c["D"])[:total]
+            place = torch.arange(total - n, total, device="cuda")[:, None]
+            token = torch.arange(total, device="cuda")[None]
+            hidden = (token > place) | (token <= place - (c["window"] or 1 << 40))
+            for q in range(h * group, (h + 1) * group):
+                score = s["q"][row:row + n, q].double() @ k.T * s["scale"]
+                out[row:row + n, q] = torch.softmax(score.masked_fill(hidden, -math.inf), dim=1) @ v
+        row += n
+    return out
