@@ -241,12 +241,19 @@ def prepare(case, seed):
 
 
 # -------------------------------------------------------------- plain forms --
+def _over(a, b):
+    """a / b, either a number: one rounding (a division by a number, or of one,
+    would go by a rounded reciprocal)."""
+    a, b = torch.broadcast_tensors(*(x if isinstance(x, torch.Tensor) else torch.tensor(x, device="cuda") for x in (a, b)))
+    return a / b
+
+
 def _plain_linear(s):
     x = s["x"].float()
     most = x.abs().amax(dim=1, keepdim=True)
     live = ~(most < TINY)
-    codes = torch.where(live, torch.round(x * (127.0 / most)), torch.zeros_like(x))
-    scale = torch.where(live, most / 127.0, torch.zeros_like(most))
+    codes = torch.where(live, torch.round(x * _over(127.0, most)), torch.zeros_like(x))
+    scale = torch.where(live, _over(most, 127.0), torch.zeros_like(most))
     y = (codes @ s["w"].float().t()) * scale * s["w_scale"]
     if s["bias"] is not None:
         y = y + s["bias"]
@@ -272,12 +279,12 @@ def _plain_enter(codes, scales, x, slots):
     first = torch.full((n,), page, device=x.device).index_reduce_(0, at, slot, "amin")
     touched = first < page
     old = torch.where((first == 0)[:, None], torch.zeros_like(scales), scales)
-    made = torch.where(most < TINY, torch.zeros_like(most), most / 127.0)
+    made = torch.where(most < TINY, torch.zeros_like(most), _over(most, 127.0))
     new = torch.where(touched[:, None], torch.maximum(old, made), scales)
     ratio = torch.where(new > 0, old / new, torch.zeros_like(new))
     kept = torch.round(codes.float() * ratio[:, :, None, None]).to(torch.int8)
     codes.copy_(torch.where((touched[:, None] & (new != scales))[:, :, None, None], kept, codes))
-    inverse = torch.where(new > 0, 1.0 / new, torch.zeros_like(new))
+    inverse = torch.where(new > 0, _over(1.0, new), torch.zeros_like(new))
     codes[at, :, slot] = torch.round(x * inverse[at][:, :, None]).clamp(-127, 127).to(torch.int8)
     scales.copy_(new)
 
