@@ -473,6 +473,138 @@ fs_status fs_profile_loop(fs_context *ctx, const fs_problem *p, fs_intervals iv,
                           fs_loop_out out, void *d_workspace, size_t workspace_bytes,
                           hipStream_t stream);
 
+/* ---- Serving operators -------------------------------------------------
+ *
+ * What a profiled cell spends its time in: the operators of one decode or
+ * prefill step of a tensor-parallel shard whose weights and key/value cache
+ * are held in 8-bit integers.  A shard of TP degree t has 1/t of the heads
+ * and of the feed-forward channels, so one GPU times the step of any degree.
+ *
+ * They take device memory with strides in elements and follow the
+ * conventions above.  Codes are signed 8-bit integers, a code c under a scale
+ * s stands for c * s.  Elements are FS_F32, FS_F16 or FS_BF16; sums, softmax
+ * statistics and scales are binary32 or 32-bit integers, results are rounded
+ * once, to nearest even, when they are stored.  No size may exceed 2^31 - 1;
+ * offsets are 64-bit.  A call with nothing to do (no rows, no tokens) returns
+ * FS_OK and enqueues nothing. */
+typedef enum fs_dtype { FS_F32 = 0, FS_F16 = 1, FS_BF16 = 2 } fs_dtype;
+
+/* Codes of each row of x [rows][cols] (row stride x_stride >= cols), with one
+ * scale a row: a = max |x|, scale = a / 127, code = x * (127 / a) rounded to
+ * nearest even.  A row with a < 2^-100 gets scale 0 and codes 0; one with a
+ * NaN or an infinity gets a scale that is not finite, so that its products
+ * are NaN.  Codes have row stride code_stride >= cols; bytes between cols and
+ * code_stride are not written. */
+fs_status fs_quantize_rows(fs_context *ctx, const void *d_x, fs_dtype type, int64_t rows, int64_t cols,
+                           int64_t x_stride, int8_t *d_codes, int64_t code_stride, float *d_scale,
+                           hipStream_t stream);
+
+/* Largest inner dimension of fs_scaled_matmul: sums of products stay below
+ * 2^31 for any codes. */
+#define FS_MAX_INNER 131071
+
+/* out[m][n] = (sum_k a[m][k] * w[n][k]) * a_scale[m] * w_scale[n] + bias[n]:
+ * the sum exact in 32-bit integers, then rounded to binary32, multiplied by
+ * the scales in this order, and the bias added (d_bias NULL: none).  a is
+ * [M][K], w [N][K] (both rows contiguous, strides >= K), out [M][N] of
+ * out_type with stride >= N.  Any alignment is accepted; rows that start on
+ * multiples of 16 bytes are faster.  Bitwise equal run to run. */
+fs_status fs_scaled_matmul_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
+fs_status fs_scaled_matmul(fs_context *ctx, const int8_t *d_a, int64_t a_stride, const float *d_a_scale,
+                           const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
+                           int64_t M, int64_t N, int64_t K, void *d_out, fs_dtype out_type, int64_t out_stride,
+                           void *d_workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* fs_quantize_rows of x [M][K], then fs_scaled_matmul with the codes (kept in
+ * the workspace): the same bits as the two calls. */
+fs_status fs_linear_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
+fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const int8_t *d_w,
+                    int64_t w_stride, const float *d_w_scale, const float *d_bias, int64_t M, int64_t N, int64_t K,
+                    void *d_out, fs_dtype out_type, int64_t out_stride, void *d_workspace, size_t workspace_bytes,
+                    hipStream_t stream);
+
+/* A paged cache of keys and values in 8 bits with one scale for each page and
+ * head.  Slot number = page * page_size + place in the page.  Values lie with
+ * the tokens of a page adjacent, so that a product over tokens reads whole
+ * words.  head_dim is 64 or 128, page_size 16, 32 or 64 (FS_ERR_UNSUPPORTED
+ * otherwise); k and v start on multiples of 16 bytes.  A scale below 2^-110
+ * stands for a page of zeros. */
+typedef struct fs_kv_cache {
+  int8_t *k;       /* [n_pages][n_heads][page_size][head_dim] */
+  int8_t *v;       /* [n_pages][n_heads][head_dim][page_size] */
+  float *k_scale;  /* [n_pages][n_heads]                      */
+  float *v_scale;  /* [n_pages][n_heads]                      */
+  int32_t n_pages, n_heads, head_dim, page_size;
+} fs_kv_cache;
+
+/* Rotates the queries and keys of n_tokens new tokens to their positions and
+ * appends keys and values to the cache.
+ *
+ * k, v: [n_tokens][n_heads][head_dim] with a token stride (heads adjacent);
+ * q: [n_tokens][n_q_heads][head_dim] likewise, or NULL; q_out
+ * [n_tokens][n_q_heads][head_dim] contiguous, of the same type (may not
+ * overlap q).  Rotation of the first rotary_dim (even, <= head_dim, 0 = none)
+ * elements, h = rotary_dim / 2, i < h, position p:
+ *   x'[i] = x[i] cos[p][i] - x[i+h] sin[p][i],  x'[i+h] = x[i+h] cos[p][i] + x[i] sin[p][i]
+ * each product and sum rounded to binary32; cos, sin are [n_positions][h].
+ *
+ * Token t enters slot d_slots[t]; a negative slot leaves the cache as it is
+ * (its query is rotated all the same).  Tokens of one page must be adjacent
+ * in the batch, in slots that follow one another.  A page whose first new
+ * token is its slot 0 starts empty; otherwise it holds its slots below the
+ * first new one.  The page's scale becomes s' = max(s, max |new| / 127); where
+ * it grows, the codes held become rint(c * (s / s')); new codes are
+ * rint(x * (1 / s')), at most 127 in magnitude (keys from their rotated
+ * binary32 values).
+ *
+ * With FS_VALIDATE=1 slots outside the cache, positions outside [0,
+ * n_positions) and tokens of a page that do not follow one another are
+ * refused (the call waits for the stream); otherwise such slots are left out
+ * and such positions count as the nearest valid one. */
+fs_status fs_cache_append(fs_context *ctx, const fs_kv_cache *cache, const void *d_k, int64_t k_stride,
+                          const void *d_v, int64_t v_stride, const void *d_q, int64_t q_stride, int32_t n_q_heads,
+                          fs_dtype type, int64_t n_tokens, const int32_t *d_slots, const int32_t *d_positions,
+                          const float *d_cos, const float *d_sin, int32_t n_positions, int32_t rotary_dim,
+                          void *d_q_out, hipStream_t stream);
+
+/* The values that the cache holds at n_tokens slots, code * scale:
+ * k_out, v_out [n_tokens][n_heads][head_dim] of `type` (either may be NULL).
+ * A slot outside the cache gives zeros (refused with FS_VALIDATE=1). */
+fs_status fs_cache_read(fs_context *ctx, const fs_kv_cache *cache, int64_t n_tokens, const int32_t *d_slots,
+                        void *d_k_out, void *d_v_out, fs_dtype type, hipStream_t stream);
+
+/* Largest number of sequences of one fs_cache_attention call. */
+#define FS_MAX_SEQUENCES 4096
+
+/* Causal attention of n_seqs sequences' new tokens over the cache.
+ *
+ * The new tokens of sequence s are rows cu_q[s] .. cu_q[s+1] of q
+ * [n_tokens][n_q_heads][head_dim] (token stride q_stride, FS_F16 or FS_BF16);
+ * they are the last ones of the ctx_lens[s] tokens that the cache holds for
+ * it, in pages block_table[s][0 ..] (row length table_width).  n_q_heads is a
+ * multiple of the cache's n_heads, query head i reads cache head
+ * i / (n_q_heads / n_heads).  The query at position p sees tokens
+ * max(0, p - window + 1) .. p (window 0: all up to p); softmax of
+ * scale * <q, k> over them weighs the values.  A query that sees nothing
+ * (its sequence's ctx_lens is smaller than its number of new tokens) gets
+ * zeros.  out: [n_tokens][n_q_heads][head_dim] contiguous, of q's type.
+ * Entries of the block table that no query sees are not used as pages, nor
+ * their scales.
+ *
+ * Queries and probabilities enter the products as pairs of 8-bit integers
+ * (15 bits against the row's or block's largest) or as binary16 values, the
+ * sums are exact or binary32.  Results are equal run to run.
+ *
+ * With FS_VALIDATE=1 lengths and pages outside their ranges are refused (the
+ * call waits for the stream); otherwise they are clamped. */
+fs_status fs_cache_attention_workspace_size(const fs_kv_cache *cache, int32_t n_q_heads, int64_t n_tokens,
+                                            int32_t n_seqs, size_t *bytes);
+fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const void *d_q, int64_t q_stride,
+                             fs_dtype type, int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs,
+                             const int32_t *d_cu_q, const int32_t *d_ctx_lens, const int32_t *d_block_table,
+                             int64_t table_width, int32_t max_q, float scale, int32_t window, void *d_out,
+                             void *d_workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

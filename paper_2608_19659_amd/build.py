@@ -9,16 +9,19 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfleetsieve.so")
-SOURCES = [os.path.join(CSRC, "fs_kernels.hip"), os.path.join(CSRC, "fs_api.cpp")]
+SOURCES = [os.path.join(CSRC, n) for n in ("fs_kernels.hip", "fs_linear.hip", "fs_cache.hip", "fs_attention.hip",
+                                           "fs_api.cpp", "fs_serving_api.cpp")]
 
 HIP_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off", "-fno-fast-math",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
@@ -31,12 +34,18 @@ def hipcc() -> str:
 
 
 def build_library(extra_flags=(), out: str = LIB, verbose: bool = False) -> str:
-    """Compile libfleetsieve.so (always recompiles)."""
+    """Compile libfleetsieve.so (always recompiles; the sources side by side)."""
     tmp = out + ".tmp"
-    cmd = [hipcc(), *HIP_FLAGS, *extra_flags, *SOURCES, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), file=sys.stderr)
-    subprocess.run(cmd, check=True, cwd=HERE)
+    with tempfile.TemporaryDirectory(prefix="fleetsieve_") as work:
+        objects = [os.path.join(work, os.path.basename(src) + ".o") for src in SOURCES]
+        compiles = [[hipcc(), *HIP_FLAGS, *extra_flags, "-c", src, "-o", obj] for src, obj in zip(SOURCES, objects)]
+        link = [hipcc(), *HIP_FLAGS, *extra_flags, "-shared", *objects, "-o", tmp]
+        if verbose:
+            for cmd in (*compiles, link):
+                print(" ".join(cmd), file=sys.stderr)
+        with ThreadPoolExecutor(max_workers=4) as pool:
+            list(pool.map(lambda cmd: subprocess.run(cmd, check=True, cwd=HERE), compiles))
+        subprocess.run(link, check=True, cwd=HERE)
     os.replace(tmp, out)
     return out
 

@@ -1,0 +1,119 @@
+// fs_serving.h -- the serving operators' launchers (host) and the element
+// conversions their kernels share.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace fs {
+
+enum Dtype : int32_t { kF32 = 0, kF16 = 1, kBF16 = 2 };
+
+// A row or block whose largest magnitude is below this counts as zero.
+constexpr float kTiny = 0x1p-100f;
+// A page scale below this stands for a page of zeros.
+constexpr float kZeroScale = 0x1p-110f;
+
+struct QuantizeArgs {
+  const void *x;
+  int8_t *codes;
+  float *scale;
+  int64_t x_stride, code_stride;
+  int32_t rows, cols, type;
+};
+hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s);
+
+struct MatmulArgs {
+  const int8_t *a, *w;
+  const float *a_scale, *w_scale, *bias;
+  void *out;
+  int64_t a_stride, w_stride, out_stride;
+  int32_t M, N, K, out_type;
+};
+size_t matmul_workspace(int32_t M, int32_t N, int32_t K);
+hipError_t launch_scaled_matmul(const MatmulArgs &A, void *ws, hipStream_t s);
+
+struct Cache {
+  int8_t *k, *v;
+  float *k_scale, *v_scale;
+  int32_t n_pages, n_heads, head_dim, page_shift;  // page size = 1 << page_shift
+};
+
+struct AppendArgs {
+  Cache c;
+  const void *k, *v, *q;
+  void *q_out;
+  const int32_t *slots, *positions;
+  const float *cosines, *sines;
+  int64_t k_stride, v_stride, q_stride;
+  int32_t n_tokens, n_q_heads, type, n_positions, half;
+};
+hipError_t launch_cache_append(const AppendArgs &A, hipStream_t s);
+
+struct ReadArgs {
+  Cache c;
+  const int32_t *slots;
+  void *k_out, *v_out;
+  int32_t n_tokens, type;
+};
+hipError_t launch_cache_read(const ReadArgs &A, hipStream_t s);
+
+struct AttendArgs {
+  Cache c;
+  const void *q;
+  void *out;
+  const int32_t *cu_q, *ctx_lens, *table;
+  int64_t q_stride, table_width;
+  int32_t n_tokens, n_seqs, n_q_heads, max_q, window, type;
+  float scale;
+};
+size_t attention_workspace(const Cache &c, int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs);
+hipError_t launch_cache_attention(const AttendArgs &A, void *ws, hipStream_t s);
+
+// FS_VALIDATE=1: counts what is out of range into the validation words
+// (flag_address) of the current device, which the caller cleared.
+hipError_t flag_address(int32_t **flag);
+hipError_t launch_clear_flag(int32_t *flag, hipStream_t s);
+hipError_t launch_check_slots(const Cache &c, const int32_t *slots, const int32_t *positions, int32_t n_positions,
+                              int32_t n_tokens, int appending, int32_t *flag, hipStream_t s);
+hipError_t launch_check_attention(const AttendArgs &A, int32_t *flag, hipStream_t s);
+
+#ifdef __HIPCC__
+using half8 = _Float16 __attribute__((ext_vector_type(8)));
+using float4v = float __attribute__((ext_vector_type(4)));
+using float16v = float __attribute__((ext_vector_type(16)));
+using int4v = int __attribute__((ext_vector_type(4)));
+
+// Element types by their number: 2-byte types travel as raw 16-bit words.
+__device__ __forceinline__ float bf16_value(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ uint16_t bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+__device__ __forceinline__ float f16_value(uint16_t w) { return (float)__builtin_bit_cast(_Float16, w); }
+__device__ __forceinline__ uint16_t f16_bits(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
+
+template <int TYPE>
+__device__ __forceinline__ float load_value(const void *p, int64_t i) {
+  if constexpr (TYPE == kF32) return ((const float *)p)[i];
+  else if constexpr (TYPE == kF16) return f16_value(((const uint16_t *)p)[i]);
+  else return bf16_value(((const uint16_t *)p)[i]);
+}
+template <int TYPE>
+__device__ __forceinline__ void store_value(void *p, int64_t i, float v) {
+  if constexpr (TYPE == kF32) ((float *)p)[i] = v;
+  else if constexpr (TYPE == kF16) ((uint16_t *)p)[i] = f16_bits(v);
+  else ((uint16_t *)p)[i] = bf16_bits(v);
+}
+// The 16-bit pattern of a value in a 2-byte type, and back.
+template <int TYPE>
+__device__ __forceinline__ uint16_t bits16(float v) {
+  if constexpr (TYPE == kF16) return f16_bits(v);
+  else return bf16_bits(v);
+}
+template <int TYPE>
+__device__ __forceinline__ float value16(uint16_t w) {
+  if constexpr (TYPE == kF16) return f16_value(w);
+  else return bf16_value(w);
+}
+#endif
+
+}  // namespace fs

@@ -40,7 +40,9 @@ EXPORTED = ("fs_context_create", "fs_context_destroy", "fs_context_set_option", 
             "fs_certify", "fs_loop_workspace_size", "fs_profile_loop", "fs_reduce_cells", "fs_reduce_samples",
             "fs_solve_batch_lex", "fs_certify_lex", "fs_refit_intervals", "fs_loop_refit_workspace_size",
             "fs_score_lex_workspace_size", "fs_score_candidates_lex", "fs_clamp_samples",
-            "fs_score_candidates_noalloc")
+            "fs_score_candidates_noalloc", "fs_quantize_rows", "fs_scaled_matmul_workspace_size", "fs_scaled_matmul",
+            "fs_linear_workspace_size", "fs_linear", "fs_cache_append", "fs_cache_read",
+            "fs_cache_attention_workspace_size", "fs_cache_attention")
 POLICY_SCORE, POLICY_ORDER = 0, 1
 CELL_SECONDS = 300.0
 
@@ -121,6 +123,18 @@ def load_library():
     Q = ctypes.POINTER(_SloPolicy)
     lib.fs_reduce_cells.argtypes = [vp, P, Q, vp, vp, i64, vp, vp]
     lib.fs_reduce_samples.argtypes = [vp, P, Q, vp, i32, vp, vp, i32, i32, vp, vp]
+    C = ctypes.POINTER(_Cache)
+    psz = ctypes.POINTER(sz)
+    lib.fs_quantize_rows.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, vp, vp]
+    lib.fs_scaled_matmul_workspace_size.argtypes = [i64, i64, i64, psz]
+    lib.fs_scaled_matmul.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.fs_linear_workspace_size.argtypes = [i64, i64, i64, psz]
+    lib.fs_linear.argtypes = [vp, vp, i32, i64, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.fs_cache_append.argtypes = [vp, C, vp, i64, vp, i64, vp, i64, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp]
+    lib.fs_cache_read.argtypes = [vp, C, i64, vp, vp, vp, i32, vp]
+    lib.fs_cache_attention_workspace_size.argtypes = [C, i32, i64, i32, psz]
+    lib.fs_cache_attention.argtypes = [vp, C, vp, i64, i32, i32, i64, i32, vp, vp, vp, i64, i32, ctypes.c_float, i32,
+                                       vp, vp, sz, vp]
     for name in EXPORTED:
         if name != "fs_context_destroy":
             getattr(lib, name).restype = ctypes.c_int
@@ -681,3 +695,293 @@ def reduce_samples(ctx: Context, problem, policy, cand, tail_s, succ_s=None, out
     float32 [O, E, S, M] device tensor, succ_s float32 [O, E, S] or None;
     returns float32 [O, E, S]."""
     return ReducePlan.samples(ctx, problem, policy, cand, tail_s, succ_s, out, stream).run()
+
+
+# ------------------------------------------------------- serving operators --
+F32, F16, BF16 = 0, 1, 2
+MAX_INNER = 131071
+MAX_SEQUENCES = 4096
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+def _invalid(message):
+    return FleetSieveError(FS_ERR_INVALID_ARGUMENT, message)
+
+
+def _element_type(dtype):
+    torch = _torch()
+    types = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    if dtype not in types:
+        raise _invalid(f"elements must be float32, float16 or bfloat16, got {dtype}")
+    return types[dtype]
+
+
+def _rows(t, shape, name, dtype=None):
+    """(pointer, stride of the first dimension) of a device tensor of this
+    shape (None: any size) whose other dimensions are adjacent in memory."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise _invalid(f"{name} must be a torch tensor on a ROCm device")
+    if dtype is not None and t.dtype != dtype:
+        raise _invalid(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != len(shape) or any(want is not None and want != got for want, got in zip(shape, t.shape)):
+        raise _invalid(f"{name} must have shape {tuple('any' if n is None else n for n in shape)}, got {tuple(t.shape)}")
+    step = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != step:
+            raise _invalid(f"{name} must be contiguous in all but its first dimension")
+        step *= size
+    # a single row's stride is of no account
+    return t.data_ptr(), (int(t.stride(0)) if t.shape[0] > 1 else step)
+
+
+def _same_device(ctx, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.is_cuda and t.device.index != ctx.device:
+            raise _invalid(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
+
+
+def quantize_rows(ctx: Context, x, stream=None):
+    """(codes int8 [rows, cols], scale float32 [rows]) of a matrix with a
+    scale for each row (fs_quantize_rows)."""
+    torch = _torch()
+    p, stride = _rows(x, (None, None), "x")
+    _same_device(ctx, x=x)
+    rows, cols = (int(n) for n in x.shape)
+    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(load_library().fs_quantize_rows(ctx.handle, p, _element_type(x.dtype), rows, cols, stride, codes.data_ptr(),
+                                           cols, scale.data_ptr(), _stream(x.device, stream)))
+    return codes, scale
+
+
+def _size(fn, *args):
+    out = ctypes.c_size_t()
+    _check(fn(*args, ctypes.byref(out)))
+    return int(out.value)
+
+
+class _Plan:
+    """A call with its arguments checked and marshalled once; run() enqueues
+    it again on the same device buffers, whose contents may change between
+    runs, and returns its output."""
+
+    def run(self):
+        _check(self._fn(*self._args))
+        return self.out
+
+
+class MatmulPlan(_Plan):
+    """out[m, n] = (sum_k a[m, k] w[n, k]) a_scale[m] w_scale[n] + bias[n]
+    (fs_scaled_matmul): a int8 [M, K], w int8 [N, K], float32 scales and bias."""
+
+    def __init__(self, ctx: Context, a, a_scale, w, w_scale, bias=None, out_dtype=None, out=None, stream=None,
+                 workspace=None):
+        torch = _torch()
+        pa, sa = _rows(a, (None, None), "a", torch.int8)
+        M, K = (int(n) for n in a.shape)
+        pw, sw = _rows(w, (None, K), "w", torch.int8)
+        N = int(w.shape[0])
+        if out is None:
+            out = torch.empty((M, N), dtype=out_dtype or torch.bfloat16, device=a.device)
+        po, so = _rows(out, (M, N), "out", out_dtype)
+        _same_device(ctx, a=a, w=w, out=out)
+        lib = load_library()
+        need = _size(lib.fs_scaled_matmul_workspace_size, M, N, K)
+        ws = workspace if workspace is not None else ctx.workspace(need)
+        self.out, self._keep = out, (a, a_scale, w, w_scale, bias, ws)
+        self._fn = lib.fs_scaled_matmul
+        self._args = (ctx.handle, pa, sa, _dev_ptr(a_scale, torch.float32, (M,), "a_scale"), pw, sw,
+                      _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
+                      M, N, K, po, _element_type(out.dtype), so, ws.data_ptr(), ws.numel(), _stream(a.device, stream))
+
+
+def scaled_matmul(ctx: Context, a, a_scale, w, w_scale, bias=None, out_dtype=None, out=None, stream=None,
+                  workspace=None):
+    """fs_scaled_matmul, one call (see MatmulPlan)."""
+    return MatmulPlan(ctx, a, a_scale, w, w_scale, bias, out_dtype, out, stream, workspace).run()
+
+
+class LinearPlan(_Plan):
+    """A projection in 8-bit integers (fs_linear): x [M, K] is quantised with
+    a scale for each row and multiplied by w int8 [N, K] with w_scale [N]."""
+
+    def __init__(self, ctx: Context, x, w, w_scale, bias=None, out_dtype=None, out=None, stream=None, workspace=None):
+        torch = _torch()
+        px, sx = _rows(x, (None, None), "x")
+        M, K = (int(n) for n in x.shape)
+        pw, sw = _rows(w, (None, K), "w", torch.int8)
+        N = int(w.shape[0])
+        if out is None:
+            out = torch.empty((M, N), dtype=out_dtype or x.dtype, device=x.device)
+        po, so = _rows(out, (M, N), "out", out_dtype)
+        _same_device(ctx, x=x, w=w, out=out)
+        lib = load_library()
+        need = _size(lib.fs_linear_workspace_size, M, N, K)
+        ws = workspace if workspace is not None else ctx.workspace(need)
+        self.out, self._keep = out, (x, w, w_scale, bias, ws)
+        self._fn = lib.fs_linear
+        self._args = (ctx.handle, px, _element_type(x.dtype), sx, pw, sw,
+                      _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
+                      M, N, K, po, _element_type(out.dtype), so, ws.data_ptr(), ws.numel(), _stream(x.device, stream))
+
+
+def linear(ctx: Context, x, w, w_scale, bias=None, out_dtype=None, out=None, stream=None, workspace=None):
+    """fs_linear, one call (see LinearPlan)."""
+    return LinearPlan(ctx, x, w, w_scale, bias, out_dtype, out, stream, workspace).run()
+
+
+@dataclass
+class KVCache:
+    """A paged cache of keys and values in 8 bits with a scale for each page
+    and head: k int8 [pages, heads, page_size, head_dim], v int8 [pages, heads,
+    head_dim, page_size], k_scale and v_scale float32 [pages, heads]."""
+    k: object
+    v: object
+    k_scale: object
+    v_scale: object
+
+    @staticmethod
+    def empty(n_pages: int, n_heads: int, head_dim: int, page_size: int, device) -> "KVCache":
+        torch = _torch()
+        z = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=device)
+        return KVCache(z((n_pages, n_heads, page_size, head_dim), torch.int8),
+                       z((n_pages, n_heads, head_dim, page_size), torch.int8),
+                       z((n_pages, n_heads), torch.float32), z((n_pages, n_heads), torch.float32))
+
+    @property
+    def page_size(self) -> int:
+        return int(self.k.shape[2])
+
+    @property
+    def n_heads(self) -> int:
+        return int(self.k.shape[1])
+
+    @property
+    def head_dim(self) -> int:
+        return int(self.k.shape[3])
+
+    def _struct(self):
+        torch = _torch()
+        if self.k.dim() != 4:
+            raise _invalid("k must be [pages, heads, page_size, head_dim]")
+        P, H, S, D = (int(n) for n in self.k.shape)
+        return _Cache(_dev_ptr(self.k, torch.int8, (P, H, S, D), "k"), _dev_ptr(self.v, torch.int8, (P, H, D, S), "v"),
+                      _dev_ptr(self.k_scale, torch.float32, (P, H), "k_scale"),
+                      _dev_ptr(self.v_scale, torch.float32, (P, H), "v_scale"), P, H, D, S)
+
+
+class AppendPlan(_Plan):
+    """Rotates a step's queries and keys to their positions and appends keys
+    and values to the cache (fs_cache_append).  k, v [T, heads, head_dim] and
+    q [T, query heads, head_dim] may be parts of wider rows; slots and
+    positions int32 [T]; cos, sin float32 [positions, rotary_dim / 2], None for
+    no rotation.  run() returns the rotated queries (None without q)."""
+
+    def __init__(self, ctx: Context, cache: KVCache, k, v, slots, q=None, positions=None, cos=None, sin=None,
+                 q_out=None, stream=None):
+        torch = _torch()
+        self._cache = cache._struct()
+        T = int(k.shape[0])
+        shape = (T, cache.n_heads, cache.head_dim)
+        pk, sk = _rows(k, shape, "k")
+        pv, sv = _rows(v, shape, "v", k.dtype)
+        pq, sq, po, heads = None, 0, None, 0
+        if q is not None:
+            pq, sq = _rows(q, (T, None, cache.head_dim), "q", k.dtype)
+            heads = int(q.shape[1])
+            if q_out is None:
+                q_out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+            po = _dev_ptr(q_out, q.dtype, (T, heads, cache.head_dim), "q_out")
+        reach = half = 0
+        if cos is not None:
+            if sin is None or positions is None:
+                raise _invalid("a rotation needs positions, cos and sin")
+            if cos.dim() != 2:
+                raise _invalid("cos must be [positions, rotary_dim / 2]")
+            reach, half = (int(n) for n in cos.shape)
+        _same_device(ctx, k=k, v=v, q=q, slots=slots, cache=cache.k)
+        self.out, self._keep = (q_out if q is not None else None), (cache, k, v, q, slots, positions, cos, sin)
+        self._fn = load_library().fs_cache_append
+        self._args = (ctx.handle, ctypes.byref(self._cache), pk, sk, pv, sv, pq, sq, heads, _element_type(k.dtype), T,
+                      _dev_ptr(slots, torch.int32, (T,), "slots"), _dev_ptr(positions, torch.int32, (T,), "positions"),
+                      _dev_ptr(cos, torch.float32, (reach, half), "cos"),
+                      _dev_ptr(sin, torch.float32, (reach, half), "sin") if cos is not None else None, reach, 2 * half,
+                      po, _stream(k.device, stream))
+
+
+def cache_append(ctx: Context, cache: KVCache, k, v, slots, q=None, positions=None, cos=None, sin=None, q_out=None,
+                 stream=None):
+    """fs_cache_append, one call (see AppendPlan)."""
+    return AppendPlan(ctx, cache, k, v, slots, q, positions, cos, sin, q_out, stream).run()
+
+
+class ReadPlan(_Plan):
+    """The values that the cache holds at slots int32 [T] (fs_cache_read):
+    run() returns (k, v) [T, heads, head_dim], float32 by default."""
+
+    def __init__(self, ctx: Context, cache: KVCache, slots, dtype=None, out=None, stream=None):
+        torch = _torch()
+        self._cache = cache._struct()
+        T = int(slots.shape[0])
+        shape = (T, cache.n_heads, cache.head_dim)
+        dtype = dtype or torch.float32
+        if out is None:
+            out = tuple(torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+        _same_device(ctx, slots=slots, cache=cache.k)
+        self.out, self._keep = out, (cache, slots)
+        self._fn = load_library().fs_cache_read
+        self._args = (ctx.handle, ctypes.byref(self._cache), T, _dev_ptr(slots, torch.int32, (T,), "slots"),
+                      _dev_ptr(out[0], dtype, shape, "k_out"), _dev_ptr(out[1], dtype, shape, "v_out"),
+                      _element_type(dtype), _stream(cache.k.device, stream))
+
+
+def cache_read(ctx: Context, cache: KVCache, slots, dtype=None, out=None, stream=None):
+    """fs_cache_read, one call (see ReadPlan)."""
+    return ReadPlan(ctx, cache, slots, dtype, out, stream).run()
+
+
+class AttentionPlan(_Plan):
+    """Causal attention of packed new tokens over the cache
+    (fs_cache_attention): q [T, query heads, head_dim] (may be part of wider
+    rows), block_table int32 [sequences, width], ctx_lens int32 [sequences]
+    (tokens in the cache, the new ones among them), cu_q int32 [sequences + 1],
+    max_q the largest number of new tokens of a sequence.  scale defaults to
+    head_dim ** -0.5; window 0 means none."""
+
+    def __init__(self, ctx: Context, cache: KVCache, q, block_table, ctx_lens, cu_q, max_q: int, scale=None,
+                 window: int = 0, out=None, stream=None, workspace=None):
+        torch = _torch()
+        self._cache = cache._struct()
+        pq, sq = _rows(q, (None, None, cache.head_dim), "q")
+        T, heads = int(q.shape[0]), int(q.shape[1])
+        S = int(ctx_lens.shape[0])
+        if block_table.dim() != 2:
+            raise _invalid("block_table must be [sequences, width]")
+        width = int(block_table.shape[1])
+        if out is None:
+            out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+        po = _dev_ptr(out, q.dtype, (T, heads, cache.head_dim), "out")
+        _same_device(ctx, q=q, block_table=block_table, ctx_lens=ctx_lens, cu_q=cu_q, cache=cache.k)
+        lib = load_library()
+        need = _size(lib.fs_cache_attention_workspace_size, ctypes.byref(self._cache), heads, T, S)
+        ws = workspace if workspace is not None else ctx.workspace(need)
+        self.out, self._keep = out, (cache, q, block_table, ctx_lens, cu_q, ws)
+        self._fn = lib.fs_cache_attention
+        self._args = (ctx.handle, ctypes.byref(self._cache), pq, sq, _element_type(q.dtype), heads, T, S,
+                      _dev_ptr(cu_q, torch.int32, (S + 1,), "cu_q"), _dev_ptr(ctx_lens, torch.int32, (S,), "ctx_lens"),
+                      _dev_ptr(block_table, torch.int32, (S, width), "block_table"), width, int(max_q),
+                      float(cache.head_dim ** -0.5 if scale is None else scale), int(window), po, ws.data_ptr(),
+                      ws.numel(), _stream(q.device, stream))
+
+
+def cache_attention(ctx: Context, cache: KVCache, q, block_table, ctx_lens, cu_q, max_q: int, scale=None,
+                    window: int = 0, out=None, stream=None, workspace=None):
+    """fs_cache_attention, one call (see AttentionPlan)."""
+    return AttentionPlan(ctx, cache, q, block_table, ctx_lens, cu_q, max_q, scale, window, out, stream, workspace).run()
