@@ -5,6 +5,11 @@
 // y[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n] + bias[n].
 // The sum is exact in 32-bit integers whatever the order, so tiles, splits
 // and instructions are free to choose and every variant gives the same bits.
+//
+// In all variants the weights are the instruction's first operand, so a
+// lane's four results are neighbouring channels of one token.
+#include <algorithm>
+
 #include "fs_serving.h"
 
 namespace fs {
@@ -17,116 +22,425 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 template <int THREADS>
 __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds) {
   for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
-  if constexpr (THREADS > 64) {
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int i = 1; i < THREADS / 64; ++i) v = max(v, lds[i]);
-  }
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lds[0];
+  for (int i = 1; i < THREADS / 64; ++i) v = max(v, lds[i]);
   return v;
 }
 
-// One block a row.
+// Eight neighbouring elements of a row, zeros from `cols` on; `whole`: rows
+// start on multiples of 16 bytes.
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs A) {
-  __shared__ uint32_t lds[4];
-  const int64_t row = blockIdx.x;
-  const int64_t at = row * A.x_stride;
+__device__ __forceinline__ void load8(const void *x, int64_t row, int c, int cols, bool whole, float (&v)[8]) {
+  if (c + 8 <= cols) {
+    if constexpr (TYPE == kF32) {
+      __builtin_memcpy(v, (const float *)x + row + c, 32);
+    } else {
+      const uint16_t *const p = (const uint16_t *)x + row + c;
+      const int4v raw = whole ? *(const int4v *)p : load16(p);
+      for (int i = 0; i < 8; ++i) v[i] = value16<TYPE>((uint16_t)(raw[i >> 1] >> 16 * (i & 1)));
+    }
+  } else {
+    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? load_value<TYPE>(x, row + c + i) : 0.0f;
+  }
+}
+
+__device__ __forceinline__ void store8(int8_t *out, int c, int cols, const float (&v)[8], float inverse) {
+  uint32_t word[2] = {0, 0};
+  for (int i = 0; i < 8; ++i) word[i >> 2] |= (uint32_t)((int)rintf(v[i] * inverse) & 0xff) << (8 * (i & 3));
+  if (c + 8 <= cols) {
+    __builtin_memcpy(out + c, word, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < cols) out[c + i] = (int8_t)(word[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+// One block a row, the row in registers: HELD groups of 8 elements a thread.
+// HELD = 0: a row too long for that is read twice (the second time from L2).
+template <int TYPE, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
+  __shared__ uint32_t lds[THREADS / 64];
+  const int64_t row = blockIdx.x, at = row * A.x_stride;
+  const int own = threadIdx.x * 8, step = THREADS * 8;
+  const bool whole = (((uintptr_t)A.x | (uintptr_t)(A.x_stride * 2)) & 15) == 0;
+  float v[HELD ? HELD : 1][8];
   uint32_t most = 0;
-  for (int c = threadIdx.x; c < A.cols; c += 256) most = max(most, magnitude(load_value<TYPE>(A.x, at + c)));
-  const float a = __uint_as_float(block_max<256>(most, lds));
+  if constexpr (HELD > 0) {
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) load8<TYPE>(A.x, at, min(own + j * step, A.cols), A.cols, whole, v[j]);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+      for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[j][i]));
+  } else {
+    for (int64_t c = own; c < A.cols; c += step) {
+      load8<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
+      for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[0][i]));
+    }
+  }
+  const float a = __uint_as_float(block_max<THREADS>(most, lds));
   const bool zero = a < kTiny;
   const float inverse = zero ? 0.0f : 127.0f / a;
-  int8_t *out = A.codes + row * A.code_stride;
-  for (int c = threadIdx.x; c < A.cols; c += 256) {
-    const float x = load_value<TYPE>(A.x, at + c);
-    out[c] = zero ? (int8_t)0 : (int8_t)(int)rintf(x * inverse);
+  int8_t *const out = A.codes + row * A.code_stride;
+  if constexpr (HELD > 0) {
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+      if (own + j * step < A.cols) store8(out, own + j * step, A.cols, v[j], inverse);
+  } else {
+    for (int64_t c = own; c < A.cols; c += step) {
+      load8<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
+      store8(out, (int)c, A.cols, v[0], inverse);
+    }
   }
   if (threadIdx.x == 0) A.scale[row] = zero ? 0.0f : a / 127.0f;
 }
 
-// 16 codes of a row from column k on, zeros beyond its end.  Rows may start
-// anywhere: the load is one of 16 bytes at any alignment.
-__device__ __forceinline__ int4v codes16(const int8_t *row, int k, int K) {
-  int4v v = {0, 0, 0, 0};
-  if (k + 16 <= K) {
-    __builtin_memcpy(&v, row + k, 16);
-  } else {
-    for (int i = 0; i < 16; ++i)
-      if (k + i < K) v[i >> 2] |= (int)((uint32_t)(uint8_t)row[k + i] << (8 * (i & 3)));
-  }
-  return v;
-}
+// 16 codes of a row (of K > 0) from column k on.  load() only asks for the
+// words, so that loads follow one another; codes() waits and shifts.  A stage
+// that passes the row's end (`over`) takes the row's last 16, and shifts zeros
+// in.
+struct Piece {
+  Words words;
 
+  __device__ __forceinline__ void load(const int8_t *row, int k, int K, bool over) {
+    if (!over) {
+      words.load(row + k);
+    } else if (K >= 16) {
+      words.load(row + min(k, K - 16));
+    } else {  // a short row: byte by byte
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 15; ++i)
+        if (i < K) w[i >> 2] |= (uint32_t)(uint8_t)row[i] << 8 * (i & 3);
+      words.set(int4v{(int)w[0], (int)w[1], (int)w[2], (int)w[3]});
+    }
+  }
+  __device__ __forceinline__ int4v codes(int k, int K, bool over) const {
+    const int4v v = words.value();
+    if (!over) return v;
+    const int beyond = k - max(0, min(k, K - 16));
+    const unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v);
+    return __builtin_bit_cast(int4v, beyond < 16 ? w >> beyond * 8 : (unsigned __int128)0);
+  }
+};
+
+// Four neighbouring channels from n (a multiple of 4) on of token m.
 template <int TYPE>
-__device__ __forceinline__ void store_products(const MatmulArgs &A, int m, int n, int4v acc, float sa) {
-  // four neighbouring channels of one token
+__device__ __forceinline__ void store_products(const MatmulArgs &A, int m, int n, int4v acc, float sa, float4v sw,
+                                               float4v bias) {
   const int64_t at = (int64_t)m * A.out_stride + n;
-  for (int i = 0; i < 4; ++i)
-    if (n + i < A.N) {
-      float y = (float)acc[i] * sa * A.w_scale[n + i];
-      if (A.bias) y += A.bias[n + i];
-      store_value<TYPE>(A.out, at + i, y);
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = (float)acc[i] * sa * sw[i];
+    if (A.bias) y[i] += bias[i];
+  }
+  if (n + 4 <= A.N) {  // one store at any alignment
+    if constexpr (TYPE == kF32) {
+      __builtin_memcpy((float *)A.out + at, y, 16);
+    } else {
+      uint16_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = bits16<TYPE>(y[i]);
+      __builtin_memcpy((uint16_t *)A.out + at, h, 8);
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < A.N) store_value<TYPE>(A.out, at + i, y[i]);
+  }
 }
 
-// Tiles of 64 tokens x 64 channels, 128 inner elements at a time through LDS.
-// The weights are the instruction's first operand, so a lane's four results
-// are neighbours in a row of the output.  LDS rows of eight 16-byte chunks,
-// chunk c of row r at place c ^ ((r >> 1) & 7): the 16 rows that a quarter of
-// a wavefront reads fall on all 64 banks.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_matmul_tile(MatmulArgs A) {
-  __shared__ int4v la[64 * 8], lw[64 * 8];
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
-  int4v acc[2][2] = {};
-  for (int k0 = 0; k0 < A.K; k0 += 128) {
-    for (int i = 0; i < 2; ++i) {
-      const int chunk = threadIdx.x + 256 * i, r = chunk >> 3, c = chunk & 7;
-      const int to = r * 8 + (c ^ ((r >> 1) & 7)), k = k0 + c * 16;
-      la[to] = codes16(A.a + (int64_t)min(m0 + r, A.M - 1) * A.a_stride, k, A.K);
-      lw[to] = codes16(A.w + (int64_t)min(n0 + r, A.N - 1) * A.w_stride, k, A.K);
-    }
-    __syncthreads();
-    for (int kk = 0; kk < 2; ++kk) {
-      int4v fa[2], fw[2];
-      for (int i = 0; i < 2; ++i) {
-        const int c = kk * 4 + (lane >> 4), ra = wm + i * 16 + (lane & 15), rw = wn + i * 16 + (lane & 15);
-        fa[i] = la[ra * 8 + (c ^ ((ra >> 1) & 7))];
-        fw[i] = lw[rw * 8 + (c ^ ((rw >> 1) & 7))];
-      }
-      for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[j], fa[i], acc[i][j], 0, 0, 0);
-    }
-    __syncthreads();
+// -------------------------------------------------------- tiles through LDS --
+// Tiles of BM tokens x BN channels, BK inner elements a stage, a ring of NS
+// stages in LDS, all but one of them in flight while one is multiplied.  Loads
+// go straight to LDS, where a lane's place is fixed, so the lanes' addresses
+// carry the order: a row of BK bytes is BK / 16 chunks, chunk c of row r at
+// place c ^ turn(r), so that the 16 rows that a quarter of a wavefront reads
+// fall on all 64 banks.
+template <int BK>
+__device__ __forceinline__ int turn(int r) {
+  if constexpr (BK >= 256) return r & 15;
+  else if constexpr (BK == 128) return (r >> 1) & 7;
+  else return (r >> 2) & 3;
+}
+
+// 16 bytes a lane from base + offset to LDS: the wavefront's 1024 bytes from
+// `to` on, in lane order.  Counted like any load; the compiler does not know
+// of it, so arrive() waits.
+__device__ __forceinline__ void load_to_lds(const int8_t *base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+}
+
+// Waits until at most LOADS of this wavefront's loads are under way and its
+// LDS reads are done.
+template <int LOADS>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(LOADS < 64, "the counter has 6 bits");
+  __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 7 << 4);
+}
+
+// The same for a ring of NS stages of L loads each when `after` stages beyond
+// the wanted one are under way: the largest of a few counts that is enough.
+template <int NS, int L>
+__device__ __forceinline__ void wait_stage(int after) {
+  if (after >= NS - 2) wait_loads<(NS - 2) * L>();
+  else if (NS > 4 && after >= NS / 2) wait_loads<NS / 2 * L>();
+  else if (NS > 6 && after >= NS / 4) wait_loads<NS / 4 * L>();
+  else wait_loads<0>();
+}
+
+template <int TYPE_, int BM_, int BN_, int WM_, int WN_, int BK_, int WK_, int NS_>
+struct Shape {
+  static constexpr int TYPE = TYPE_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
+  // WK wavefronts share a part of the tile, each with its part of a stage:
+  // fewer, longer stages, where waiting for each is what costs
+  static constexpr int WK = WK_, TILES = (BM / WM) * (BN / WN);
+  static constexpr int WAVES = TILES * WK, THREADS = 64 * WAVES, MT = WM / 16, NT = WN / 16, CH = BK / 16;
+  static constexpr int LA = BM * CH / THREADS, LW = BN * CH / THREADS;  // loads of a thread a stage
+  static constexpr int PART_A = BM * BK, STAGE = (BM + BN) * BK, BYTES = NS * STAGE;
+  static_assert(BK % (64 * WK) == 0, "a part of a stage is whole steps");
+  static_assert(WK == 1 || WAVES * MT * NT * 1024 <= BYTES, "the parts' sums fit the ring");
+  static_assert(LA * THREADS == BM * CH && LW * THREADS == BN * CH && LA > 0 && LW > 0, "whole loads");
+};
+
+template <class S>
+__device__ __forceinline__ void multiply_stage(const int8_t *la, const int8_t *lw, int wm, int wn, int wk, int lane,
+                                               int4v (&acc)[S::MT][S::NT]) {
+  constexpr int STEPS = S::BK / 64 / S::WK;
+#pragma unroll
+  for (int kk = 0; kk < STEPS; ++kk) {
+    int4v fa[S::MT], fw[S::NT];
+    const int r = lane & 15, at = (((wk * STEPS + kk) * 4 + (lane >> 4)) ^ turn<S::BK>(r)) * 16;  // rows differ by multiples of 16
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i) fa[i] = *(const int4v *)(la + (wm + i * 16 + r) * S::BK + at);
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) fw[j] = *(const int4v *)(lw + (wn + j * 16 + r) * S::BK + at);
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[j], fa[i], acc[i][j], 0, 0, 0);
   }
-  for (int i = 0; i < 2; ++i) {
+}
+
+// Row and first inner element of a thread's i-th place in a part of a stage.
+template <class S>
+__device__ __forceinline__ int2 place(int i) {
+  const int slot = i * S::THREADS + threadIdx.x, r = slot / S::CH;
+  return {r, (slot % S::CH ^ turn<S::BK>(r)) * 16};
+}
+
+// DIRECT: rows start on multiples of 16 bytes.
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m, int tiles_n) {
+  __shared__ __attribute__((aligned(1024))) int8_t lds[S::BYTES];
+  // Workgroups go round the eight XCDs in turn: each XCD gets a run of tiles,
+  // in groups of eight rows of tiles, so that its L2 serves both operands.
+  const int total = tiles_m * tiles_n, per = (total + 7) / 8;
+  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  const int group = id / (8 * tiles_n), gm = min(8, tiles_m - group * 8), in = id - group * 8 * tiles_n;
+  const int m0 = (group * 8 + in % gm) * S::BM, n0 = in / gm * S::BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wk = wave / S::TILES, wt = wave % S::TILES;
+  const int wm = wt / (S::BN / S::WN) * S::WM, wn = wt % (S::BN / S::WN) * S::WN;
+  const int8_t *const ta = A.a + (int64_t)m0 * A.a_stride, *const tw = A.w + (int64_t)n0 * A.w_stride;
+  const int last_a = A.M - 1 - m0, last_w = A.N - 1 - n0;
+  int4v acc[S::MT][S::NT] = {};
+  int done = 0;
+
+  if constexpr (DIRECT) {
+    const int full = A.K / S::BK;
+    const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)lds + wave * 1024;
+    // a lane's places in a stage, from the tile's first row on (strides fit 32 bits: see matmul_as)
+    uint32_t oa[S::LA], ow[S::LW];
+#pragma unroll
+    for (int i = 0; i < S::LA; ++i) oa[i] = (uint32_t)min(place<S>(i).x, last_a) * (uint32_t)A.a_stride + place<S>(i).y;
+#pragma unroll
+    for (int i = 0; i < S::LW; ++i) ow[i] = (uint32_t)min(place<S>(i).x, last_w) * (uint32_t)A.w_stride + place<S>(i).y;
+    const auto load = [&](int t, int slot) {
+#pragma unroll
+      for (int i = 0; i < S::LA; ++i)
+        load_to_lds(ta + (int64_t)t * S::BK, oa[i], base + slot * S::STAGE + i * S::THREADS * 16);
+#pragma unroll
+      for (int i = 0; i < S::LW; ++i)
+        load_to_lds(tw + (int64_t)t * S::BK, ow[i], base + slot * S::STAGE + S::PART_A + i * S::THREADS * 16);
+    };
+    for (int t = 0; t < S::NS - 1 && t < full; ++t) load(t, t);
+    for (int t = 0, slot = 0; t < full; ++t, slot = slot == S::NS - 1 ? 0 : slot + 1) {
+      const int left = full - 1 - t;
+      wait_stage<S::NS, S::LA + S::LW>(left);
+      // all wavefronts' loads of stage t are there, and all have read stage t - 1
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (left >= S::NS - 1) load(t + S::NS - 1, slot ? slot - 1 : S::NS - 1);
+      multiply_stage<S>(lds + slot * S::STAGE, lds + slot * S::STAGE + S::PART_A, wm, wn, wk, lane, acc);
+    }
+    done = full * S::BK;
+  }
+  // Rows at any alignment, or their last part: through registers, AHEAD stages'
+  // loads under way (as many as there are registers for).
+  if (done < A.K) {
+    constexpr int AHEAD = DIRECT || S::MT * S::NT > 8 ? 1 : 2;
+    Piece ra[AHEAD][S::LA], rw[AHEAD][S::LW];
+    const int8_t *pa[S::LA], *pw[S::LW];
+#pragma unroll
+    for (int i = 0; i < S::LA; ++i) pa[i] = ta + (int64_t)min(place<S>(i).x, last_a) * A.a_stride;
+#pragma unroll
+    for (int i = 0; i < S::LW; ++i) pw[i] = tw + (int64_t)min(place<S>(i).x, last_w) * A.w_stride;
+    const auto fetch = [&](int p, int k) {
+      const bool over = k + S::BK > A.K;
+#pragma unroll
+      for (int i = 0; i < S::LA; ++i) ra[p][i].load(pa[i], k + place<S>(i).y, A.K, over);
+#pragma unroll
+      for (int i = 0; i < S::LW; ++i) rw[p][i].load(pw[i], k + place<S>(i).y, A.K, over);
+    };
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p)
+      if (done + p * S::BK < A.K) fetch(p, done + p * S::BK);
+    for (int k0 = done; k0 < A.K; k0 += AHEAD * S::BK) {
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p) {
+        const int k = k0 + p * S::BK;
+        if (k >= A.K) break;
+        const bool over = k + S::BK > A.K;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < S::LA; ++i)
+          *(int4v *)(lds + (i * S::THREADS + threadIdx.x) * 16) = ra[p][i].codes(k + place<S>(i).y, A.K, over);
+#pragma unroll
+        for (int i = 0; i < S::LW; ++i)
+          *(int4v *)(lds + S::PART_A + (i * S::THREADS + threadIdx.x) * 16) = rw[p][i].codes(k + place<S>(i).y, A.K, over);
+        __syncthreads();
+        if (k + AHEAD * S::BK < A.K) fetch(p, k + AHEAD * S::BK);
+        multiply_stage<S>(lds, lds + S::PART_A, wm, wn, wk, lane, acc);
+      }
+    }
+  }
+  if constexpr (S::WK > 1) {  // the parts' sums meet in LDS, each tile at its first wavefront
+    __syncthreads();
+    int4v *const sums = (int4v *)lds;
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) sums[(wave * S::MT * S::NT + i * S::NT + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j)
+        for (int p = 1; p < S::WK; ++p)
+          acc[i][j] += sums[((p * S::TILES + wave) * S::MT * S::NT + i * S::NT + j) * 64 + lane];
+  }
+  // the scales first, all loads under way together
+  float sa[S::MT];
+  float4v sw[S::NT], bias[S::NT];
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i) sa[i] = A.a_scale[min(m0 + wm + i * 16 + (lane & 15), A.M - 1)];
+  const auto channels = [&](const float *from, float4v (&to)[S::NT]) {
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[j][i] = from[min(n0 + wn + j * 16 + (lane >> 4) * 4 + i, A.N - 1)];
+  };
+  channels(A.w_scale, sw);
+  if (A.bias) channels(A.bias, bias);
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i) {
     const int m = m0 + wm + i * 16 + (lane & 15);
-    if (m >= A.M) continue;
-    const float sa = A.a_scale[m];
-    for (int j = 0; j < 2; ++j) store_products<TYPE>(A, m, n0 + wn + j * 16 + (lane >> 4) * 4, acc[i][j], sa);
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+      const int n = n0 + wn + j * 16 + (lane >> 4) * 4;
+      if (m < A.M && n < A.N) store_products<S::TYPE>(A, m, n, acc[i][j], sa[i], sw[j], bias[j]);
+    }
+  }
+}
+
+template <int TYPE, int THREADS, int HELD>
+hipError_t quantize_as(const QuantizeArgs &A, hipStream_t s) {
+  k_quantize_rows<TYPE, THREADS, HELD><<<A.rows, THREADS, 0, s>>>(A);
+  return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t quantize_of(const QuantizeArgs &A, hipStream_t s) {
+  // few rows: all of a CU's wavefronts on one; many: smaller blocks
+  if (A.rows <= 256 && A.cols <= 3 * 8192) return quantize_as<TYPE, 1024, 3>(A, s);
+  if (A.cols <= 4 * 2048) return quantize_as<TYPE, 256, 4>(A, s);
+  if (A.cols <= 10 * 2048) return quantize_as<TYPE, 256, 10>(A, s);
+  return quantize_as<TYPE, 1024, 0>(A, s);
+}
+
+template <int TYPE, int BM, int BN, int WM, int WN, int BK, int WK, int NS>
+hipError_t matmul_as(const MatmulArgs &A, hipStream_t s) {
+  using S = Shape<TYPE, BM, BN, WM, WN, BK, WK, NS>;
+  const int tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
+  const int64_t total = (int64_t)tm * tn, grid = (total + 7) / 8 * 8;
+  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const bool direct = (((uintptr_t)A.a | (uintptr_t)A.w | (uintptr_t)A.a_stride | (uintptr_t)A.w_stride) & 15) == 0 &&
+                      std::max(A.a_stride, A.w_stride) <= (1 << 23);
+  if (direct) k_matmul<S, true><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else k_matmul<S, false><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
+  return hipGetLastError();
+}
+
+// The tile whose rounds over the 256 CUs take least: a round's time is about
+// 1.5 us and, for each 5120 inner elements, what is measured with the tile at
+// one block a CU.  (K = 5120, us: 64 tokens x 5120 channels 9.6 with tiles of
+// 64 x 32, 11.0 with 32 x 32, 12.7 with 64 x 64; 64 x 896 4.2 with 16 x 16 and
+// 7.4 with 32 x 32; 128 x 5120 12.6 with 64 x 64, 16.4 with 64 x 32; 2048 x
+// 5120 70 with 128 x 64, 78 with 256 x 256; 8192 x 20480 831 with 256 x 256,
+// 951 with 256 x 128.)
+struct Tile {
+  int bm, bn;
+  double us;
+};
+constexpr Tile kTiles[] = {{16, 16, 2.4},  {16, 32, 5.5},   {32, 32, 6.1},    {64, 32, 8.1},   {64, 64, 11.1},
+                           {128, 64, 13.0}, {128, 128, 25.0}, {256, 128, 43.5}, {256, 256, 78.0}};
+
+int best_tile(int32_t M, int32_t N, int32_t K) {
+  int best = 0;
+  double least = 0.0;
+  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+    const Tile &t = kTiles[i];
+    const int64_t tiles = ((int64_t)(M + (int64_t)t.bm - 1) / t.bm) * ((N + (int64_t)t.bn - 1) / t.bn);
+    const double time = (double)((tiles + 255) / 256) * (1.5 + t.us * K / 5120.0);
+    if (i == 0 || time < least) {
+      best = i;
+      least = time;
+    }
+  }
+  return best;
+}
+
+template <int TYPE>
+hipError_t matmul_of(const MatmulArgs &A, hipStream_t s) {
+  switch (best_tile(A.M, A.N, A.K)) {
+    case 0: return matmul_as<TYPE, 16, 16, 16, 16, 512, 8, 4>(A, s);
+    case 1: return matmul_as<TYPE, 16, 32, 16, 16, 512, 4, 3>(A, s);
+    case 2: return matmul_as<TYPE, 32, 32, 16, 16, 512, 2, 4>(A, s);
+    case 3: return matmul_as<TYPE, 64, 32, 32, 16, 512, 2, 3>(A, s);
+    case 4: return matmul_as<TYPE, 64, 64, 32, 32, 256, 2, 4>(A, s);
+    case 5: return matmul_as<TYPE, 128, 64, 32, 32, 128, 1, 3>(A, s);
+    case 6: return matmul_as<TYPE, 128, 128, 32, 64, 128, 1, 3>(A, s);
+    case 7: return matmul_as<TYPE, 256, 128, 64, 64, 128, 1, 3>(A, s);
+    default: return matmul_as<TYPE, 256, 256, 128, 64, 128, 1, 2>(A, s);
   }
 }
 
 }  // namespace
 
 hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s) {
-  if (A.type == kF32) k_quantize_rows<kF32><<<A.rows, 256, 0, s>>>(A);
-  else if (A.type == kF16) k_quantize_rows<kF16><<<A.rows, 256, 0, s>>>(A);
-  else k_quantize_rows<kBF16><<<A.rows, 256, 0, s>>>(A);
-  return hipGetLastError();
+  return A.type == kF32 ? quantize_of<kF32>(A, s) : A.type == kF16 ? quantize_of<kF16>(A, s) : quantize_of<kBF16>(A, s);
 }
 
 size_t matmul_workspace(int32_t, int32_t, int32_t) { return 0; }
 
 hipError_t launch_scaled_matmul(const MatmulArgs &A, void *, hipStream_t s) {
-  const dim3 grid((A.N + 63) / 64, (A.M + 63) / 64);
-  if (A.out_type == kF32) k_matmul_tile<kF32><<<grid, 256, 0, s>>>(A);
-  else if (A.out_type == kF16) k_matmul_tile<kF16><<<grid, 256, 0, s>>>(A);
-  else k_matmul_tile<kBF16><<<grid, 256, 0, s>>>(A);
-  return hipGetLastError();
+  return A.out_type == kF32 ? matmul_of<kF32>(A, s) : A.out_type == kF16 ? matmul_of<kF16>(A, s) : matmul_of<kBF16>(A, s);
 }
 
 }  // namespace fs

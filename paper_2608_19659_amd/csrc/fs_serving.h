@@ -85,6 +85,36 @@ using float4v = float __attribute__((ext_vector_type(4)));
 using float16v = float __attribute__((ext_vector_type(16)));
 using int4v = int __attribute__((ext_vector_type(4)));
 
+// 16 bytes from any address: the five words that hold them, shifted when they
+// are there.  A load of 16 bytes off a word boundary takes the memory pipe
+// many times as long.  Only words of which a byte is wanted are read.
+struct Words {
+  int4v first;
+  uint32_t next, off;
+
+  __device__ __forceinline__ void load(const void *p) {
+    using int4w = int __attribute__((ext_vector_type(4), aligned(4)));
+    using Word = const __attribute__((address_space(1))) uint32_t;
+    off = (uint32_t)(uintptr_t)p & 3;
+    Word *const w = (Word *)((uintptr_t)p & ~(uintptr_t)3);
+    first = *(const __attribute__((address_space(1))) int4w *)w;
+    next = w[off ? 4 : 3];
+  }
+  __device__ __forceinline__ void set(int4v v) {
+    first = v;
+    next = off = 0;
+  }
+  __device__ __forceinline__ int4v value() const {
+    return int4v{(int)__builtin_amdgcn_alignbyte(first[1], first[0], off), (int)__builtin_amdgcn_alignbyte(first[2], first[1], off),
+                 (int)__builtin_amdgcn_alignbyte(first[3], first[2], off), (int)__builtin_amdgcn_alignbyte(next, first[3], off)};
+  }
+};
+__device__ __forceinline__ int4v load16(const void *p) {
+  Words w;
+  w.load(p);
+  return w.value();
+}
+
 // Element types by their number: 2-byte types travel as raw 16-bit words.
 __device__ __forceinline__ float bf16_value(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ uint16_t bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
