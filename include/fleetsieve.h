@@ -527,8 +527,8 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
  * head.  Slot number = page * page_size + place in the page.  Values lie with
  * the tokens of a page adjacent, so that a product over tokens reads whole
  * words.  head_dim is 64 or 128, page_size 16, 32 or 64 (FS_ERR_UNSUPPORTED
- * otherwise); k and v start on multiples of 16 bytes.  A scale below 2^-110
- * stands for a page of zeros. */
+ * otherwise); k and v start on multiples of 16 bytes.  Scales are
+ * not negative; one below 2^-110 stands for a page of zeros. */
 typedef struct fs_kv_cache {
   int8_t *k;       /* [n_pages][n_heads][page_size][head_dim] */
   int8_t *v;       /* [n_pages][n_heads][head_dim][page_size] */

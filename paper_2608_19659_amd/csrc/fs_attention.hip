@@ -2,8 +2,13 @@
 //
 // o_i = sum_j softmax_j(scale <q_i, K_j>) V_j with K_j = kscale * kcode_j and
 // V_j = vscale * vcode_j.  One pass over the tokens with the running maximum
-// and sum; the context is split over blocks when there are few rows, and a
-// second kernel joins the parts.
+// and sum; the context is cut over blocks, and of the blocks that have parts
+// of a row tile the last to arrive adds them up.
+#include <algorithm>
+#include <atomic>
+#include <chrono>
+#include <random>
+
 #include "fs_serving.h"
 
 namespace fs {
@@ -13,126 +18,285 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kFloor = -1e30f;  // a maximum over no tokens: finite, so differences stay numbers
 constexpr int kTile = 64;         // tokens of one step of a wavefront
 
-// ------------------------------------------------------------ the work list --
-// Work items: (sequence, tile of R rows, cache head, part of the context).
-// A row is a (new token, query head of the group) pair of one cache head.
-// Each block derives the same list from the lengths alone.
+// ------------------------------------------------------------ who does what --
+// An item is a tile of R rows of one sequence and cache head; a row is a (new
+// token, query head of the group) pair.  An item has as many units of work as
+// its sequence has 64-token tiles that some query sees (causal rows see fewer:
+// early and late row tiles alternate, which evens that out).  The units of all
+// items in a row are cut into equal runs, one a block, wherever the cuts fall,
+// so that ragged lengths leave no block with more to do.  A block writes an
+// item that lies within its run, and the unnormalised part of one that does
+// not: at most two, one at either end.  The last block to write a part of an
+// item adds them up, in their order, so that results do not depend on which
+// block that is.
+// All of this follows from the lengths alone, and each block derives it.
+// (Units are counted in 32 bits: launch_cache_attention sees to their number.)
+
+// Rows to (token, head of the group): a row tile's first row is divided once,
+// the few from there on by a multiplication (exact while group + 256 rows
+// times group stay below 2^32).
+struct Rows {
+  int token, head;  // of the first row
+  uint32_t group, per;
+
+  __device__ __forceinline__ Rows(int r0, int g, uint32_t inverse) : group(g), per(inverse) {
+    token = r0 / g;
+    head = r0 - token * g;
+  }
+  __device__ __forceinline__ int2 operator()(int i) const {
+    const uint32_t x = head + i, t = group == 1 ? x : __umulhi(x, per);
+    return {token + (int)t, (int)(x - t * group)};
+  }
+};
+
+constexpr int kItemUnits = 8;
 
 struct Seq {
-  int q0, n;         // first row of q, new tokens
-  int length;        // tokens in the cache
-  int t0, t1;        // 64-token tiles that some query sees
+  int q0, n;   // first row of q, new tokens
+  int length;  // tokens in the cache
+  int t0;      // first tile that some query sees
+  int units;   // tiles from there on; at least kItemUnits, which an item costs in any case
 };
 
 __device__ __forceinline__ Seq sequence(const AttendArgs &A, int s) {
   Seq q;
   q.q0 = min(max(A.cu_q[s], 0), A.n_tokens);
-  q.n = min(max(A.cu_q[s + 1], q.q0), A.n_tokens) - q.q0;
+  q.n = min(min(max(A.cu_q[s + 1], q.q0), A.n_tokens) - q.q0, A.max_q);
   const int64_t room = min(A.table_width << A.c.page_shift, (int64_t)0x7fffffc0);
   q.length = (int)min((int64_t)max(A.ctx_lens[s], 0), room);
   const int64_t first = (int64_t)q.length - q.n;
   const int64_t from = A.window ? max((int64_t)0, first - A.window + 1) : 0;
   q.t0 = (int)(from / kTile);
-  q.t1 = q.n ? (int)(((int64_t)q.length + kTile - 1) / kTile) : q.t0;
+  q.units = max(kItemUnits, (int)(((int64_t)q.length + kTile - 1) / kTile) - q.t0);
   return q;
 }
 
-struct List {
-  int items, partials;  // items in all; those of split contexts
-  int chunk;            // tiles an item has at most
+// What a kernel takes: sequences of lo .. hi - 1 rows, in runs of at least
+// `least` units.
+struct Share {
+  int least, lo, hi;
 };
 
-__device__ __forceinline__ int row_tiles(const Seq &q, int group, int R) { return (int)(((int64_t)q.n * group + R - 1) / R); }
-__device__ __forceinline__ int parts_of(const Seq &q, int chunk) { return max(1, (q.t1 - q.t0 + chunk - 1) / chunk); }
+__device__ __forceinline__ int row_tiles(const Seq &q, int group, int R, const Share &w) {
+  const int64_t rows = (int64_t)q.n * group;
+  return rows < w.lo || rows >= w.hi ? 0 : (int)((rows + R - 1) / R);
+}
 
-// Prefix sums over the sequences of items (pre) and of items of split
-// contexts (part), in LDS; all threads of the block call it.
+// Prefix sums of the sequences' units (pre, in LDS) and their total; all
+// threads of the block call it.
 template <int THREADS, int R>
-__device__ List make_list(const AttendArgs &A, int group, int target, int least, int *pre, int *part) {
-  __shared__ int64_t work[THREADS / 64];
-  __shared__ int2 carry[THREADS / 64];
+__device__ uint32_t list_units(const AttendArgs &A, int group, const Share &share, uint32_t *pre) {
+  __shared__ uint32_t carry[THREADS / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t heads = A.c.n_heads;
-  int64_t w = 0;
-  for (int s = threadIdx.x; s < A.n_seqs; s += THREADS) {
-    const Seq q = sequence(A, s);
-    w += heads * row_tiles(q, group, R) * (q.t1 - q.t0);
-  }
-  for (int o = 32; o; o >>= 1) w += __shfl_xor(w, o);
-  if (lane == 0) work[wave] = w;
-  __syncthreads();
-  w = 0;
-  for (int i = 0; i < THREADS / 64; ++i) w += work[i];
-  List L;
-  L.chunk = (int)min(max((w + target - 1) / target, (int64_t)least), (int64_t)0x3fffffff);
-  int2 base = {0, 0};
+  uint32_t base = 0;
   for (int s0 = 0; s0 < A.n_seqs; s0 += THREADS) {
     const int s = s0 + threadIdx.x;
-    int2 v = {0, 0};
+    uint32_t v = 0;
     if (s < A.n_seqs) {
       const Seq q = sequence(A, s);
-      const int parts = parts_of(q, L.chunk);
-      v.x = (int)heads * row_tiles(q, group, R) * parts;
-      v.y = parts > 1 ? v.x : 0;
+      v = (uint32_t)(A.c.n_heads * row_tiles(q, group, R, share)) * q.units;
     }
-    int2 sum = v;
+    uint32_t sum = v;
     for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(sum.x, o), y = __shfl_up(sum.y, o);
-      if (lane >= o) {
-        sum.x += x;
-        sum.y += y;
-      }
+      const uint32_t x = (uint32_t)__shfl_up((int)sum, o);
+      if (lane >= o) sum += x;
     }
     if (lane == 63) carry[wave] = sum;
     __syncthreads();
-    int2 before = base;
+    uint32_t before = base;
     for (int i = 0; i < THREADS / 64; ++i) {
-      if (i < wave) {
-        before.x += carry[i].x;
-        before.y += carry[i].y;
-      }
-      base.x += carry[i].x;
-      base.y += carry[i].y;
+      if (i < wave) before += carry[i];
+      base += carry[i];
     }
-    if (s < A.n_seqs) {
-      pre[s] = before.x + sum.x - v.x;
-      part[s] = before.y + sum.y - v.y;
-    }
+    if (s < A.n_seqs) pre[s] = before + sum - v;
     __syncthreads();
   }
-  L.items = base.x;
-  L.partials = base.y;
-  return L;
+  return base;
 }
 
-// The last sequence whose prefix is at most `item` (one with items: those
-// without share their prefix with the next).
-__device__ __forceinline__ int find(const int *prefix, int n, int item) {
-  int lo = 0, hi = n;
+__device__ __forceinline__ uint32_t run_length(uint32_t total, uint32_t blocks, const Share &share) {
+  return max((total + blocks - 1) / blocks, (uint32_t)share.least);
+}
+
+struct Item {
+  int s, h, r0;       // sequence, cache head, first row
+  uint32_t start;     // its first unit
+  uint32_t units;
+  Seq q;
+};
+
+// The item of a unit.  Sequences without units share their prefix with the
+// next, so the last one whose prefix is at most `unit` has it.
+template <int R>
+__device__ __forceinline__ Item item_at(const AttendArgs &A, int group, const Share &share, const uint32_t *pre, uint32_t unit) {
+  int lo = 0, hi = A.n_seqs;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (prefix[mid] <= item) lo = mid;
+    if (pre[mid] <= unit) lo = mid;
     else hi = mid;
   }
-  return lo;
+  Item it;
+  it.s = lo;
+  it.q = sequence(A, lo);
+  it.units = it.q.units;
+  const uint32_t rel = unit - pre[lo], at = rel / it.units;
+  it.start = pre[lo] + at * it.units;
+  const uint32_t tiles = row_tiles(it.q, group, R, share), k = at % tiles;
+  it.h = (int)(at / tiles);
+  it.r0 = (int)(k & 1 ? tiles - 1 - k / 2 : k / 2) * R;
+  return it;
 }
 
-// The tiles of part `ch` of `parts` of the tokens that rows r0 .. r1 - 1 see.
-__device__ __forceinline__ int2 tiles_of(const AttendArgs &A, const Seq &q, int group, int r0, int r1, int parts, int ch) {
-  const int64_t first = (int64_t)q.length - q.n;
-  const int64_t j0 = r0 / group, j1 = min((int64_t)q.n - 1, (int64_t)(r1 - 1) / group);
-  const int64_t end = min((int64_t)q.length, first + j1 + 1);
-  const int64_t from = A.window ? max((int64_t)0, first + j0 - A.window + 1) : 0;
-  if (end <= from) return {0, 0};
-  const int a = (int)(from / kTile), b = (int)((end + kTile - 1) / kTile);
-  const int len = (b - a + parts - 1) / parts;
-  return {min(b, a + ch * len), min(b, a + (ch + 1) * len)};
+// A cut costs a block about as much as 16 tiles.  Items that are small beside
+// a run, or where runs are short not much longer, are not cut: a cut within
+// one moves to its nearer end.
+__device__ __forceinline__ bool stays_whole(uint32_t units, uint32_t run) {
+  return units * 4 <= run || (run < 24 && units <= 2 * run);
 }
 
-// Workspace: per part of a split context the rows' maximum and sum, then
-// their unnormalised outputs.
+// The units of an item that a run up to `stop` does, from `unit` on (which
+// moves past them); false if there are none.
+__device__ __forceinline__ bool take(const Item &it, uint32_t run, uint32_t stop, uint32_t &unit, uint32_t &from, uint32_t &to) {
+  const uint32_t end = it.start + it.units;
+  from = unit - it.start;
+  to = min(it.units, from + stop - unit);
+  if (stays_whole(it.units, run)) {
+    const bool of_last = from > 0 && 2 * from >= it.units;                      // the run before has it
+    const bool of_next = stop < end && 2 * (stop - it.start) < it.units;        // the one after
+    from = 0;
+    to = it.units;
+    unit = end;
+    return !of_last && !of_next;
+  }
+  unit += to - from;
+  return true;
+}
+
+// The tiles of units from .. to - 1 of an item whose rows belong to the
+// sequence's new tokens j0 .. j1 that some of them see.
+__device__ __forceinline__ int2 tiles_of(const AttendArgs &A, const Seq &q, int j0, int j1, bool whole, int from, int to) {
+  const int first = q.length - q.n, end = min(q.length, first + j1 + 1);
+  const int low = A.window ? max(0, first + j0 - A.window + 1) : 0;
+  if (end <= low) return {0, 0};
+  const int a = low / kTile, b = (end + kTile - 1) / kTile;
+  if (whole) return {a, b};
+  return {max(a, q.t0 + from), min(b, q.t0 + to)};
+}
+
+// Workspace: a counter a run, then of each part of an item the rows' maximum
+// and sum and their unnormalised outputs.
 constexpr int kRows = 16;
 __host__ __device__ constexpr int64_t part_floats(int R, int D) { return (int64_t)R * (D + 2); }
+// A run's part of the item that it starts in the middle of, or that it leaves.
+__device__ __forceinline__ int64_t part_index(uint32_t run, bool from_start) { return 2 * (int64_t)run + from_start; }
+struct Parts {
+  unsigned long long *arrived;  // of the item that goes on beyond a run, by the run that it starts in
+  float *floats;
+  // The workspace comes with any contents, so a count is one only under the
+  // call's own number (52 bits, above 12 of the count); the last to arrive
+  // leaves 0, for a graph that runs the call again.
+  unsigned long long call;  // 0: the parts are left to k_join
+};
+
+// Workgroups go round the eight XCDs in turn: each XCD gets neighbouring runs
+// (grids are multiples of eight), so that row tiles of one head meet in its L2.
+__device__ __forceinline__ uint32_t run_of_block() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
+
+// Parts go from block to block, whose L2 may be another XCD's: they are stored
+// and read at the device's scope, two floats at a time, past the L2.  (A fence
+// would write back or drop all of an L2: 64 users 281 us instead of 80.)
+__device__ __forceinline__ void put(float *to, float a, float b) {
+  const unsigned long long v = __float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+  __hip_atomic_store((unsigned long long *)to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get(const float *from) {
+  const unsigned long long v =
+      __hip_atomic_load((unsigned long long *)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return {__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+
+// Whether this block is the last of `parts` to have written its part.
+__device__ __forceinline__ bool last_to_arrive(const Parts &P, uint32_t b0, int parts) {
+  __shared__ int last;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each wavefront's stores are done before the block counts as there
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned long long *const slot = P.arrived + b0;
+    unsigned long long seen = __hip_atomic_load(slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), now;
+    for (;;) {
+      now = ((seen & ~0xfffull) == P.call ? seen : P.call) + 1;
+      const unsigned long long was = atomicCAS(slot, seen, now);
+      if (was == seen) break;
+      seen = was;
+    }
+    last = (int)(now & 0xfff) == parts;
+    if (last) atomicExch(slot, 0ull);
+  }
+  __syncthreads();
+  return last;
+}
+
+// Adds up the parts of an item, four neighbouring elements a lane.  Where
+// there are many the wavefronts share them.
+template <int TYPE, int D, int R, int WAVES>
+__device__ void join(const AttendArgs &A, const Item &it, const Rows &of, int rows, uint32_t b0, int parts, const float *floats) {
+  __shared__ float lm[WAVES][64], ll[WAVES][64];
+  __shared__ float4v lo[WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool together = parts > 8;
+  const int pieces = rows * (D / 4), step = together ? 64 : 64 * WAVES;
+  for (int at = together ? 0 : wave * 64; at < pieces; at += step) {
+    const int e = min(at + lane, pieces - 1), i = e / (D / 4), d = e % (D / 4) * 4;
+    float M = kFloor, sum = 0.0f;
+    float4v out = {0.0f, 0.0f, 0.0f, 0.0f};
+    // many loads under way at a time; beyond the last part, the last again with no weight
+    constexpr int AHEAD = 8;
+    const int p_step = together ? WAVES : 1;
+    for (int p0 = together ? wave : 0; p0 < parts; p0 += AHEAD * p_step) {
+      float2 ml[AHEAD], v0[AHEAD], v1[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int p = min(p0 + j * p_step, parts - 1);
+        const float *const f = floats + part_index(b0 + p, p == 0) * part_floats(R, D);
+        ml[j] = get(f + 2 * i);
+        v0[j] = get(f + 2 * R + i * D + d);
+        v1[j] = get(f + 2 * R + i * D + d + 2);
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        if (p0 + j * p_step >= parts) break;
+        const float m_new = fmaxf(M, ml[j].x);
+        const float keep = __builtin_amdgcn_exp2f(M - m_new), add = __builtin_amdgcn_exp2f(ml[j].x - m_new);
+        sum = sum * keep + ml[j].y * add;
+        out = out * keep + float4v{v0[j].x, v0[j].y, v1[j].x, v1[j].y} * add;
+        M = m_new;
+      }
+    }
+    if (together) {
+      lm[wave][lane] = M;
+      ll[wave][lane] = sum;
+      lo[wave][lane] = out;
+      __syncthreads();
+      for (int w = 0; w < WAVES; ++w) M = fmaxf(M, lm[w][lane]);
+      sum = 0.0f;
+      out = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(lm[w][lane] - M);
+        sum += f * ll[w][lane];
+        out += f * lo[w][lane];
+      }
+      __syncthreads();
+    }
+    if (at + lane < pieces && (!together || wave == 0)) {
+      const int2 to = of(i);
+      uint16_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = bits16<TYPE>(sum == 0.0f ? 0.0f : out[j] / sum);
+      __builtin_memcpy((uint16_t *)A.out + ((int64_t)(it.q.q0 + to.x) * A.n_q_heads + it.h * (int)of.group + to.y) * D + d, w, 8);
+    }
+  }
+  __syncthreads();
+}
 
 // --------------------------------------------------- rows by 16, 8-bit products --
 // One wavefront takes 64 tokens of the context at a time for 16 rows.
@@ -147,121 +311,170 @@ __host__ __device__ constexpr int64_t part_floats(int R, int D) { return (int64_
 // scale is added to the exponent (log2), so one tile may span pages; the sum
 // of the softmax is kept in binary32 without it.
 
-template <int TYPE, int D>
-__global__ __launch_bounds__(256) void k_attend_rows(AttendArgs A, int target, int least, float *ws) {
+// A wavefront loads its next tile while it works on one.
+
+// Four sums with 128 in them to their second bytes, and their first as signed.
+__device__ __forceinline__ int2 split_bytes(const uint32_t (&b)[4]) {
+  const uint32_t u = __builtin_amdgcn_perm(b[1], b[0], 0x05010400), v = __builtin_amdgcn_perm(b[3], b[2], 0x05010400);
+  return {(int)__builtin_amdgcn_perm(v, u, 0x07060302), (int)(__builtin_amdgcn_perm(v, u, 0x05040100) ^ 0x80808080u)};
+}
+
+// ONE: pages of 64 tokens, so a tile is a page and its address is scalar.
+template <int TYPE, int D, int WAVES, bool ONE>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Share share, Parts P) {
   constexpr int STEPS = D / 64, DT = D / 16;
-  extern __shared__ int dynamic[];
-  int *const pre = dynamic, *const part = dynamic + A.n_seqs;
-  __shared__ float lo[4][kRows][D + 4];
-  __shared__ float lm[4][kRows], ll[4][kRows];
+  extern __shared__ uint32_t pre[];
+  __shared__ float lo[WAVES][kRows][D + 4];
+  __shared__ float lm[WAVES][kRows], ll[WAVES][kRows];
   const Cache &c = A.c;
   const int group = A.n_q_heads / c.n_heads;
-  const List L = make_list<256, kRows>(A, group, target, least, pre, part);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t total = list_units<64 * WAVES, kRows>(A, group, share, pre), run = run_length(total, gridDim.x, share);
+  const uint32_t mine = run_of_block();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = lane & 15, G = lane >> 4, kg = row >> 2;
-  const int PS = 1 << c.page_shift;
+  const int PS = ONE ? 64 : 1 << c.page_shift;
 
-  for (int item = blockIdx.x; item < L.items; item += gridDim.x) {
-    const int s = find(pre, A.n_seqs, item);
-    const Seq q = sequence(A, s);
-    const int parts = parts_of(q, L.chunk);
-    int at = item - pre[s];
-    const int ch = at % parts;
-    at /= parts;
-    const int h = at % c.n_heads, r0 = at / c.n_heads * kRows, rows = min(kRows, q.n * group - r0);
-    const int2 span = tiles_of(A, q, group, r0, r0 + rows, parts, ch);
+  struct Tile {
+    int4v k[4][STEPS], v[DT];
+    float ks, vs;
+  };
+  const uint32_t stop = min((mine + 1) * run, total);
+  for (uint32_t unit = mine * run; unit < stop;) {
+    const Item it = item_at<kRows>(A, group, share, pre, unit);
+    const Seq &q = it.q;
+    const int s = it.s, h = it.h, r0 = it.r0, rows = min(kRows, q.n * group - r0);
+    uint32_t from, to;
+    if (!take(it, run, stop, unit, from, to)) continue;
+    const bool whole = from == 0 && to == it.units;
+    const Rows of(r0, group, A.per_group);
+    const int2 mine_of = of(row);  // (token, head of the group)
+    const int j1 = of(rows - 1).x;
+    const int2 span = tiles_of(A, q, of.token, j1, whole, (int)from, (int)to);
     const int first = q.length - q.n;
-    const int r = r0 + row, token = row < rows ? r / group : 0;
-    const int64_t q_row = q.q0 + token;
-    const int q_head = h * group + r % group;
-    // what this row sees
+    const int token = row < rows ? mine_of.x : 0, q_head = h * group + mine_of.y;
+    // what this row sees, what some row sees, what all do
     const int last_seen = row < rows ? first + token : -1;
     const int first_seen = A.window ? max(0, last_seen - A.window + 1) : 0;
-    // pages that some row of the tile sees
-    const int top = first + min(q.n - 1, (r0 + rows - 1) / group);
-    const int low = A.window ? max(0, first + r0 / group - A.window + 1) : 0;
+    const int all_top = first + of.token, top = first + j1;
+    const int low = A.window ? max(0, all_top - A.window + 1) : 0, all_low = A.window ? top - A.window + 1 : 0;
     const int page_top = max(top, 0) >> c.page_shift, page_low = min(low, max(top, 0)) >> c.page_shift;
-
-    // the row's codes
-    float x[STEPS][16];
-    uint32_t most = 0;
-    for (int st = 0; st < STEPS; ++st) {
-      uint16_t raw[16] = {};
-      if (row < rows)
-        __builtin_memcpy(raw, (const uint16_t *)A.q + q_row * A.q_stride + q_head * D + st * 64 + G * 16, 32);
-      for (int i = 0; i < 16; ++i) {
-        x[st][i] = value16<TYPE>(raw[i]);
-        most = max(most, __float_as_uint(x[st][i]) & 0x7fffffffu);
-      }
-    }
-    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-    const float largest = __uint_as_float(most);
-    const float inverse = largest < kTiny ? 0.0f : 32512.0f / largest;
-    const float q_step = (largest < kTiny ? 0.0f : largest / 32512.0f) * (A.scale * kLog2e);
-    int4v q_hi[STEPS], q_lo[STEPS];
-    for (int st = 0; st < STEPS; ++st)
-      for (int w = 0; w < 4; ++w) {
-        uint32_t hi = 0, low_bytes = 0;
-        for (int i = 0; i < 4; ++i) {
-          const int v = (int)rintf(x[st][w * 4 + i] * inverse);
-          hi |= (uint32_t)(((v + 128) >> 8) & 0xff) << (8 * i);
-          low_bytes |= (uint32_t)(v & 0xff) << (8 * i);  // v - 256 * ((v + 128) >> 8), as a signed byte
-        }
-        q_hi[st][w] = (int)hi;
-        q_lo[st][w] = (int)low_bytes;
-      }
-
-    float4v o[DT] = {};
-    float m = kFloor, l = 0.0f;
     const int32_t *const table = A.table + s * A.table_width;
-    for (int tile = span.x + wave; tile < span.y; tile += 4) {
+
+    int32_t id_k = 0, id_v = 0;  // table entries as loaded: what is made of them waits for them
+    const auto pages = [&](int tile) {
+      if constexpr (ONE) {
+        id_k = id_v = table[min(max(tile, page_low), page_top)];
+      } else {
+        const int tok = tile * kTile;
+        id_k = table[min(max((tok + kg * 16) >> c.page_shift, page_low), page_top)];
+        id_v = table[min(max((tok + G * 16) >> c.page_shift, page_low), page_top)];
+      }
+    };
+    const auto fetch = [&](int tile, Tile &t) {
+      const auto page = [&](int32_t id) { return (int64_t)min((uint32_t)id, (uint32_t)(c.n_pages - 1)) * c.n_heads + h; };
+      const int64_t pk = page(id_k), pv = page(id_v);
+      const int at_k = ONE ? kg * 16 : (tile * kTile + kg * 16) & (PS - 1), at_v = ONE ? G * 16 : (tile * kTile + G * 16) & (PS - 1);
+      const int8_t *const kp = c.k + pk * (PS * D) + ((at_k + (row & 3)) * D + G * 16);
+      const int8_t *const vp = c.v + pv * (PS * D) + (row * PS + at_v);
+      t.ks = c.k_scale[pv];
+      t.vs = c.v_scale[pv];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) t.k[i][st] = *(const int4v *)(kp + i * 4 * D + st * 64);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) t.v[dt] = *(const int4v *)(vp + dt * 16 * PS);
+    };
+    Tile ta, tb;
+    int tile = span.x + wave;
+    if (tile < span.y) {
+      pages(tile);
+      fetch(tile, ta);
+      if (tile + WAVES < span.y) pages(tile + WAVES);
+    }
+
+    // the row's codes, 15 bits against its largest: in the low bits of a sum
+    // with 1.5 * 2^23 + 128 (the 128 makes the low byte signed)
+    int4v q_hi[STEPS], q_lo[STEPS];
+    float q_step;
+    {
+      using ushort2v = unsigned short __attribute__((ext_vector_type(2)));
+      int4v raw[STEPS][2];
+      ushort2v most = {0, 0};  // both types' magnitudes are in the order of their bits, a NaN's above all
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          raw[st][j] = int4v{0, 0, 0, 0};
+          if (row < rows)
+            raw[st][j] = load16((const uint16_t *)A.q + (int64_t)(q.q0 + token) * A.q_stride + q_head * D + st * 64 + G * 16 + j * 8);
+        }
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2v, raw[st][j][i] & 0x7fff7fff));
+      int bits = max((int)most[0], (int)most[1]);
+      bits = max(bits, __shfl_xor(bits, 16));
+      bits = max(bits, __shfl_xor(bits, 32));
+      const float largest = value16<TYPE>((uint16_t)bits);
+      const float inverse = largest < kTiny ? 0.0f : 32512.0f / largest;
+      q_step = (largest < kTiny ? 0.0f : largest / 32512.0f) * (A.scale * kLog2e);
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t b[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint16_t word = (uint16_t)(raw[st][w >> 1][(w & 1) * 2 + (i >> 1)] >> 16 * (i & 1));
+            b[i] = __float_as_uint(__builtin_fmaf(value16<TYPE>(word), inverse, 12582912.0f + 128.0f));
+          }
+          const int2 bytes = split_bytes(b);
+          q_hi[st][w] = bytes.x;
+          q_lo[st][w] = bytes.y;
+        }
+    }
+
+    float4v o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = kFloor, l = 0.0f;
+    const auto work = [&](int tile, const Tile &t) {
       const int base = tile * kTile;
-      const auto page_of = [&](int tok) {
-        const int i = min(max(tok >> c.page_shift, page_low), page_top);
-        return (int64_t)min((uint32_t)table[i], (uint32_t)(c.n_pages - 1)) * c.n_heads + h;
-      };
-      const int64_t pk = page_of(base + kg * 16), pv = page_of(base + G * 16);
-      const int8_t *const kp = c.k + (pk * PS + ((base + kg * 16) & (PS - 1)) + (row & 3)) * D + G * 16;
-      const int8_t *const vp = c.v + (pv * D + row) * PS + ((base + G * 16) & (PS - 1));
-      int4v kf[4][STEPS], vf[DT];
+      float sc[16];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int j = 0; j < 4; ++j) {
+        int4v hi = {0, 0, 0, 0}, low_sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) kf[t][st] = *(const int4v *)(kp + t * 4 * D + st * 64);
+        for (int st = 0; st < STEPS; ++st) {
+          hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.k[j][st], q_hi[st], hi, 0, 0, 0);
+          low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.k[j][st], q_lo[st], low_sum, 0, 0, 0);
+        }
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) vf[dt] = *(const int4v *)(vp + dt * 16 * PS);
-      float ks = c.k_scale[pk - pk + pv], vs = c.v_scale[pv];
-      // tokens of this lane that the row sees: base + G*16 + [a, b]
-      const int mine = base + G * 16;
-      const bool all = base >= first_seen && base + kTile - 1 <= last_seen;
-      const bool masked = __any(!all);
-      if (masked && (last_seen < mine || first_seen > mine + 15)) ks = vs = 1.0f;  // no page of this row's
+        for (int i = 0; i < 4; ++i) sc[j * 4 + i] = (float)(hi[i] * 256 + low_sum[i]);
+      }
+      // sc[i]: token base + G * 16 + i
+      float ks = t.ks, vs = t.vs;
+      const bool edge = base < all_low || base + kTile - 1 > all_top;  // some row does not see all of it
+      int least = first_seen - base - G * 16, most = last_seen - base - G * 16;
+      if (edge && (most < 0 || least > 15)) ks = vs = 1.0f;  // no page of this row's
       const bool zero = vs < kZeroScale;
       const float lift = zero ? -60.0f : __builtin_amdgcn_logf(vs);
       const float per = zero ? 0x1p60f : 1.0f / vs;
       const float cq = q_step * ks;
-      float sc[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = __builtin_fmaf(sc[i], cq, lift);
+      if (edge) {
+        asm volatile("" : "+v"(least), "+v"(most));  // keeps the comparisons in here
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = i >= least && i <= most ? sc[i] : -INFINITY;
+      }
       float top_s = kFloor;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        int4v hi = {0, 0, 0, 0}, low_sum = {0, 0, 0, 0};
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[t][st], q_hi[st], hi, 0, 0, 0);
-          low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[t][st], q_lo[st], low_sum, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float v = __builtin_fmaf((float)(hi[i] * 256 + low_sum[i]), cq, lift);
-          if (masked) {
-            const int tok = mine + t * 4 + i;
-            v = tok >= first_seen && tok <= last_seen ? v : -INFINITY;
-          }
-          sc[t * 4 + i] = v;
-          top_s = fmaxf(top_s, v);
-        }
-      }
+      for (int i = 0; i < 16; ++i) top_s = fmaxf(top_s, sc[i]);
       top_s = fmaxf(top_s, __shfl_xor(top_s, 16));
       top_s = fmaxf(top_s, __shfl_xor(top_s, 32));
       const float m_new = fmaxf(m, top_s);
@@ -273,31 +486,50 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs A, int target, i
       float sum = 0.0f;
       int4v p_hi, p_lo;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+      for (int j = 0; j < 4; ++j) {
         uint32_t b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(sc[t * 4 + i] - top_s);
+          const float p = __builtin_amdgcn_exp2f(sc[j * 4 + i] - top_s);
           sum += p;
           b[i] = __float_as_uint(__builtin_fmaf(p, full, 8388608.0f + 128.0f));
         }
-        const uint32_t u = __builtin_amdgcn_perm(b[1], b[0], 0x05010400), v = __builtin_amdgcn_perm(b[3], b[2], 0x05010400);
-        p_lo[t] = (int)(__builtin_amdgcn_perm(v, u, 0x05040100) ^ 0x80808080u);
-        p_hi[t] = (int)__builtin_amdgcn_perm(v, u, 0x07060302);
+        const int2 bytes = split_bytes(b);
+        p_hi[j] = bytes.x;
+        p_lo[j] = bytes.y;
       }
       l = l * keep + sum * per * add;
+      if (__any(keep != 1.0f)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= keep;
+      }
       const float step = add * (1.0f / 32512.0f);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const int4v none = {0, 0, 0, 0};
-        const int4v hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[dt], p_hi, none, 0, 0, 0);
-        const int4v low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[dt], p_lo, none, 0, 0, 0);
+        const int4v hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.v[dt], p_hi, none, 0, 0, 0);
+        const int4v low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.v[dt], p_lo, none, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          o[dt][i] = __builtin_fmaf((float)(hi[i] * 256 + low_sum[i]), step, o[dt][i] * keep);
+          o[dt][i] = __builtin_fmaf((float)(hi[i] * 256 + low_sum[i]), step, o[dt][i]);
       }
+    };
+    while (tile < span.y) {
+      if (tile + WAVES < span.y) {
+        fetch(tile + WAVES, tb);
+        if (tile + 2 * WAVES < span.y) pages(tile + 2 * WAVES);
+      }
+      work(tile, ta);
+      tile += WAVES;
+      if (tile >= span.y) break;
+      if (tile + WAVES < span.y) {
+        fetch(tile + WAVES, ta);
+        if (tile + 2 * WAVES < span.y) pages(tile + 2 * WAVES);
+      }
+      work(tile, tb);
+      tile += WAVES;
     }
-    // the row's sum over the four lanes that hold it, then the four wavefronts
+    // the row's sum over the four lanes that hold it, then the wavefronts
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (G == 0) {
@@ -307,64 +539,423 @@ __global__ __launch_bounds__(256) void k_attend_rows(AttendArgs A, int target, i
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) *(float4v *)&lo[wave][row][dt * 16 + G * 4] = o[dt];
     __syncthreads();
-    for (int e = threadIdx.x; e < rows * D; e += 256) {
-      const int i = e / D, d = e % D;
+    for (int e = threadIdx.x; e < rows * (D / 2); e += 64 * WAVES) {
+      const int i = e / (D / 2), d = e % (D / 2) * 2;
       float M = lm[0][i];
-      for (int w = 1; w < 4; ++w) M = fmaxf(M, lm[w][i]);
-      float sum = 0.0f, out = 0.0f;
-      for (int w = 0; w < 4; ++w) {
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) M = fmaxf(M, lm[w][i]);
+      float sum = 0.0f, out0 = 0.0f, out1 = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
         const float f = __builtin_amdgcn_exp2f(lm[w][i] - M);
         sum += f * ll[w][i];
-        out += f * lo[w][i][d];
+        out0 += f * lo[w][i][d];
+        out1 += f * lo[w][i][d + 1];
       }
-      if (parts > 1) {
-        float *const to = ws + (part[s] + item - pre[s]) * part_floats(kRows, D);
-        if (d == 0) {
-          to[i] = M;
-          to[kRows + i] = sum;
-        }
-        to[2 * kRows + i * D + d] = out;
+      if (!whole) {
+        float *const part = P.floats + part_index(mine, from == 0) * part_floats(kRows, D);
+        if (d == 0) put(part + 2 * i, M, sum);
+        put(part + 2 * kRows + i * D + d, out0, out1);
       } else {
-        const int rr = r0 + i;
-        store_value<TYPE>(A.out, ((int64_t)(q.q0 + rr / group) * A.n_q_heads + h * group + rr % group) * D + d,
-                          sum == 0.0f ? 0.0f : out / sum);
+        const int2 at = of(i);
+        const uint16_t w[2] = {bits16<TYPE>(sum == 0.0f ? 0.0f : out0 / sum), bits16<TYPE>(sum == 0.0f ? 0.0f : out1 / sum)};
+        __builtin_memcpy((uint16_t *)A.out + ((int64_t)(q.q0 + at.x) * A.n_q_heads + h * group + at.y) * D + d, w, 4);
       }
     }
-    __syncthreads();
+    if (whole || P.call == 0) {
+      __syncthreads();
+    } else {
+      const uint32_t b0 = it.start / run, b1 = (it.start + it.units - 1) / run;  // the runs that have parts of it
+      if (last_to_arrive(P, b0, (int)(b1 - b0 + 1)))
+        join<TYPE, D, kRows, WAVES>(A, it, of, rows, b0, (int)(b1 - b0 + 1), P.floats);
+    }
   }
 }
 
-// Joins the parts of split contexts: a block takes one row tile of one head.
-template <int TYPE, int D, int R>
-__global__ __launch_bounds__(256) void k_join(AttendArgs A, int target, int least, const float *ws) {
-  extern __shared__ int dynamic[];
-  int *const pre = dynamic, *const part = dynamic + A.n_seqs;
-  const int group = A.n_q_heads / A.c.n_heads;
-  const List L = make_list<256, R>(A, group, target, least, pre, part);
-  for (int at = blockIdx.x; at < L.partials; at += gridDim.x) {
-    const int s = find(part, A.n_seqs, at);
-    const Seq q = sequence(A, s);
-    const int parts = parts_of(q, L.chunk);
-    int rel = at - part[s];
-    const int which = rel % parts;  // the blocks of a tile's parts share its rows
-    rel /= parts;
-    const int h = rel % A.c.n_heads, r0 = rel / A.c.n_heads * R, rows = min(R, q.n * group - r0);
-    const float *const from = ws + (int64_t)(at - which) * part_floats(R, D);
-    for (int e = which * 256 + threadIdx.x; e < rows * D; e += parts * 256) {
-      const int i = e / D, d = e % D;
-      float M = kFloor, sum = 0.0f, out = 0.0f;
-      for (int p = 0; p < parts; ++p) {
-        const float *const f = from + p * part_floats(R, D);
-        const float m = f[i], m_new = fmaxf(M, m);
-        const float keep = __builtin_amdgcn_exp2f(M - m_new), add = __builtin_amdgcn_exp2f(m - m_new);
-        sum = sum * keep + f[R + i] * add;
-        out = out * keep + f[2 * R + i * D + d] * add;
-        M = m_new;
+// ------------------------------------------------- many rows, binary16 products --
+// A block takes 256 rows, 32 a wavefront, and 64 tokens at a time, whose codes
+// it turns into binary16 in LDS once for all rows (exactly: codes are small
+// integers), two tiles ahead.  A step has two parts, the products (of the
+// tile's keys, and of the values of the tile before) and the exponentials; one
+// of the two wavefronts of a SIMD is a part behind the other, so that one
+// multiplies while the other takes exponentials.  S^T = K Q^T and
+// O^T = V^T P^T with 32 x 32 x 16 products: a lane has one row, and K's rows
+// are dealt so that its eight tokens of each 16 are neighbours, which makes
+// the probabilities the second operand of the second product as they stand.
+//
+// Queries are scaled by a power of two, below 2 in magnitude, before they are
+// rounded to binary16 (bfloat16 ones exactly, but for elements under 2^-14 of
+// the row's largest).  The maximum that probabilities are taken against may
+// lag by 2^8, so the output is seldom rescaled; with 2^6 on top probabilities
+// reach 2^14 and keep 11 bits down to 2^-20 of the largest.
+constexpr int kChunkRows = 256, kChunkThreads = 512, kChunkLeast = 128;
+constexpr float kLag = 8.0f, kLift = 6.0f;
+
+// The block's barrier after this wavefront's LDS accesses; its loads go on.
+__device__ __forceinline__ void part_end() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// N products with an operand each from LDS, read AHEAD products ahead, which
+// covers the reads' latency (left to itself the compiler reads, waits and
+// multiplies in turn).
+template <int N, int AHEAD, class Read, class Multiply>
+__device__ __forceinline__ void products(Read read, Multiply multiply) {
+  half8 held[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) held[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(i, held[i % AHEAD]);
+    if (i + AHEAD < N) held[i % AHEAD] = read(i + AHEAD);
+  }
+}
+
+// 16 codes to binary16: 1024 + (code + 128) is the byte under 0x64.
+__device__ __forceinline__ void widen(int4v codes, int4v (&out)[2]) {
+  using half2v = _Float16 __attribute__((ext_vector_type(2)));
+  const half2v bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t b = (uint32_t)codes[i] ^ 0x80808080u;
+    const half2v a = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400)) + bias;
+    const half2v c = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402)) + bias;
+    out[i >> 1][(i & 1) * 2] = __builtin_bit_cast(int, a);
+    out[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(int, c);
+  }
+}
+
+template <int TYPE, int D>
+__global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A, Share share, Parts P) {
+  constexpr int kAhead = 6;
+  constexpr int KK = D / 16, DT = D / 32, KC = D / 8;  // KC: 16-byte chunks of a token's binary16 keys
+  extern __shared__ uint32_t pre[];
+  __shared__ int4v lk[4][kTile * KC], lv[4][D * 8];
+  __shared__ float4v scales[4][4];  // of 16 tokens: key scale, log2 and inverse of the value scale
+  const Cache &c = A.c;
+  const int group = A.n_q_heads / c.n_heads;
+  const uint32_t total = list_units<kChunkThreads, kChunkRows>(A, group, share, pre), run = run_length(total, gridDim.x, share);
+  const uint32_t mine = run_of_block(), stop = min((mine + 1) * run, total);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int PS = 1 << c.page_shift;
+  // this thread's piece of a tile: 16 elements of a token's keys, 16 tokens of an element's values
+  const int piece = D == 128 ? threadIdx.x : threadIdx.x & 255;
+  const bool of_k = D == 128 || threadIdx.x < 256, of_v = D == 128 || threadIdx.x >= 256;
+  const int k_token = piece / KK, k_part = piece % KK, v_row = piece >> 2, v_group = piece & 3;
+  const auto k_place = [](int token, int chunk) {
+    return token * KC + (chunk ^ (D == 128 ? token & 15 : (token >> 1) & 7));
+  };
+  const auto v_place = [](int d, int chunk) { return d * 8 + (chunk ^ ((d >> 1) & 7)); };
+
+  for (uint32_t unit = mine * run; unit < stop;) {
+    const Item it = item_at<kChunkRows>(A, group, share, pre, unit);
+    const Seq &q = it.q;
+    const int s = it.s, h = it.h, r0 = it.r0, rows = min(kChunkRows, q.n * group - r0);
+    uint32_t from, to;
+    if (!take(it, run, stop, unit, from, to)) continue;
+    const bool whole = from == 0 && to == it.units;
+    const Rows of(r0, group, A.per_group);
+    const int2 mine_of = of(wave * 32 + col);  // (token, head of the group)
+    const int j1 = of(rows - 1).x;
+    const int2 span = tiles_of(A, q, of.token, j1, whole, (int)from, (int)to);
+    const int first = q.length - q.n;
+    const bool live = wave * 32 + col < rows;
+    const int token = live ? mine_of.x : 0, q_head = h * group + (live ? mine_of.y : 0);
+    const int last_seen = live ? first + token : -1;
+    const int first_seen = A.window && live ? max(0, last_seen - A.window + 1) : 0;
+    // tiles that some row of this wavefront sees
+    const int wave_rows = min(32, rows - wave * 32);
+    const int wave_first = of(wave * 32).x, wave_last = of(wave * 32 + max(wave_rows, 1) - 1).x;
+    const int wave_top = wave_rows > 0 ? first + wave_last : -1;
+    const int wave_low = A.window && wave_rows > 0 ? max(0, first + wave_first - A.window + 1) : 0;
+    // tokens that all of its rows see
+    const int all_top = wave_rows > 0 ? first + wave_first : -1;
+    const int all_low = A.window && wave_rows > 0 ? wave_top - A.window + 1 : 0;
+    // pages that some row of the block sees
+    const int top = first + j1;
+    const int low = A.window ? max(0, first + of.token - A.window + 1) : 0;
+    const int page_top = max(top, 0) >> c.page_shift, page_low = min(low, max(top, 0)) >> c.page_shift;
+    const int32_t *const table = A.table + s * A.table_width;
+    const auto entry = [&](int tok) { return table[min(max(tok >> c.page_shift, page_low), page_top)]; };
+    const auto page_of = [&](int32_t id) { return (int64_t)min((uint32_t)id, (uint32_t)(c.n_pages - 1)) * c.n_heads + h; };
+
+    // the row in binary16
+    half8 qf[KK];
+    float q_step;
+    {
+      int4v raw[KK];
+      uint32_t most = 0;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        raw[kk] = int4v{0, 0, 0, 0};
+        if (live) raw[kk] = load16((const uint16_t *)A.q + (int64_t)(q.q0 + token) * A.q_stride + q_head * D + kk * 16 + half * 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          most = max(most, __float_as_uint(value16<TYPE>((uint16_t)(raw[kk][i >> 1] >> 16 * (i & 1)))) & 0x7fffffffu);
       }
-      const int rr = r0 + i;
-      store_value<TYPE>(A.out, ((int64_t)(q.q0 + rr / group) * A.n_q_heads + h * group + rr % group) * D + d,
+      most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+      // by a power of two near the largest; rows below 2^-100 count as zero
+      const uint32_t e = min(max(most >> 23, 27u), 253u);
+      const float up = __uint_as_float((254 - e) << 23 | (A.scale < 0.0f ? 0x80000000u : 0u)), down = __uint_as_float(e << 23);
+      q_step = most >= 0x7f800000u ? NAN : down * (fabsf(A.scale) * kLog2e);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          qf[kk][i] = (_Float16)(value16<TYPE>((uint16_t)(raw[kk][i >> 1] >> 16 * (i & 1))) * up);
+    }
+
+    float16v o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+    float m = kFloor, l = 0.0f;
+
+    int32_t id_k = 0, id_v = 0;  // table entries, as loaded: what is made of them waits for them
+    int4v codes_k, codes_v;
+    float scale_k = 0.0f, scale_v = 0.0f;
+    const auto pages = [&](int tile) {
+      id_k = entry(tile * kTile + k_token);
+      id_v = entry(tile * kTile + v_group * 16);
+    };
+    const auto fetch = [&](int tile) {
+      const int64_t page_k = page_of(id_k), page_v = page_of(id_v);
+      if (of_k) codes_k = *(const int4v *)(c.k + (page_k * PS + ((tile * kTile + k_token) & (PS - 1))) * D + k_part * 16);
+      if (of_v) codes_v = *(const int4v *)(c.v + (page_v * D + v_row) * PS + ((tile * kTile + v_group * 16) & (PS - 1)));
+      scale_v = c.v_scale[page_v];
+      scale_k = c.k_scale[page_v];  // of threads 0 .. 3 the four groups'
+    };
+    const auto deposit = [&](int buf) {
+      int4v wide[2];
+      if (of_k) {
+        widen(codes_k, wide);
+        lk[buf][k_place(k_token, k_part * 2)] = wide[0];
+        lk[buf][k_place(k_token, k_part * 2 + 1)] = wide[1];
+      }
+      if (of_v) {
+        widen(codes_v, wide);
+        if (scale_v < kZeroScale) wide[0] = wide[1] = int4v{0, 0, 0, 0};
+        lv[buf][v_place(v_row, v_group * 2)] = wide[0];
+        lv[buf][v_place(v_row, v_group * 2 + 1)] = wide[1];
+      }
+      if (threadIdx.x < 4) {
+        const bool none = scale_v < kZeroScale;
+        scales[buf][threadIdx.x] =
+            float4v{scale_k, none ? -60.0f : __builtin_amdgcn_logf(scale_v), none ? 0x1p60f : 1.0f / scale_v, 0.0f};
+      }
+    };
+    const int last_tile = span.y - 1;
+    if (span.x < span.y) {
+      pages(span.x);
+      fetch(span.x);
+      pages(min(span.x + 1, last_tile));
+      deposit(span.x & 3);
+      fetch(min(span.x + 1, last_tile));
+      pages(min(span.x + 2, last_tile));
+      deposit((span.x + 1) & 3);
+      fetch(min(span.x + 2, last_tile));
+      pages(min(span.x + 3, last_tile));
+    }
+    half8 pf[4];
+    bool waiting = false;  // pf holds the tile before
+    const auto weigh = [&](int buf) {
+      products<4 * DT, kAhead>(
+          [&](int i) { return __builtin_bit_cast(half8, lv[buf][v_place(i % DT * 32 + col, i / DT * 2 + half)]); },
+          [&](int i, half8 v) { o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[i / DT], o[i % DT], 0, 0, 0); });
+    };
+    part_end();
+    if (wave >= 4) part_end();
+    for (int tile = span.x; tile < span.y; ++tile) {
+      const int base = tile * kTile, buf = tile & 3;
+      const bool seen = base <= wave_top && base + kTile > wave_low;
+      float16v sc[2];
+      if (seen) {
+        const int tok = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+        products<2 * KK, kAhead>(
+            [&](int i) { return __builtin_bit_cast(half8, lk[buf][k_place(i % 2 * 32 + tok, i / 2 * 2 + half)]); },
+            [&](int i, half8 k) { sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[i / 2], sc[i % 2], 0, 0, 0); });
+      }
+      if (waiting) weigh((tile - 1) & 3);
+      waiting = seen;
+      part_end();
+      if (seen) {
+        // register i of tile t: token half * 8 + i % 8 of group g = 2 t + i / 8;
+        // its logit (base 2, with the value scale) is x * slope[g] + add[g]
+        float slope[4], add[4], per[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4v by = scales[buf][g];
+          slope[g] = q_step * by[0];
+          add[g] = by[1];
+          per[g] = by[2];
+        }
+        if (base < all_low || base + kTile - 1 > all_top) {  // some row does not see all of it
+          int least = first_seen - base - half * 8, most = last_seen - base - half * 8;
+          asm volatile("" : "+v"(least), "+v"(most));  // keeps the comparisons in here
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            if (g * 16 - half * 8 > most || g * 16 + 15 - half * 8 < least) per[g] = 0.0f;  // no page of this row's
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int at_i = (g & 1) * 8 + i, place = g * 16 + i;
+              const float v = __builtin_fmaf(sc[g >> 1][at_i], slope[g], add[g]);
+              sc[g >> 1][at_i] = place >= least && place <= most ? v : -INFINITY;
+            }
+            slope[g] = 1.0f;
+            add[g] = 0.0f;
+          }
+        }
+        float top_s = kFloor;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int f = (g & 1) * 8;
+          float most = fmaxf(sc[g >> 1][f], sc[g >> 1][f + 1]);
+#pragma unroll
+          for (int i = 2; i < 8; ++i) most = fmaxf(most, sc[g >> 1][f + i]);
+          top_s = fmaxf(top_s, __builtin_fmaf(most, slope[g], add[g]));
+        }
+        top_s = fmaxf(top_s, __shfl_xor(top_s, 32));
+        if (__any(fabsf(top_s) > 0x1p20f)) {  // logits so large that one rounding less would tell: as they are
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int at_i = (g & 1) * 8 + i;
+              sc[g >> 1][at_i] = __builtin_fmaf(sc[g >> 1][at_i], slope[g], add[g]);
+            }
+            slope[g] = 1.0f;
+            add[g] = 0.0f;
+          }
+        }
+        if (__any(top_s > m + kLag)) {
+          const float m_new = fmaxf(m, top_s), keep = __builtin_amdgcn_exp2f(m - m_new);
+          m = m_new;
+          l *= keep;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] *= keep;
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float plus = add[g] - (m - kLift);
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[g >> 1][(g & 1) * 8 + i], slope[g], plus));
+            sum += p;
+            pf[g][i] = (_Float16)p;
+          }
+          l = __builtin_fmaf(sum, per[g], l);
+        }
+      }
+      // tile + 2, read first two parts from here; its place was last read two
+      // parts ago.  Beyond the last tile it is the last again: with no
+      // condition nothing waits for the loads here.
+      deposit((tile + 2) & 3);
+      fetch(min(tile + 3, last_tile));
+      pages(min(tile + 4, last_tile));
+      part_end();
+    }
+    if (waiting) weigh(last_tile & 3);
+    if (wave < 4) part_end();
+    part_end();
+    l += __shfl_xor(l, 32);
+    if (live) {
+      if (!whole) {
+        float *const part = P.floats + part_index(mine, from == 0) * part_floats(kChunkRows, D);
+        const int i = wave * 32 + col;
+        if (half == 0) put(part + 2 * i, m, l);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float *const to = part + 2 * kChunkRows + (int64_t)i * D + dt * 32 + j * 8 + half * 4;
+            put(to, o[dt][j * 4], o[dt][j * 4 + 1]);
+            put(to + 2, o[dt][j * 4 + 2], o[dt][j * 4 + 3]);
+          }
+      } else {
+        const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *const to = (uint16_t *)A.out + ((int64_t)(q.q0 + token) * A.n_q_heads + q_head) * D;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint16_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = bits16<TYPE>(o[dt][j * 4 + i] * inverse);
+            __builtin_memcpy(to + dt * 32 + j * 8 + half * 4, w, 8);
+          }
+      }
+    }
+    if (!whole) {
+      const uint32_t b0 = it.start / run, b1 = (it.start + it.units - 1) / run;  // the runs that have parts of it
+      if (last_to_arrive(P, b0, (int)(b1 - b0 + 1)))
+        join<TYPE, D, kChunkRows, kChunkThreads / 64>(A, it, of, rows, b0, (int)(b1 - b0 + 1), P.floats);
+    }
+  }
+}
+
+// The row kernel's parts where an item has many, which one block would be long
+// in adding up (4 users of 131072 tokens, 64 parts an item: 92 us instead of
+// 61).  A block takes one cut between runs; the cuts within one item share its
+// elements, 64 a block, and its wavefronts share the parts.
+constexpr int kJoinWaves = 8;
+template <int TYPE, int D>
+__global__ __launch_bounds__(64 * kJoinWaves) void k_join(AttendArgs A, Share share, int blocks, const float *floats) {
+  constexpr int R = kRows;
+  extern __shared__ uint32_t pre[];
+  __shared__ float lm[kJoinWaves][64], ll[kJoinWaves][64], lo[kJoinWaves][64];
+  const int group = A.n_q_heads / A.c.n_heads;
+  const uint32_t total = list_units<64 * kJoinWaves, R>(A, group, share, pre), run = run_length(total, blocks, share);
+  const uint32_t cut = (blockIdx.x + 1) * run;
+  if (cut >= total) return;
+  const Item it = item_at<R>(A, group, share, pre, cut);
+  if (it.start == cut || stays_whole(it.units, run)) return;
+  const uint32_t b0 = it.start / run, b1 = (it.start + it.units - 1) / run;  // the runs that have parts of it
+  const int parts = (int)(b1 - b0 + 1), rows = min(R, it.q.n * group - it.r0);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Rows of(it.r0, group, A.per_group);
+  for (int e = (int)(blockIdx.x - b0) * 64 + lane; e - lane < rows * D; e += (parts - 1) * 64) {  // rows * D is a multiple of 64
+    const int i = e / D, d = e % D;
+    float M = kFloor, sum = 0.0f, out = 0.0f;
+#pragma unroll 8
+    for (int p = wave; p < parts; p += kJoinWaves) {
+      const float *const f = floats + part_index(b0 + p, p == 0) * part_floats(R, D);
+      const float m = f[2 * i], l = f[2 * i + 1], v = f[2 * R + i * D + d];
+      const float m_new = fmaxf(M, m);
+      const float keep = __builtin_amdgcn_exp2f(M - m_new), add = __builtin_amdgcn_exp2f(m - m_new);
+      sum = sum * keep + l * add;
+      out = out * keep + v * add;
+      M = m_new;
+    }
+    lm[wave][lane] = M;
+    ll[wave][lane] = sum;
+    lo[wave][lane] = out;
+    __syncthreads();
+    if (wave == 0) {
+      for (int w = 1; w < kJoinWaves; ++w) M = fmaxf(M, lm[w][lane]);
+      sum = out = 0.0f;
+      for (int w = 0; w < kJoinWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(lm[w][lane] - M);
+        sum += f * ll[w][lane];
+        out += f * lo[w][lane];
+      }
+      const int2 at = of(i);
+      store_value<TYPE>(A.out, ((int64_t)(it.q.q0 + at.x) * A.n_q_heads + it.h * group + at.y) * D + d,
                         sum == 0.0f ? 0.0f : out / sum);
     }
+    __syncthreads();
   }
 }
 
@@ -385,42 +976,88 @@ __global__ void k_check_attention(AttendArgs A, int32_t *flag) {
   }
 }
 
-// Blocks of the row kernel: four a CU, each with four wavefronts, which holds
-// enough loads in flight; at most twice as many parts as its target.
-constexpr int kRowBlocks = 1024;
+// Blocks of the row kernel: two a CU, each with four wavefronts of two tiles
+// in flight; of the other: one a CU.
+constexpr int kRowBlocks = 512, kChunkBlocks = 256;
+static_assert(kRowBlocks < 4096, "counts of parts have 12 bits");
 
-struct Choice {
-  int target, least;
-};
+template <class Kernel>
+hipError_t allow_lds(Kernel kernel, size_t bytes) {  // beyond 64 KB with the static part
+  if (bytes <= 16384) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
 
-Choice choose(const AttendArgs &) { return {kRowBlocks, 4}; }
+unsigned long long next_call() {  // a number that no other call of the process has; from a random start
+  static std::atomic<unsigned long long> number{((unsigned long long)std::random_device{}() << 20) ^
+                                                (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count()};
+  unsigned long long n;
+  do n = ++number << 12;
+  while (n == 0);
+  return n;
+}
 
-template <int TYPE, int D>
-hipError_t attend_as(const AttendArgs &A, float *ws, hipStream_t s) {
-  const Choice C = choose(A);
-  const size_t lds = 2 * sizeof(int) * A.n_seqs;
-  if (lds > 16384) {  // beyond 64 KB with the static part
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_attend_rows<TYPE, D>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+template <int TYPE, int D, bool ONE>
+hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
+  const size_t lds = sizeof(uint32_t) * A.n_seqs;
+  const int64_t group = A.n_q_heads / A.c.n_heads, most_rows = A.max_q * group;
+  const int everything = 0x7fffffff;
+  // From what the host knows, at most: row tiles of 16 rows in all, and tiles
+  // of 64 tokens that one sees.
+  const int64_t row_tiles = (A.n_tokens * group / kRows + A.n_seqs) * A.c.n_heads;
+  int64_t tiles = (A.table_width << A.c.page_shift) / kTile + kItemUnits;
+  if (A.window) tiles = std::min(tiles, ((int64_t)A.window + A.max_q) / kTile + kItemUnits);
+  // The chunk kernel does about 1700 units of 16 rows a us, the row kernel 675,
+  // but it takes 30 us more where there is little to do (2 x 2048 tokens of 40
+  // heads over 8192: 1716 us by the row kernel, 680 by this one; 389 tokens of
+  // 12 heads in a window of 1000: 25 and 80).
+  const bool chunks = most_rows >= kChunkLeast && row_tiles * tiles >= 32768;
+  Parts P{(unsigned long long *)ws, (float *)((unsigned long long *)ws + kRowBlocks), 0};
+  hipError_t e;
+  if (chunks) {  // a sequence alone has no other kernel, whatever it turns out to be
+    const Share many{8, A.n_seqs == 1 ? 1 : kChunkLeast, everything};
+    P.call = next_call();
+    e = allow_lds(&k_attend_chunk<TYPE, D>, lds);
     if (e != hipSuccess) return e;
+    k_attend_chunk<TYPE, D><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
+    if (A.n_seqs == 1) return hipGetLastError();
   }
-  k_attend_rows<TYPE, D><<<kRowBlocks, 256, lds, s>>>(A, C.target, C.least, ws);
-  k_join<TYPE, D, kRows><<<kRowBlocks, 256, lds, s>>>(A, C.target, C.least, ws);
+  const Share few{4, 1, chunks ? kChunkLeast : everything};
+  // parts of an item: by the length of its context, or by its share of the blocks
+  const int64_t items = std::max<int64_t>(1, (int64_t)A.n_seqs * A.c.n_heads * ((std::min<int64_t>(most_rows, kChunkLeast) + kRows - 1) / kRows));
+  const bool few_parts = std::min((tiles - kItemUnits) / few.least, 2 * kRowBlocks / items) < 12;
+  P.call = few_parts ? next_call() : 0;
+  e = allow_lds(&k_attend_rows<TYPE, D, 4, ONE>, lds);
+  if (e != hipSuccess) return e;
+  k_attend_rows<TYPE, D, 4, ONE><<<kRowBlocks, 256, lds, s>>>(A, few, P);
+  if (!few_parts) k_join<TYPE, D><<<kRowBlocks - 1, 64 * kJoinWaves, lds, s>>>(A, few, kRowBlocks, P.floats);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attention_workspace(const Cache &c, int32_t, int64_t, int32_t) {
-  // items of split contexts have at least half a chunk each: at most twice the target
-  return 2 * (size_t)kRowBlocks * part_floats(kRows, c.head_dim) * sizeof(float);
+  // a counter a run and at most two parts; the kernels run one after the other
+  return kRowBlocks * sizeof(unsigned long long) +
+         2 * sizeof(float) * std::max(kRowBlocks * part_floats(kRows, c.head_dim), kChunkBlocks * part_floats(kChunkRows, c.head_dim));
+}
+
+bool attention_fits(const AttendArgs &A) {
+  const int64_t group = A.n_q_heads / A.c.n_heads, most_rows = A.max_q * group;
+  const int64_t tiles = (A.table_width << A.c.page_shift) / kTile + kItemUnits, limit = 0x7fffffff;
+  const auto fits = [&](int64_t row_tiles) { return row_tiles <= limit / A.c.n_heads / tiles; };
+  const int64_t rows = (int64_t)A.n_tokens * group;
+  if (most_rows < kChunkLeast || rows / kRows + A.n_seqs <= 32768 / tiles) return fits(rows / kRows + A.n_seqs);
+  return fits(rows / kChunkRows + A.n_seqs) && fits((int64_t)A.n_seqs * (kChunkLeast / kRows));
+}
+
+template <int TYPE>
+static hipError_t attend_of(const AttendArgs &A, void *ws, hipStream_t s) {
+  if (A.c.page_shift == 6) return A.c.head_dim == 64 ? attend_as<TYPE, 64, true>(A, ws, s) : attend_as<TYPE, 128, true>(A, ws, s);
+  return A.c.head_dim == 64 ? attend_as<TYPE, 64, false>(A, ws, s) : attend_as<TYPE, 128, false>(A, ws, s);
 }
 
 hipError_t launch_cache_attention(const AttendArgs &A, void *ws, hipStream_t s) {
-  float *const w = (float *)ws;
-  if (A.type == kF16)
-    return A.c.head_dim == 64 ? attend_as<kF16, 64>(A, w, s) : attend_as<kF16, 128>(A, w, s);
-  return A.c.head_dim == 64 ? attend_as<kBF16, 64>(A, w, s) : attend_as<kBF16, 128>(A, w, s);
+  return A.type == kF16 ? attend_of<kF16>(A, ws, s) : attend_of<kBF16>(A, ws, s);
 }
 
 hipError_t launch_check_attention(const AttendArgs &A, int32_t *flag, hipStream_t s) {

@@ -67,7 +67,10 @@ struct AttendArgs {
   int64_t q_stride, table_width;
   int32_t n_tokens, n_seqs, n_q_heads, max_q, window, type;
   float scale;
+  uint32_t per_group;  // 2^32 / query heads of a group, rounded up (of no account for 1)
 };
+// Whether the call's units of work can be counted in 32 bits.
+bool attention_fits(const AttendArgs &A);
 size_t attention_workspace(const Cache &c, int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs);
 hipError_t launch_cache_attention(const AttendArgs &A, void *ws, hipStream_t s);
 

@@ -249,6 +249,7 @@ static fs_status check_heads(const fs_kv_cache *cache, int32_t n_q_heads, int64_
   if (st != FS_OK) return st;
   if (n_q_heads < 1 || n_q_heads % cache->n_heads)
     return fail(FS_ERR_INVALID_ARGUMENT, "n_q_heads must be a positive multiple of the cache's heads");
+  if (n_q_heads > 65536 / 2) return fail(FS_ERR_UNSUPPORTED, "n_q_heads must be at most 32768");
   if (n_tokens < 0 || n_tokens > kMost || n_tokens * n_q_heads > kMost)
     return fail(FS_ERR_INVALID_ARGUMENT, "n_tokens * n_q_heads must be in [0, 2^31)");
   if (n_seqs < 0) return fail(FS_ERR_INVALID_ARGUMENT, "n_seqs must be >= 0");
@@ -293,8 +294,12 @@ fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const vo
   if ((uintptr_t)d_workspace & 15) return fail(FS_ERR_INVALID_ARGUMENT, "the workspace must start on a multiple of 16 bytes");
   DeviceGuard dg(ctx->device);
   if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
+  const int32_t group = n_q_heads / cache->n_heads;
   const fs::AttendArgs A{to_cache(cache), d_q, d_out, d_cu_q, d_ctx_lens, d_block_table, q_stride, table_width,
-                         (int32_t)n_tokens, n_seqs, n_q_heads, max_q, window, (int32_t)type, scale};
+                         (int32_t)n_tokens, n_seqs, n_q_heads, max_q, window, (int32_t)type, scale,
+                         (uint32_t)((0x100000000ull + (uint64_t)group - 1) / (uint64_t)group)};
+  if (!fs::attention_fits(A))
+    return fail(FS_ERR_UNSUPPORTED, "more than 2^31 tiles of rows and tokens: split the call");
   if (fs::env_validate()) {
     st = checked([&](int32_t *flag) { return fs::launch_check_attention(A, flag, stream); }, stream,
                  "fs_cache_attention", {"sequences with lengths out of range", "pages outside the cache", ""});

@@ -612,3 +612,115 @@ def test_nothing_to_do_is_no_error(env):
     fs.cache_attention(ctx, kv, e(0, 1, 64), cu[None], cu[:1], cu, 0)
     codes, scale = fs.quantize_rows(ctx, e(0, 5))
     assert codes.shape == (0, 5) and scale.shape == (0,)
+
+
+# ------------------------------------- attention of many rows over long tables --
+def wide(lengths, heads, D, page, seed, spread=1.0):
+    """A cache whose block table has room for far longer contexts: the host
+    then expects work enough for the kernel of many rows."""
+    c = ref.Paged(lengths, heads, D, page, seed=seed, spread=spread)
+    table = torch.full((len(lengths), 16384), -7, dtype=torch.int32)
+    table[:, :c.table.shape[1]] = c.table
+    c.table = table
+    return c
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [0, 1, 40, 300])
+@pytest.mark.parametrize("D,page,heads,group", [(128, 64, 2, 5), (64, 16, 1, 1), (64, 32, 3, 4), (128, 16, 1, 8),
+                                                (128, 32, 1, 17), (64, 64, 2, 2)])
+def test_many_rows(env, D, page, heads, group, window, dtype):
+    lengths, news = [200, 33, 530, 1, 130, 0, 90, 64, 65], [200, 1, 137, 1, 16, 2, 90, 64, 63]
+    attention_case(env, lengths, news, heads, group, D, page, window, dtype,
+                   cache=wide(lengths, heads, D, page, seed=window + D + page))
+
+
+@pytest.mark.parametrize("lengths,news,heads,group", [([1500], [1100], 1, 1), ([3000, 2900], [150, 700], 1, 2),
+                                                      ([4000], [130], 2, 1), ([260] * 12, [256] * 12, 2, 1),
+                                                      ([600, 100, 90], [500, 1, 90], 1, 3)])
+def test_many_rows_cut_over_blocks(env, lengths, news, heads, group):
+    attention_case(env, lengths, news, heads, group, 64, 64, 0, "bf16", cache=wide(lengths, heads, 64, 64, seed=7))
+    attention_case(env, lengths, news, heads, group, 128, 16, 0, "f16", cache=wide(lengths, heads, 128, 16, seed=8))
+
+
+def test_many_rows_of_a_sequence_with_more_tokens_than_its_cache(env):
+    lengths, news = [100, 300], [250, 200]
+    attention_case(env, lengths, news, 1, 2, 64, 32, 0, "f16", cache=wide(lengths, 1, 64, 32, seed=4))
+
+
+def test_many_rows_with_one_large_logit(env):
+    fs, ctx = env
+    lengths, new = [4000], 160
+    c = wide(lengths, 1, 64, 64, seed=3, spread=0.0)
+    c.k[:] = 0
+    c.k[int(c.table[0, 0]), 0, 0, 0] = 127
+    q = torch.zeros(new, 1, 64, dtype=torch.bfloat16)
+    q[:, 0, 0] = torch.linspace(-20.0, 26.5, new)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    got = fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32(lengths), i32([0, new]), new).cpu()
+    k, v = c.values(0)
+    want = ref.attend(q, k, v, 4000 - new, 0.125)
+    bound = ref.attention_bound(q, k, v, 4000 - new, 0.125, 0, want, STEP["bf16"])
+    assert ((got.double() - want).abs() <= bound).all()
+
+
+def test_many_rows_over_pages_of_zeros_and_of_very_different_scales(env):
+    for scales in ([0.0, 1.0], [1e-3, 1e3], [1e-30, 1.0], [0.0, 0.0]):
+        c = wide([200], 1, 64, 16, seed=2)
+        for i in range(13):
+            c.v_scale[int(c.table[0, i])] = scales[i % 2]
+        attention_case(env, [200], [150], 1, 2, 64, 16, 0, "bf16", cache=c)
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
+def test_attention_scales(env, scale):
+    c = wide([300, 200], 1, 64, 64, seed=12)
+    attention_case(env, [300, 200], [150, 1], 1, 2, 64, 64, 0, "bf16", scale=scale, q_std=0.3, cache=c)
+
+
+def test_many_rows_with_queries_that_are_no_numbers_or_zero(env):
+    fs, ctx = env
+    new = 200
+    c = wide([300], 1, 64, 64, seed=3)
+    q = torch.randn(new, 2, 64, generator=gen(new)).to(torch.bfloat16)
+    q[0, 0, 5], q[7, 1, 0] = math.nan, math.inf
+    q[0, 1] = 0.0
+    q[9] *= 1e30
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    got = fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32([300]), i32([0, new]), new,
+                             ).cpu()
+    none = torch.zeros(new, 2, dtype=torch.bool)
+    none[0, 0] = none[7, 1] = True
+    assert torch.isnan(got[none]).all() and torch.isfinite(got[~none]).all()
+    k, v = c.values(0)
+    mean = v[:101, 0].mean(dim=0)
+    assert ((got[0, 1].double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 2.0 ** -10 * v.abs().amax()).all()
+
+
+def test_a_page_that_is_no_number_reaches_only_rows_that_see_it(env):
+    """A NaN scale: later rows are NaN, rows before the page are not."""
+    fs, ctx = env
+    for c, new in ((wide([300], 1, 64, 16, seed=5), 200), (ref.Paged([300], 1, 64, 16, seed=5), 40)):
+        at = 280  # a page of tokens 272 .. 287
+        c.v_scale[int(c.table[0, at // 16])] = math.nan
+        q = torch.randn(new, 1, 64, generator=gen(2)).to(torch.bfloat16)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+        got = fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32([300]), i32([0, new]),
+                                 new).cpu()
+        sees = torch.arange(300 - new, 300) >= 272
+        assert torch.isnan(got[sees]).all() and torch.isfinite(got[~sees]).all()
+
+
+def test_workspaces_of_any_contents(env):
+    """The counters of arrived parts take no contents of the workspace for a count."""
+    fs, ctx = env
+    c = ref.Paged([3000, 900], 1, 128, 64, seed=1)
+    kv = c.device(fs)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    q = torch.randn(2, 5, 128, generator=gen(1)).to(torch.bfloat16).to("cuda:0")
+    results = []
+    for fill in (0, 255, 1):
+        ws = torch.full((256 << 20,), fill, dtype=torch.uint8, device="cuda:0")
+        plan = fs.AttentionPlan(ctx, kv, q, c.table.to("cuda:0"), i32([3000, 900]), i32([0, 1, 2]), 1, workspace=ws)
+        results += [plan.run().clone(), plan.run().clone()]
+    assert all(torch.equal(bits(r), bits(results[0])) for r in results)
