@@ -32,21 +32,15 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds) {
 // Eight neighbouring elements of a row, zeros from `cols` on; `whole`: rows
 // start on multiples of 16 bytes.
 template <int TYPE>
-__device__ __forceinline__ void load8(const void *x, int64_t row, int c, int cols, bool whole, float (&v)[8]) {
+__device__ __forceinline__ void load8_of(const void *x, int64_t row, int c, int cols, bool whole, float (&v)[8]) {
   if (c + 8 <= cols) {
-    if constexpr (TYPE == kF32) {
-      __builtin_memcpy(v, (const float *)x + row + c, 32);
-    } else {
-      const uint16_t *const p = (const uint16_t *)x + row + c;
-      const int4v raw = whole ? *(const int4v *)p : load16(p);
-      for (int i = 0; i < 8; ++i) v[i] = value16<TYPE>((uint16_t)(raw[i >> 1] >> 16 * (i & 1)));
-    }
+    load8<TYPE>(x, row + c, whole, v);
   } else {
     for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? load_value<TYPE>(x, row + c + i) : 0.0f;
   }
 }
 
-__device__ __forceinline__ void store8(int8_t *out, int c, int cols, const float (&v)[8], float inverse) {
+__device__ __forceinline__ void store_codes8(int8_t *out, int c, int cols, const float (&v)[8], float inverse) {
   uint32_t word[2] = {0, 0};
   for (int i = 0; i < 8; ++i) word[i >> 2] |= (uint32_t)((int)rintf(v[i] * inverse) & 0xff) << (8 * (i & 3));
   if (c + 8 <= cols) {
@@ -70,13 +64,13 @@ __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
   uint32_t most = 0;
   if constexpr (HELD > 0) {
 #pragma unroll
-    for (int j = 0; j < HELD; ++j) load8<TYPE>(A.x, at, min(own + j * step, A.cols), A.cols, whole, v[j]);
+    for (int j = 0; j < HELD; ++j) load8_of<TYPE>(A.x, at, min(own + j * step, A.cols), A.cols, whole, v[j]);
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
       for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[j][i]));
   } else {
     for (int64_t c = own; c < A.cols; c += step) {
-      load8<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
+      load8_of<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
       for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[0][i]));
     }
   }
@@ -87,11 +81,11 @@ __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
   if constexpr (HELD > 0) {
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
-      if (own + j * step < A.cols) store8(out, own + j * step, A.cols, v[j], inverse);
+      if (own + j * step < A.cols) store_codes8(out, own + j * step, A.cols, v[j], inverse);
   } else {
     for (int64_t c = own; c < A.cols; c += step) {
-      load8<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
-      store8(out, (int)c, A.cols, v[0], inverse);
+      load8_of<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
+      store_codes8(out, (int)c, A.cols, v[0], inverse);
     }
   }
   if (threadIdx.x == 0) A.scale[row] = zero ? 0.0f : a / 127.0f;

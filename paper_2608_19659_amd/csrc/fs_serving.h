@@ -147,6 +147,31 @@ __device__ __forceinline__ float value16(uint16_t w) {
   if constexpr (TYPE == kF16) return f16_value(w);
   else return bf16_value(w);
 }
+// Eight neighbouring elements from any place; `whole`: it is a multiple of 16
+// bytes.
+template <int TYPE>
+__device__ __forceinline__ void load8(const void *x, int64_t at, bool whole, float (&v)[8]) {
+  if constexpr (TYPE == kF32) {
+    __builtin_memcpy(v, (const float *)x + at, 32);
+  } else {
+    const uint16_t *const p = (const uint16_t *)x + at;
+    const int4v raw = whole ? *(const int4v *)p : load16(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = value16<TYPE>((uint16_t)(raw[i >> 1] >> 16 * (i & 1)));
+  }
+}
+// Eight to a place that is a multiple of 16 bytes.
+template <int TYPE>
+__device__ __forceinline__ void store8(void *x, int64_t at, const float (&v)[8]) {
+  if constexpr (TYPE == kF32) {
+    __builtin_memcpy((float *)x + at, v, 32);
+  } else {
+    int4v raw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = (int)(bits16<TYPE>(v[2 * i]) | (uint32_t)bits16<TYPE>(v[2 * i + 1]) << 16);
+    *(int4v *)((uint16_t *)x + at) = raw;
+  }
+}
 #endif
 
 }  // namespace fs
