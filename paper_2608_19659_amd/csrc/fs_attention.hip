@@ -18,6 +18,16 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kFloor = -1e30f;  // a maximum over no tokens: finite, so differences stay numbers
 constexpr int kTile = 64;         // tokens of one step of a wavefront
 
+// The larger of a lane's value and of the one 32 (or 16) lanes on.
+__device__ __forceinline__ float max_over_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_over_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // ------------------------------------------------------------ who does what --
 // An item is a tile of R rows of one sequence and cache head; a row is a (new
 // token, query head of the group) pair.  An item has as many units of work as
@@ -475,8 +485,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
       float top_s = kFloor;
 #pragma unroll
       for (int i = 0; i < 16; ++i) top_s = fmaxf(top_s, sc[i]);
-      top_s = fmaxf(top_s, __shfl_xor(top_s, 16));
-      top_s = fmaxf(top_s, __shfl_xor(top_s, 32));
+      top_s = max_over_32(max_over_16(top_s));
       const float m_new = fmaxf(m, top_s);
       const float keep = __builtin_amdgcn_exp2f(m - m_new), add = __builtin_amdgcn_exp2f(top_s - m_new);
       m = m_new;
@@ -602,8 +611,9 @@ __device__ __forceinline__ void part_end() {
 // N products with an operand each from LDS, read AHEAD products ahead, which
 // covers the reads' latency (left to itself the compiler reads, waits and
 // multiplies in turn).
-template <int N, int AHEAD, class Read, class Multiply>
-__device__ __forceinline__ void products(Read read, Multiply multiply) {
+// `between` is done while products are under way.
+template <int N, int AHEAD, class Read, class Multiply, class Between>
+__device__ __forceinline__ void products(Read read, Multiply multiply, Between between) {
   half8 held[AHEAD];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) held[i] = read(i);
@@ -612,24 +622,22 @@ __device__ __forceinline__ void products(Read read, Multiply multiply) {
     __builtin_amdgcn_sched_barrier(0);
     multiply(i, held[i % AHEAD]);
     if (i + AHEAD < N) held[i % AHEAD] = read(i + AHEAD);
+    between(i);
   }
 }
 
-// 16 codes to binary16: 1024 + (code + 128) is the byte under 0x64.
-__device__ __forceinline__ void widen(int4v codes, int4v (&out)[2]) {
+// Four codes to binary16, two words: 1024 + (code + 128) is the byte under 0x64.
+__device__ __forceinline__ int2 widen(int codes) {
   using half2v = _Float16 __attribute__((ext_vector_type(2)));
   const half2v bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t b = (uint32_t)codes[i] ^ 0x80808080u;
-    const half2v a = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400)) + bias;
-    const half2v c = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402)) + bias;
-    out[i >> 1][(i & 1) * 2] = __builtin_bit_cast(int, a);
-    out[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(int, c);
-  }
+  const uint32_t b = (uint32_t)codes ^ 0x80808080u;
+  const half2v x = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400)) + bias;
+  const half2v y = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402)) + bias;
+  return {__builtin_bit_cast(int, x), __builtin_bit_cast(int, y)};
 }
 
-template <int TYPE, int D>
+// ONE: pages of 64 tokens, so a tile is a page and its address is scalar.
+template <int TYPE, int D, bool ONE>
 __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A, Share share, Parts P) {
   constexpr int kAhead = 6;
   constexpr int KK = D / 16, DT = D / 32, KC = D / 8;  // KC: 16-byte chunks of a token's binary16 keys
@@ -642,7 +650,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
   const uint32_t mine = run_of_block(), stop = min((mine + 1) * run, total);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int PS = 1 << c.page_shift;
+  const int PS = ONE ? 64 : 1 << c.page_shift;
   // this thread's piece of a tile: 16 elements of a token's keys, 16 tokens of an element's values
   const int piece = D == 128 ? threadIdx.x : threadIdx.x & 255;
   const bool of_k = D == 128 || threadIdx.x < 256, of_v = D == 128 || threadIdx.x >= 256;
@@ -721,53 +729,68 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
     int4v codes_k, codes_v;
     float scale_k = 0.0f, scale_v = 0.0f;
     const auto pages = [&](int tile) {
-      id_k = entry(tile * kTile + k_token);
-      id_v = entry(tile * kTile + v_group * 16);
+      if constexpr (ONE) {
+        id_k = id_v = table[min(max(tile, page_low), page_top)];
+      } else {
+        id_k = entry(tile * kTile + k_token);
+        id_v = entry(tile * kTile + v_group * 16);
+      }
     };
-    const auto fetch = [&](int tile) {
+    const int k_at = ((k_token & (PS - 1)) * D) + k_part * 16, v_at = v_row * PS + (v_group * 16 & (PS - 1));
+    const auto fetch = [&]() {
       const int64_t page_k = page_of(id_k), page_v = page_of(id_v);
-      if (of_k) codes_k = *(const int4v *)(c.k + (page_k * PS + ((tile * kTile + k_token) & (PS - 1))) * D + k_part * 16);
-      if (of_v) codes_v = *(const int4v *)(c.v + (page_v * D + v_row) * PS + ((tile * kTile + v_group * 16) & (PS - 1)));
+      if (of_k) codes_k = *(const int4v *)(c.k + page_k * (PS * D) + k_at);
+      if (of_v) codes_v = *(const int4v *)(c.v + page_v * (PS * D) + v_at);
       scale_v = c.v_scale[page_v];
       scale_k = c.k_scale[page_v];  // of threads 0 .. 3 the four groups'
     };
-    const auto deposit = [&](int buf) {
-      int4v wide[2];
-      if (of_k) {
-        widen(codes_k, wide);
-        lk[buf][k_place(k_token, k_part * 2)] = wide[0];
-        lk[buf][k_place(k_token, k_part * 2 + 1)] = wide[1];
+    // the codes fetched to binary16 in LDS, in eight steps
+    int4v wide_k[2], wide_v[2];
+    const auto deposit = [&](int buf, int step) {
+      const int j = step & 3;
+      if (step < 4 ? of_k : of_v) {
+        const int2 w = widen(step < 4 ? codes_k[j] : codes_v[j]);
+        int4v &to = (step < 4 ? wide_k : wide_v)[j >> 1];
+        to[(j & 1) * 2] = w.x;
+        to[(j & 1) * 2 + 1] = w.y;
+        if (step == 3) {
+          lk[buf][k_place(k_token, k_part * 2)] = wide_k[0];
+          lk[buf][k_place(k_token, k_part * 2 + 1)] = wide_k[1];
+        }
+        if (step == 7) {
+          if (scale_v < kZeroScale) wide_v[0] = wide_v[1] = int4v{0, 0, 0, 0};
+          lv[buf][v_place(v_row, v_group * 2)] = wide_v[0];
+          lv[buf][v_place(v_row, v_group * 2 + 1)] = wide_v[1];
+        }
       }
-      if (of_v) {
-        widen(codes_v, wide);
-        if (scale_v < kZeroScale) wide[0] = wide[1] = int4v{0, 0, 0, 0};
-        lv[buf][v_place(v_row, v_group * 2)] = wide[0];
-        lv[buf][v_place(v_row, v_group * 2 + 1)] = wide[1];
-      }
-      if (threadIdx.x < 4) {
+      if (step == 7 && threadIdx.x < 4) {
         const bool none = scale_v < kZeroScale;
-        scales[buf][threadIdx.x] =
-            float4v{scale_k, none ? -60.0f : __builtin_amdgcn_logf(scale_v), none ? 0x1p60f : 1.0f / scale_v, 0.0f};
+        scales[buf][threadIdx.x] = float4v{scale_k, none ? -60.0f : __builtin_amdgcn_logf(scale_v),
+                                           none ? 0x1p60f : __builtin_amdgcn_rcpf(scale_v), 0.0f};
       }
+    };
+    const auto deposit_all = [&](int buf) {
+#pragma unroll
+      for (int step = 0; step < 8; ++step) deposit(buf, step);
     };
     const int last_tile = span.y - 1;
     if (span.x < span.y) {
       pages(span.x);
-      fetch(span.x);
+      fetch();
       pages(min(span.x + 1, last_tile));
-      deposit(span.x & 3);
-      fetch(min(span.x + 1, last_tile));
+      deposit_all(span.x & 3);
+      fetch();
       pages(min(span.x + 2, last_tile));
-      deposit((span.x + 1) & 3);
-      fetch(min(span.x + 2, last_tile));
+      deposit_all((span.x + 1) & 3);
+      fetch();
       pages(min(span.x + 3, last_tile));
     }
     half8 pf[4];
     bool waiting = false;  // pf holds the tile before
-    const auto weigh = [&](int buf) {
+    const auto weigh = [&](int buf, auto between) {
       products<4 * DT, kAhead>(
           [&](int i) { return __builtin_bit_cast(half8, lv[buf][v_place(i % DT * 32 + col, i / DT * 2 + half)]); },
-          [&](int i, half8 v) { o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[i / DT], o[i % DT], 0, 0, 0); });
+          [&](int i, half8 v) { o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[i / DT], o[i % DT], 0, 0, 0); }, between);
     };
     part_end();
     if (wave >= 4) part_end();
@@ -783,11 +806,24 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
           for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
         products<2 * KK, kAhead>(
             [&](int i) { return __builtin_bit_cast(half8, lk[buf][k_place(i % 2 * 32 + tok, i / 2 * 2 + half)]); },
-            [&](int i, half8 k) { sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[i / 2], sc[i % 2], 0, 0, 0); });
+            [&](int i, half8 k) { sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[i / 2], sc[i % 2], 0, 0, 0); }, [](int) {});
       }
-      if (waiting) weigh((tile - 1) & 3);
+      // between the products tile + 2 goes to LDS: its place was last read a
+      // step ago, and it is read two steps from here
+      const int into = (tile + 2) & 3;
+      if (waiting) {
+        weigh((tile - 1) & 3, [&](int i) {
+          if (i < 8) deposit(into, i);
+        });
+      } else {
+        deposit_all(into);
+      }
       waiting = seen;
       part_end();
+      // the codes of tile + 3 (beyond the last the last again: with no
+      // condition nothing waits for the loads here)
+      fetch();
+      pages(min(tile + 4, last_tile));
       if (seen) {
         // register i of tile t: token half * 8 + i % 8 of group g = 2 t + i / 8;
         // its logit (base 2, with the value scale) is x * slope[g] + add[g]
@@ -824,7 +860,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
           for (int i = 2; i < 8; ++i) most = fmaxf(most, sc[g >> 1][f + i]);
           top_s = fmaxf(top_s, __builtin_fmaf(most, slope[g], add[g]));
         }
-        top_s = fmaxf(top_s, __shfl_xor(top_s, 32));
+        top_s = max_over_32(top_s);
         if (__any(fabsf(top_s) > 0x1p20f)) {  // logits so large that one rounding less would tell: as they are
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
@@ -859,15 +895,9 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
           l = __builtin_fmaf(sum, per[g], l);
         }
       }
-      // tile + 2, read first two parts from here; its place was last read two
-      // parts ago.  Beyond the last tile it is the last again: with no
-      // condition nothing waits for the loads here.
-      deposit((tile + 2) & 3);
-      fetch(min(tile + 3, last_tile));
-      pages(min(tile + 4, last_tile));
       part_end();
     }
-    if (waiting) weigh(last_tile & 3);
+    if (waiting) weigh(last_tile & 3, [](int) {});
     if (wave < 4) part_end();
     part_end();
     l += __shfl_xor(l, 32);
@@ -1016,9 +1046,9 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   if (chunks) {  // a sequence alone has no other kernel, whatever it turns out to be
     const Share many{8, A.n_seqs == 1 ? 1 : kChunkLeast, everything};
     P.call = next_call();
-    e = allow_lds(&k_attend_chunk<TYPE, D>, lds);
+    e = allow_lds(&k_attend_chunk<TYPE, D, ONE>, lds);
     if (e != hipSuccess) return e;
-    k_attend_chunk<TYPE, D><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
+    k_attend_chunk<TYPE, D, ONE><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
     if (A.n_seqs == 1) return hipGetLastError();
   }
   const Share few{4, 1, chunks ? kChunkLeast : everything};
