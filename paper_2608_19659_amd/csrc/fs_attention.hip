@@ -1011,12 +1011,6 @@ __global__ void k_check_attention(AttendArgs A, int32_t *flag) {
 constexpr int kRowBlocks = 512, kChunkBlocks = 256;
 static_assert(kRowBlocks < 4096, "counts of parts have 12 bits");
 
-template <class Kernel>
-hipError_t allow_lds(Kernel kernel, size_t bytes) {  // beyond 64 KB with the static part
-  if (bytes <= 16384) return hipSuccess;
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
-
 unsigned long long next_call() {  // a number that no other call of the process has; from a random start
   static std::atomic<unsigned long long> number{((unsigned long long)std::random_device{}() << 20) ^
                                                 (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count()};

@@ -40,15 +40,28 @@ __device__ __forceinline__ void load8_of(const void *x, int64_t row, int c, int 
   }
 }
 
+// Eight codes: x * inverse (of at most 127) to the nearest whole number, ties to
+// even, by the addition of 1.5 * 2^23, whose result holds it in its low byte.
+__device__ __forceinline__ int2 codes8(const float (&v)[8], float inverse) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i] * inverse + 12582912.0f);
+  int word[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    word[i] = (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm(w[4 * i + 3], w[4 * i + 2], 0x0c0c0400),
+                                         __builtin_amdgcn_perm(w[4 * i + 1], w[4 * i], 0x0c0c0400), 0x05040100);
+  return {word[0], word[1]};
+}
+
 __device__ __forceinline__ void store_codes8(int8_t *out, int c, int cols, const float (&v)[8], float inverse) {
-  uint32_t word[2] = {0, 0};
-  for (int i = 0; i < 8; ++i) word[i >> 2] |= (uint32_t)((int)rintf(v[i] * inverse) & 0xff) << (8 * (i & 3));
+  const int2 word = codes8(v, inverse);
   if (c + 8 <= cols) {
-    __builtin_memcpy(out + c, word, 8);
+    __builtin_memcpy(out + c, &word, 8);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < cols) out[c + i] = (int8_t)(word[i >> 2] >> (8 * (i & 3)));
+      if (c + i < cols) out[c + i] = (int8_t)((i < 4 ? word.x : word.y) >> (8 * (i & 3)));
   }
 }
 
@@ -226,6 +239,54 @@ __device__ __forceinline__ int2 place(int i) {
   return {r, (slot % S::CH ^ turn<S::BK>(r)) * 16};
 }
 
+// The sums of the wavefronts that share a tile meet in LDS, each tile at its
+// first one; the others are done.
+template <class S>
+__device__ __forceinline__ bool join_parts(int8_t *lds, int wk, int wave, int lane, int4v (&acc)[S::MT][S::NT]) {
+  if constexpr (S::WK > 1) {
+    __syncthreads();
+    int4v *const sums = (int4v *)lds;
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) sums[(wave * S::MT * S::NT + i * S::NT + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    if (wk > 0) return false;
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j)
+        for (int p = 1; p < S::WK; ++p)
+          acc[i][j] += sums[((p * S::TILES + wave) * S::MT * S::NT + i * S::NT + j) * 64 + lane];
+  }
+  return true;
+}
+
+// A wavefront's part of a tile, from token m and channel n on.
+template <class S>
+__device__ __forceinline__ void store_tile(const MatmulArgs &A, int m, int n, int lane, int4v (&acc)[S::MT][S::NT],
+                                           const float (&sa)[S::MT]) {
+  // the scales first, all loads under way together
+  float4v sw[S::NT], bias[S::NT];
+  const auto channels = [&](const float *from, float4v (&to)[S::NT]) {
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[j][i] = from[min(n + j * 16 + (lane >> 4) * 4 + i, A.N - 1)];
+  };
+  channels(A.w_scale, sw);
+  if (A.bias) channels(A.bias, bias);
+#pragma unroll
+  for (int i = 0; i < S::MT; ++i) {
+    const int row = m + i * 16 + (lane & 15);
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+      const int channel = n + j * 16 + (lane >> 4) * 4;
+      if (row < A.M && channel < A.N) store_products<S::TYPE>(A, row, channel, acc[i][j], sa[i], sw[j], bias[j]);
+    }
+  }
+}
+
 // DIRECT: rows start on multiples of 16 bytes.
 template <class S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m, int tiles_n) {
@@ -313,44 +374,139 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
       }
     }
   }
-  if constexpr (S::WK > 1) {  // the parts' sums meet in LDS, each tile at its first wavefront
-    __syncthreads();
-    int4v *const sums = (int4v *)lds;
-#pragma unroll
-    for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-      for (int j = 0; j < S::NT; ++j) sums[(wave * S::MT * S::NT + i * S::NT + j) * 64 + lane] = acc[i][j];
-    __syncthreads();
-    if (wk > 0) return;
-#pragma unroll
-    for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-      for (int j = 0; j < S::NT; ++j)
-        for (int p = 1; p < S::WK; ++p)
-          acc[i][j] += sums[((p * S::TILES + wave) * S::MT * S::NT + i * S::NT + j) * 64 + lane];
-  }
-  // the scales first, all loads under way together
+  if (!join_parts<S>(lds, wk, wave, lane, acc)) return;
   float sa[S::MT];
-  float4v sw[S::NT], bias[S::NT];
 #pragma unroll
   for (int i = 0; i < S::MT; ++i) sa[i] = A.a_scale[min(m0 + wm + i * 16 + (lane & 15), A.M - 1)];
-  const auto channels = [&](const float *from, float4v (&to)[S::NT]) {
+  store_tile<S>(A, m0 + wm, n0 + wn, lane, acc, sa);
+}
+
+// ------------------------------------------------- few rows, in one launch --
+// A projection of up to four rows: every block makes the codes of all of them
+// itself, so that no kernel has to end before another starts.  The rows go to
+// LDS as they are, behind them the first stages of weights are under way while
+// the largest values are found and the codes made.  A last stage that passes
+// K ends in codes of zero, and its weights are the row's last ones again.
+constexpr int kFewRows = 4, kFewThreads = 512, kFewBytes = 152 << 10;
+
+// Codes of the rows in LDS (`raw`, rows `raw_pitch` bytes apart) and their
+// scales.  The block's wavefronts share out the rows.
+template <class S, int XTYPE>
+__device__ __forceinline__ void codes_in_lds(const int8_t *raw, int raw_pitch, int8_t *codes, int pitch, float *scales,
+                                             uint32_t *most_of, int M, int K, int wave, int lane) {
+  const int each = S::WAVES / (M == 1 ? 1 : M == 2 ? 2 : 4);  // wavefronts of a row
+  const int row = wave / each, first = (wave % each * 64 + lane) * 8, step = each * 512;
+  const int8_t *const from = raw + row * raw_pitch;
+  uint32_t most = 0;
+  if (row < M) {
+    if constexpr (XTYPE == kF32) {
+      for (int c = first; c < K; c += step) {
+        float v[8];
+        load8<XTYPE>(from, c, true, v);
 #pragma unroll
-    for (int j = 0; j < S::NT; ++j)
+        for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
+      }
+    } else {  // without the sign the types' words are in the values' order
+      using short2 = uint16_t __attribute__((ext_vector_type(2)));
+      short2 two = {0, 0};
+      for (int c = first; c < K; c += step) {
+        const int4v raw = *(const int4v *)(from + 2 * c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) to[j][i] = from[min(n0 + wn + j * 16 + (lane >> 4) * 4 + i, A.N - 1)];
-  };
-  channels(A.w_scale, sw);
-  if (A.bias) channels(A.bias, bias);
-#pragma unroll
-  for (int i = 0; i < S::MT; ++i) {
-    const int m = m0 + wm + i * 16 + (lane & 15);
-#pragma unroll
-    for (int j = 0; j < S::NT; ++j) {
-      const int n = n0 + wn + j * 16 + (lane >> 4) * 4;
-      if (m < A.M && n < A.N) store_products<S::TYPE>(A, m, n, acc[i][j], sa[i], sw[j], bias[j]);
+        for (int i = 0; i < 4; ++i) two = __builtin_elementwise_max(two, __builtin_bit_cast(short2, raw[i] & 0x7fff7fff));
+      }
+      most = magnitude(value16<XTYPE>(max(two.x, two.y)));
     }
   }
+  for (int o = 32; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  if (lane == 0) most_of[wave] = most;
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // LDS only: the weights' loads stay under way
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  for (int i = 0; i < each; ++i) most = max(most, most_of[row * each + i]);
+  const float a = __uint_as_float(most);
+  const bool zero = a < kTiny;
+  const float inverse = zero ? 0.0f : 127.0f / a;
+  if (row < M) {
+    for (int c = first; c < pitch; c += step) {
+      float v[8] = {};
+      if (c < K) load8<XTYPE>(from, c, true, v);
+      *(int2 *)(codes + row * pitch + c) = codes8(v, c < K ? inverse : 0.0f);
+    }
+    if (first == 0) scales[row] = zero ? 0.0f : a / 127.0f;
+  }
+  asm volatile("" ::: "memory");
+}
+
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void k_linear_few(QuantizeArgs X, MatmulArgs A, int tiles_n) {
+  extern __shared__ __attribute__((aligned(1024))) int8_t few_lds[];
+  __shared__ float scales[kFewRows];
+  __shared__ uint32_t most_of[S::WAVES];
+  constexpr int STAGE = S::BN * S::BK;
+  const int per = (tiles_n + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= tiles_n) return;
+  const int n0 = id * S::BN, stages = (A.K + S::BK - 1) / S::BK;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wk = wave / S::TILES, wn = wave % S::TILES * S::WN;
+  const int x_bytes = A.K * (X.type == kF32 ? 4 : 2), x_loads = (x_bytes + S::THREADS * 16 - 1) / (S::THREADS * 16);
+  const int raw_pitch = x_loads * S::THREADS * 16, pitch = stages * S::BK + 64;
+  int8_t *const raw = few_lds + S::NS * STAGE, *const codes = raw + A.M * raw_pitch;
+  const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)few_lds + wave * 1024;
+
+  for (int m = 0; m < A.M; ++m)
+    for (int i = 0; i < x_loads; ++i)
+      load_to_lds((const int8_t *)X.x + m * X.x_stride * (X.type == kF32 ? 4 : 2),
+                  (uint32_t)min((i * S::THREADS + (int)threadIdx.x) * 16, x_bytes - 16),
+                  base + S::NS * STAGE + m * raw_pitch + i * S::THREADS * 16);
+  const int8_t *const tw = A.w + (int64_t)n0 * A.w_stride;
+  uint32_t row_at[S::LW];
+  int in_row[S::LW];
+#pragma unroll
+  for (int i = 0; i < S::LW; ++i) {
+    const int2 at = place<S>(i);
+    row_at[i] = (uint32_t)min(at.x, A.N - 1 - n0) * (uint32_t)A.w_stride;
+    in_row[i] = at.y;
+  }
+  const auto load = [&](int t, int slot) {
+#pragma unroll
+    for (int i = 0; i < S::LW; ++i)
+      load_to_lds(tw, row_at[i] + min(t * S::BK + in_row[i], A.K - 16), base + slot * STAGE + i * S::THREADS * 16);
+  };
+  for (int t = 0; t < S::NS - 1 && t < stages; ++t) load(t, t);
+  if (stages >= S::NS - 1) wait_loads<(S::NS - 1) * S::LW>();
+  else wait_loads<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  if (X.type == kF32) codes_in_lds<S, kF32>(raw, raw_pitch, codes, pitch, scales, most_of, A.M, A.K, wave, lane);
+  else if (X.type == kF16) codes_in_lds<S, kF16>(raw, raw_pitch, codes, pitch, scales, most_of, A.M, A.K, wave, lane);
+  else codes_in_lds<S, kBF16>(raw, raw_pitch, codes, pitch, scales, most_of, A.M, A.K, wave, lane);
+
+  int4v acc[1][S::NT] = {};
+  const int r = lane & 15;
+  const int8_t *const own = codes + min(r, A.M - 1) * pitch;  // the rows beyond M are no one's
+  constexpr int STEPS = S::BK / 64 / S::WK;
+  for (int t = 0, slot = 0; t < stages; ++t, slot = slot == S::NS - 1 ? 0 : slot + 1) {
+    const int left = stages - 1 - t;
+    wait_stage<S::NS, S::LW>(left);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (left >= S::NS - 1) load(t + S::NS - 1, slot ? slot - 1 : S::NS - 1);
+    const int8_t *const lw = few_lds + slot * STAGE;
+#pragma unroll
+    for (int kk = 0; kk < STEPS; ++kk) {
+      const int chunk = (wk * STEPS + kk) * 4 + (lane >> 4);
+      const int4v fa = *(const int4v *)(own + t * S::BK + chunk * 16);
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        const int4v fw = *(const int4v *)(lw + (wn + j * 16 + r) * S::BK + (chunk ^ turn<S::BK>(r)) * 16);
+        acc[0][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fa, acc[0][j], 0, 0, 0);
+      }
+    }
+  }
+  if (!join_parts<S>(few_lds, wk, wave, lane, acc)) return;
+  const float sa[1] = {scales[min(r, A.M - 1)]};
+  store_tile<S>(A, 0, n0 + wn, lane, acc, sa);
 }
 
 template <int TYPE, int THREADS, int HELD>
@@ -425,7 +581,45 @@ hipError_t matmul_of(const MatmulArgs &A, hipStream_t s) {
   }
 }
 
+template <int TYPE, int BN, int WK, int NS>
+hipError_t few_as(const QuantizeArgs &X, const MatmulArgs &A, int64_t rows_bytes, hipStream_t s) {
+  using S = Shape<TYPE, 16, BN, 16, 16, 512, WK, NS>;
+  constexpr int RING = S::NS * S::BN * S::BK;
+  static_assert(RING >= S::WAVES * S::NT * 1024, "the parts' sums fit the ring");
+  static_assert(S::THREADS == kFewThreads, "whole loads of a row");
+  const hipError_t e = allow_lds(&k_linear_few<S>, kFewBytes);
+  if (e != hipSuccess) return e;
+  const int tiles = (A.N + BN - 1) / BN;
+  k_linear_few<S><<<(tiles + 7) / 8 * 8, S::THREADS, (size_t)(RING + rows_bytes), s>>>(X, A, tiles);
+  return hipGetLastError();
+}
+
+// Where one launch is faster than two: a block a CU or less, or a single row
+// and two blocks a CU.  (bfloat16, us of one launch and of two: 1 x 7168 x 5120
+// 9.5 and 12.5, 4 rows 11.3 and 12.7; 1 x 896 x 5120 5.9 and 8.2; 1 x 5120 x 640
+// 4.6 and 8.2; 1 x 5120 x 20480 23.8 and 28.9; 1 x 10240 x 5120 13.2 and 16.1;
+// 4 x 10240 x 5120 18.9 and 16.5, where every CU makes the codes twice.  896
+// channels in tiles of 32: 7.1.)
+template <int TYPE>
+bool few_of(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_t *e) {
+  const int64_t size = X.type == kF32 ? 4 : 2, load = kFewThreads * 16;
+  const int64_t bytes = A.M * ((A.K * size + load - 1) / load * load + (A.K + 511) / 512 * 512 + 64);
+  if (A.N <= 256 * 16 && 6 * 8192 + bytes <= kFewBytes) *e = few_as<TYPE, 16, 8, 6>(X, A, bytes, s);
+  else if (A.N <= 256 * 32 && 4 * 16384 + bytes <= kFewBytes) *e = few_as<TYPE, 32, 4, 4>(X, A, bytes, s);
+  else if (A.M == 1 && 3 * 16384 + bytes <= 80 << 10) *e = few_as<TYPE, 32, 4, 3>(X, A, bytes, s);
+  else return false;
+  return true;
+}
+
 }  // namespace
+
+bool launch_linear_few(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_t *e) {
+  const int64_t size = X.type == kF32 ? 4 : 2;
+  if (A.M > kFewRows || A.K < 16 || A.K % 16 || A.w_stride > (1 << 23)) return false;
+  // loads of 16 bytes, of a row's own
+  if (((uintptr_t)X.x | (uintptr_t)(A.M > 1 ? X.x_stride * size : 0) | (uintptr_t)A.w | (uintptr_t)A.w_stride) & 15) return false;
+  return A.out_type == kF32 ? few_of<kF32>(X, A, s, e) : A.out_type == kF16 ? few_of<kF16>(X, A, s, e) : few_of<kBF16>(X, A, s, e);
+}
 
 hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s) {
   return A.type == kF32 ? quantize_of<kF32>(A, s) : A.type == kF16 ? quantize_of<kF16>(A, s) : quantize_of<kBF16>(A, s);

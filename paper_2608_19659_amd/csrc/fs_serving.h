@@ -34,6 +34,10 @@ struct MatmulArgs {
 size_t matmul_workspace(int32_t M, int32_t N, int32_t K);
 hipError_t launch_scaled_matmul(const MatmulArgs &A, void *ws, hipStream_t s);
 
+// Both steps in one launch where there are few rows (codes and scales stay
+// unset); false: not for this call, nothing done.
+bool launch_linear_few(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_t *e);
+
 struct Cache {
   int8_t *k, *v;
   float *k_scale, *v_scale;
@@ -83,6 +87,12 @@ hipError_t launch_check_slots(const Cache &c, const int32_t *slots, const int32_
 hipError_t launch_check_attention(const AttendArgs &A, int32_t *flag, hipStream_t s);
 
 #ifdef __HIPCC__
+template <class Kernel>
+inline hipError_t allow_lds(Kernel kernel, size_t bytes) {  // beyond 64 KB with the static part
+  if (bytes <= 16384) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
 using half8 = _Float16 __attribute__((ext_vector_type(8)));
 using float4v = float __attribute__((ext_vector_type(4)));
 using float16v = float __attribute__((ext_vector_type(16)));

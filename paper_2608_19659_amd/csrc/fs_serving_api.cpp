@@ -162,12 +162,15 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
   if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
   int8_t *const codes = (int8_t *)d_workspace;
   float *const scale = (float *)(codes + linear_codes(M, K));
-  const hipError_t e = fs::launch_quantize_rows(
-      {d_x, codes, scale, x_stride, padded(K), (int32_t)M, (int32_t)K, (int32_t)type}, stream);
+  const fs::QuantizeArgs rows{d_x, codes, scale, x_stride, padded(K), (int32_t)M, (int32_t)K, (int32_t)type};
+  const fs::MatmulArgs product{codes, d_w, scale, d_w_scale, d_bias, d_out, padded(K), w_stride, out_stride, (int32_t)M,
+                               (int32_t)N, (int32_t)K, (int32_t)out_type};
+  hipError_t e = hipSuccess;
+  if (fs::launch_linear_few(rows, product, stream, &e))
+    return e == hipSuccess ? FS_OK : hip_fail(e, "linear launch");
+  e = fs::launch_quantize_rows(rows, stream);
   if (e != hipSuccess) return hip_fail(e, "quantize launch");
-  return matmul({codes, d_w, scale, d_w_scale, d_bias, d_out, padded(K), w_stride, out_stride, (int32_t)M, (int32_t)N,
-                 (int32_t)K, (int32_t)out_type},
-                (uint8_t *)scale + align256(4 * (size_t)M), stream);
+  return matmul(product, (uint8_t *)scale + align256(4 * (size_t)M), stream);
 }
 
 fs_status fs_cache_append(fs_context *ctx, const fs_kv_cache *cache, const void *d_k, int64_t k_stride,

@@ -64,7 +64,7 @@ class Class:
     slo: float
 
 
-CLASSES = (Class("chat", 1024, 256, 40.0, 3.5), Class("code", 2048, 32, 40.0, 0.6))
+CLASSES = (Class("chat", 1024, 256, 16.0, 3.0), Class("code", 2048, 32, 12.0, 0.6))
 LEVELS = (1.0, 2.0, 4.0, 8.0, 16.0, 32.0)
 
 

@@ -724,3 +724,41 @@ def test_workspaces_of_any_contents(env):
         plan = fs.AttentionPlan(ctx, kv, q, c.table.to("cuda:0"), i32([3000, 900]), i32([0, 1, 2]), 1, workspace=ws)
         results += [plan.run().clone(), plan.run().clone()]
     assert all(torch.equal(bits(r), bits(results[0])) for r in results)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("N,K", [(100, 16), (16, 512), (33, 528), (4096, 64), (4097, 1040), (5120, 640), (8193, 1536),
+                                 (8200, 48), (30, 5120), (4200, 6160), (6, 20480)])
+def test_linear_of_few_rows(env, M, N, K, dtype):
+    """Rows that start on multiples of 16 bytes, whose codes may be made where
+    they are used: the bits are those of the two calls."""
+    fs, ctx = env
+    note(f"few {M}x{N}x{K} {dtype}")
+    x = (torch.randn(M, K + 16, generator=gen(K)) * 2).to(TYPES[dtype])[:, :K]
+    if M > 2:
+        x[1] = 0.0
+        x[2, K - 1], x[2, 0] = 1e4, -1e-3
+    x = x.to("cuda:0")
+    _, _, w, sw, bias = products(1, N, K, 5)
+    wide = torch.full((N, K + 32), 77, dtype=torch.int8)
+    wide[:, :K] = w
+    w, sw, bias = wide.to("cuda:0")[:, :K], sw.to("cuda:0"), bias.to("cuda:0")
+    codes, scale = fs.quantize_rows(ctx, x)
+    for b in (bias, None):
+        two = fs.scaled_matmul(ctx, codes, scale, w, sw, b, out_dtype=TYPES[dtype])
+        out = torch.full((M, N + 5), 9.0, dtype=TYPES[dtype], device="cuda:0")
+        one = fs.linear(ctx, x, w, sw, b, out=out[:, :N])
+        assert torch.equal(bits(one.contiguous()), bits(two))
+        assert (out[:, N:] == 9.0).all()
+
+
+def test_linear_of_few_rows_that_are_no_numbers(env):
+    fs, ctx = env
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn(4, 256, generator=gen(4)).to(dtype)
+        x[1, 5], x[2, 199] = math.nan, -math.inf
+        x[0] = 0.0
+        _, _, w, sw, _ = products(1, 50, 256, 5)
+        y = fs.linear(ctx, x.to("cuda:0"), w.to("cuda:0"), sw.to("cuda:0")).cpu()
+        assert (y[0] == 0).all() and not torch.isfinite(y[1:3]).any() and torch.isfinite(y[3:]).all()
