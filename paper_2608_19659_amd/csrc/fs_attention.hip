@@ -7,7 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <chrono>
-#include <random>
+#include <type_traits>
 
 #include "fs_serving.h"
 
@@ -321,8 +321,6 @@ __device__ void join(const AttendArgs &A, const Item &it, const Rows &of, int ro
 // scale is added to the exponent (log2), so one tile may span pages; the sum
 // of the softmax is kept in binary32 without it.
 
-// A wavefront loads its next tile while it works on one.
-
 // Four sums with 128 in them to their second bytes, and their first as signed.
 __device__ __forceinline__ int2 split_bytes(const uint32_t (&b)[4]) {
   const uint32_t u = __builtin_amdgcn_perm(b[1], b[0], 0x05010400), v = __builtin_amdgcn_perm(b[3], b[2], 0x05010400);
@@ -344,10 +342,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
   const int row = lane & 15, G = lane >> 4, kg = row >> 2;
   const int PS = ONE ? 64 : 1 << c.page_shift;
 
-  struct Tile {
-    int4v k[4][STEPS], v[DT];
-    float ks, vs;
-  };
   const uint32_t stop = min((mine + 1) * run, total);
   for (uint32_t unit = mine * run; unit < stop;) {
     const Item it = item_at<kRows>(A, group, share, pre, unit);
@@ -380,26 +374,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
         id_v = table[min(max((tok + G * 16) >> c.page_shift, page_low), page_top)];
       }
     };
-    const auto fetch = [&](int tile, Tile &t) {
-      const auto page = [&](int32_t id) { return (int64_t)min((uint32_t)id, (uint32_t)(c.n_pages - 1)) * c.n_heads + h; };
+    // One place for a tile's keys and one for its values: the next tile's are
+    // asked for as soon as this one's have been multiplied.  (With two places for
+    // whole tiles, and the loop's body twice, 4 users of 131072 tokens took 53.7
+    // us instead of 50.0, 64 of 512 to 8192 74.6 instead of 73.5.)
+    const auto page = [&](int32_t id) { return (int64_t)min((uint32_t)id, (uint32_t)(c.n_pages - 1)) * c.n_heads + h; };
+    int4v tk[4][STEPS], tv[DT];
+    float next_ks = 0.0f, next_vs = 0.0f;
+    const auto fetch_k = [&](int tile) {
       const int64_t pk = page(id_k), pv = page(id_v);
-      const int at_k = ONE ? kg * 16 : (tile * kTile + kg * 16) & (PS - 1), at_v = ONE ? G * 16 : (tile * kTile + G * 16) & (PS - 1);
+      const int at_k = ONE ? kg * 16 : (tile * kTile + kg * 16) & (PS - 1);
       const int8_t *const kp = c.k + pk * (PS * D) + ((at_k + (row & 3)) * D + G * 16);
-      const int8_t *const vp = c.v + pv * (PS * D) + (row * PS + at_v);
-      t.ks = c.k_scale[pv];
-      t.vs = c.v_scale[pv];
+      next_ks = c.k_scale[pv];
+      next_vs = c.v_scale[pv];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) t.k[i][st] = *(const int4v *)(kp + i * 4 * D + st * 64);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) t.v[dt] = *(const int4v *)(vp + dt * 16 * PS);
+        for (int st = 0; st < STEPS; ++st) tk[i][st] = *(const int4v *)(kp + i * 4 * D + st * 64);
     };
-    Tile ta, tb;
+    const auto fetch_v = [&](int tile) {
+      const int at_v = ONE ? G * 16 : (tile * kTile + G * 16) & (PS - 1);
+      const int8_t *const vp = c.v + page(id_v) * (PS * D) + (row * PS + at_v);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) tv[dt] = *(const int4v *)(vp + dt * 16 * PS);
+    };
     int tile = span.x + wave;
     if (tile < span.y) {
       pages(tile);
-      fetch(tile, ta);
+      fetch_k(tile);
+      fetch_v(tile);
       if (tile + WAVES < span.y) pages(tile + WAVES);
     }
 
@@ -452,7 +455,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     float m = kFloor, l = 0.0f;
-    const auto work = [&](int tile, const Tile &t) {
+    for (; tile < span.y; tile += WAVES) {
       const int base = tile * kTile;
       float sc[16];
 #pragma unroll
@@ -460,14 +463,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
         int4v hi = {0, 0, 0, 0}, low_sum = {0, 0, 0, 0};
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-          hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.k[j][st], q_hi[st], hi, 0, 0, 0);
-          low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.k[j][st], q_lo[st], low_sum, 0, 0, 0);
+          hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(tk[j][st], q_hi[st], hi, 0, 0, 0);
+          low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(tk[j][st], q_lo[st], low_sum, 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) sc[j * 4 + i] = (float)(hi[i] * 256 + low_sum[i]);
       }
       // sc[i]: token base + G * 16 + i
-      float ks = t.ks, vs = t.vs;
+      float ks = next_ks, vs = next_vs;
+      const bool more = tile + WAVES < span.y;
+      if (more) fetch_k(tile + WAVES);
       const bool edge = base < all_low || base + kTile - 1 > all_top;  // some row does not see all of it
       int least = first_seen - base - G * 16, most = last_seen - base - G * 16;
       if (edge && (most < 0 || least > 15)) ks = vs = 1.0f;  // no page of this row's
@@ -516,27 +521,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const int4v none = {0, 0, 0, 0};
-        const int4v hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.v[dt], p_hi, none, 0, 0, 0);
-        const int4v low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.v[dt], p_lo, none, 0, 0, 0);
+        const int4v hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(tv[dt], p_hi, none, 0, 0, 0);
+        const int4v low_sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(tv[dt], p_lo, none, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           o[dt][i] = __builtin_fmaf((float)(hi[i] * 256 + low_sum[i]), step, o[dt][i]);
       }
-    };
-    while (tile < span.y) {
-      if (tile + WAVES < span.y) {
-        fetch(tile + WAVES, tb);
+      if (more) {
+        fetch_v(tile + WAVES);
         if (tile + 2 * WAVES < span.y) pages(tile + 2 * WAVES);
       }
-      work(tile, ta);
-      tile += WAVES;
-      if (tile >= span.y) break;
-      if (tile + WAVES < span.y) {
-        fetch(tile + WAVES, ta);
-        if (tile + 2 * WAVES < span.y) pages(tile + 2 * WAVES);
-      }
-      work(tile, tb);
-      tile += WAVES;
     }
     // the row's sum over the four lanes that hold it, then the wavefronts
     l += __shfl_xor(l, 16);
@@ -1011,9 +1005,12 @@ __global__ void k_check_attention(AttendArgs A, int32_t *flag) {
 constexpr int kRowBlocks = 512, kChunkBlocks = 256;
 static_assert(kRowBlocks < 4096, "counts of parts have 12 bits");
 
-unsigned long long next_call() {  // a number that no other call of the process has; from a random start
-  static std::atomic<unsigned long long> number{((unsigned long long)std::random_device{}() << 20) ^
-                                                (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count()};
+// A number that no other call of the process has; the start differs from process
+// to process (a clock and where the program lies; nothing here may throw).
+unsigned long long next_call() {
+  static std::atomic<unsigned long long> number{
+      (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull ^
+      (unsigned long long)(uintptr_t)&next_call};
   unsigned long long n;
   do n = ++number << 12;
   while (n == 0);
@@ -1046,15 +1043,27 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
     if (A.n_seqs == 1) return hipGetLastError();
   }
   const Share few{4, 1, chunks ? kChunkLeast : everything};
-  // parts of an item: by the length of its context, or by its share of the blocks
-  const int64_t items = std::max<int64_t>(1, (int64_t)A.n_seqs * A.c.n_heads * ((std::min<int64_t>(most_rows, kChunkLeast) + kRows - 1) / kRows));
-  const bool few_parts = std::min((tiles - kItemUnits) / few.least, 2 * kRowBlocks / items) < 12;
-  P.call = few_parts ? next_call() : 0;
-  e = allow_lds(&k_attend_rows<TYPE, D, 4, ONE>, lds);
-  if (e != hipSuccess) return e;
-  k_attend_rows<TYPE, D, 4, ONE><<<kRowBlocks, 256, lds, s>>>(A, few, P);
-  if (!few_parts) k_join<TYPE, D><<<kRowBlocks - 1, 64 * kJoinWaves, lds, s>>>(A, few, kRowBlocks, P.floats);
-  return hipGetLastError();
+  // Two blocks a CU of four wavefronts, or where there are fewer items than CUs
+  // one of eight, which have half the tiles each before the parts are joined.
+  // (us a call, four and eight: 4 users of 1000 tokens and 8 heads 14.6 and
+  // 11.8, 64 of 1000 and one head 15.3 and 12.0, 4 of 4000 and one head 19.8 and
+  // 16.5, one of 1000 and one head 9.8 and 10.0; 32 of 4000 and 8 heads, 256
+  // items, 27.1 and 29.1, 64 of 512 to 8192 73.5 and 94.7.)
+  const auto rows = [&](auto waves_of) {
+    constexpr int WAVES = decltype(waves_of)::value, BLOCKS = kRowBlocks * 4 / WAVES;
+    // parts of an item: by the length of its context, or by its share of the blocks
+    const int64_t items = std::max<int64_t>(1, (int64_t)A.n_seqs * A.c.n_heads * ((std::min<int64_t>(most_rows, kChunkLeast) + kRows - 1) / kRows));
+    const bool few_parts = std::min((tiles - kItemUnits) / few.least, 2 * BLOCKS / items) < 12;
+    P.call = few_parts ? next_call() : 0;
+    hipError_t e = allow_lds(&k_attend_rows<TYPE, D, WAVES, ONE>, lds);
+    if (e != hipSuccess) return e;
+    k_attend_rows<TYPE, D, WAVES, ONE><<<BLOCKS, 64 * WAVES, lds, s>>>(A, few, P);
+    if (!few_parts) k_join<TYPE, D><<<BLOCKS - 1, 64 * kJoinWaves, lds, s>>>(A, few, BLOCKS, P.floats);
+    return hipGetLastError();
+  };
+  // about what there is: a sequence has a token at least
+  const int64_t likely = ((int64_t)A.n_seqs * ((group + kRows - 1) / kRows) + std::max(0, A.n_tokens - A.n_seqs) * group / kRows) * A.c.n_heads;
+  return likely <= 224 ? rows(std::integral_constant<int, 8>{}) : rows(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
