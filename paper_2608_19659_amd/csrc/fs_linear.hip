@@ -186,6 +186,7 @@ __device__ __forceinline__ void load_to_lds(const int8_t *base, uint32_t offset,
 template <int LOADS>
 __device__ __forceinline__ void wait_loads() {
   static_assert(LOADS < 64, "the counter has 6 bits");
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt((LOADS & 15) | (LOADS >> 4) << 14 | 7 << 4);
 }
 
@@ -287,8 +288,12 @@ __device__ __forceinline__ void store_tile(const MatmulArgs &A, int m, int n, in
   }
 }
 
-// DIRECT: rows start on multiples of 16 bytes.
-template <class S, bool DIRECT>
+// Which operands go from memory to LDS as they are: both where all rows start on
+// multiples of 16 bytes, the codes where those rows do and hold whole pieces of
+// 16 (fs_linear's own do whatever K is), else none.
+enum Direct { kBoth, kCodes, kNone };
+
+template <class S, Direct DIRECT>
 __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m, int tiles_n) {
   __shared__ __attribute__((aligned(1024))) int8_t lds[S::BYTES];
   // Workgroups go round the eight XCDs in turn: each XCD gets a run of tiles,
@@ -306,7 +311,58 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
   int4v acc[S::MT][S::NT] = {};
   int done = 0;
 
-  if constexpr (DIRECT) {
+  if constexpr (DIRECT == kCodes) {
+    // Weights at any alignment go through registers to their slot of the ring,
+    // a stage or two ahead, behind the codes of the same stage.  The last stage's
+    // weights end in zeros, so whatever codes stand beside them are of no account:
+    // places beyond the row take its last piece.  (us a call, so and with
+    // both operands through registers: 333 x 1001 x 1999 11.8 and 14.6, 64 x 5001 x
+    // 5119 17.4 and 23.1, 3000 x 5001 x 2999 78 and 90.)
+    constexpr int AHEAD = S::NS >= 3 && S::MT * S::NT <= 8 ? 2 : 1;
+    const int stages = (A.K + S::BK - 1) / S::BK;
+    const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)lds + wave * 1024;
+    Piece rw[AHEAD][S::LW];
+    uint32_t row_a[S::LA];
+    const int8_t *pw[S::LW];
+#pragma unroll
+    for (int i = 0; i < S::LA; ++i) row_a[i] = (uint32_t)min(place<S>(i).x, last_a) * (uint32_t)A.a_stride;
+#pragma unroll
+    for (int i = 0; i < S::LW; ++i) pw[i] = tw + (int64_t)min(place<S>(i).x, last_w) * A.w_stride;
+    const int last_piece = (A.K - 1) & ~15;
+    const auto fetch = [&](int p, int t, int slot) {
+#pragma unroll
+      for (int i = 0; i < S::LA; ++i)
+        load_to_lds(ta, row_a[i] + min(t * S::BK + place<S>(i).y, last_piece), base + slot * S::STAGE + i * S::THREADS * 16);
+      const bool over = (t + 1) * S::BK > A.K;
+#pragma unroll
+      for (int i = 0; i < S::LW; ++i) rw[p][i].load(pw[i], t * S::BK + place<S>(i).y, A.K, over);
+    };
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p)
+      if (p < stages) fetch(p, p, p);
+    for (int t0 = 0, slot = 0; t0 < stages; t0 += AHEAD) {
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p) {
+        const int t = t0 + p;
+        if (t >= stages) break;
+        const bool over = (t + 1) * S::BK > A.K;
+        int8_t *const la = lds + slot * S::STAGE, *const lw = la + S::PART_A;
+#pragma unroll
+        for (int i = 0; i < S::LW; ++i)
+          *(int4v *)(lw + (i * S::THREADS + threadIdx.x) * 16) = rw[p][i].codes(t * S::BK + place<S>(i).y, A.K, over);
+        // the codes of stage t: behind them its weights' loads and a stage's where two are under way
+        if (t + 1 < stages) wait_loads<(AHEAD == 2 ? S::LA + 2 * S::LW : S::LW)>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();  // all of stage t is there, and all have read stage t - 1
+        asm volatile("" ::: "memory");
+        if (t + AHEAD < stages) fetch(p, t + AHEAD, (slot + AHEAD) % S::NS);
+        multiply_stage<S>(la, lw, wm, wn, wk, lane, acc);
+        slot = slot == S::NS - 1 ? 0 : slot + 1;
+      }
+    }
+    done = A.K;
+  }
+  if constexpr (DIRECT == kBoth) {
     const int full = A.K / S::BK;
     const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)lds + wave * 1024;
     // a lane's places in a stage, from the tile's first row on (strides fit 32 bits: see matmul_as)
@@ -337,8 +393,8 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
   }
   // Rows at any alignment, or their last part: through registers, AHEAD stages'
   // loads under way (as many as there are registers for).
-  if (done < A.K) {
-    constexpr int AHEAD = DIRECT || S::MT * S::NT > 8 ? 1 : 2;
+  if (DIRECT != kCodes && done < A.K) {
+    constexpr int AHEAD = DIRECT == kBoth || S::MT * S::NT > 8 ? 1 : 2;
     Piece ra[AHEAD][S::LA], rw[AHEAD][S::LW];
     const int8_t *pa[S::LA], *pw[S::LW];
 #pragma unroll
@@ -530,10 +586,11 @@ hipError_t matmul_as(const MatmulArgs &A, hipStream_t s) {
   const int tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
   const int64_t total = (int64_t)tm * tn, grid = (total + 7) / 8 * 8;
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const bool direct = (((uintptr_t)A.a | (uintptr_t)A.w | (uintptr_t)A.a_stride | (uintptr_t)A.w_stride) & 15) == 0 &&
-                      std::max(A.a_stride, A.w_stride) <= (1 << 23);
-  if (direct) k_matmul<S, true><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
-  else k_matmul<S, false><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
+  const auto whole = [](const int8_t *p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)stride) & 15) == 0 && stride <= 1 << 23; };
+  const bool a = whole(A.a, A.a_stride), w = whole(A.w, A.w_stride);
+  if (a && w) k_matmul<S, kBoth><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else if (a && (A.a_padded || A.K % 16 == 0)) k_matmul<S, kCodes><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else k_matmul<S, kNone><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
   return hipGetLastError();
 }
 

@@ -30,6 +30,7 @@ struct MatmulArgs {
   void *out;
   int64_t a_stride, w_stride, out_stride;
   int32_t M, N, K, out_type;
+  int32_t a_padded;  // rows of a may be read (not their values used) to the next multiple of 16
 };
 size_t matmul_workspace(int32_t M, int32_t N, int32_t K);
 hipError_t launch_scaled_matmul(const MatmulArgs &A, void *ws, hipStream_t s);

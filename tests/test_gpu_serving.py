@@ -762,3 +762,22 @@ def test_linear_of_few_rows_that_are_no_numbers(env):
         _, _, w, sw, _ = products(1, 50, 256, 5)
         y = fs.linear(ctx, x.to("cuda:0"), w.to("cuda:0"), sw.to("cuda:0")).cpu()
         assert (y[0] == 0).all() and not torch.isfinite(y[1:3]).any() and torch.isfinite(y[3:]).all()
+
+
+@pytest.mark.parametrize("K", [1, 15, 16, 17, 129, 511, 513, 1030, 1999])
+@pytest.mark.parametrize("M,N", [(5, 41), (20, 1001), (40, 3001), (70, 2003), (130, 1999), (300, 2500), (1000, 1001), (2500, 3001)])
+def test_linear_with_weights_at_any_alignment(env, M, N, K):
+    fs, ctx = env
+    note(f"linear, weights at any alignment, {M}x{N}x{K}")
+    x = (torch.randn(M, K, generator=gen(M + K)) * 2).bfloat16().to("cuda:0")
+    g = torch.Generator(device="cuda:0").manual_seed(N)
+    # a part of wider rows, from an odd place on
+    w = torch.randint(-127, 128, (N, K + 2), generator=g, dtype=torch.int8, device="cuda:0")[:, 1:K + 1]
+    sw, bias = torch.rand(N, generator=g, device="cuda:0") * 1e-3, torch.randn(N, generator=g, device="cuda:0")
+    # codes beside the rows' own must not count
+    ws = torch.randint(-128, 128, (1 << 23,), generator=g, dtype=torch.int8, device="cuda:0").view(torch.uint8)
+    codes, scale = fs.quantize_rows(ctx, x)
+    one = fs.linear(ctx, x, w, sw, bias, out_dtype=torch.float32, workspace=ws)
+    total = torch.round(codes.double() @ w.double().t().contiguous())  # exact: below 2^53
+    want = total.float() * scale[:, None] * sw[None] + bias
+    assert torch.equal(one, want)
