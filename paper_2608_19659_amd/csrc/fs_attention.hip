@@ -82,10 +82,15 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &A, int s) {
 }
 
 // What a kernel takes: sequences of lo .. hi - 1 rows, in runs of at least
-// `least` units.
+// `least` units.  An item's units are rounded up to a multiple of round + 1 (a
+// power of two): where that is the length of a run, no block has the end of an
+// item and the start of the next.
 struct Share {
-  int least, lo, hi;
+  int least, lo, hi, round;
 };
+
+// Units of an item of a sequence.
+__device__ __forceinline__ uint32_t item_units(const Seq &q, const Share &w) { return (uint32_t)(q.units + w.round) & ~(uint32_t)w.round; }
 
 __device__ __forceinline__ int row_tiles(const Seq &q, int group, int R, const Share &w) {
   const int64_t rows = (int64_t)q.n * group;
@@ -104,7 +109,7 @@ __device__ uint32_t list_units(const AttendArgs &A, int group, const Share &shar
     uint32_t v = 0;
     if (s < A.n_seqs) {
       const Seq q = sequence(A, s);
-      v = (uint32_t)(A.c.n_heads * row_tiles(q, group, R, share)) * q.units;
+      v = (uint32_t)(A.c.n_heads * row_tiles(q, group, R, share)) * item_units(q, share);
     }
     uint32_t sum = v;
     for (int o = 1; o < 64; o <<= 1) {
@@ -148,7 +153,7 @@ __device__ __forceinline__ Item item_at(const AttendArgs &A, int group, const Sh
   Item it;
   it.s = lo;
   it.q = sequence(A, lo);
-  it.units = it.q.units;
+  it.units = item_units(it.q, share);
   const uint32_t rel = unit - pre[lo], at = rel / it.units;
   it.start = pre[lo] + at * it.units;
   const uint32_t tiles = row_tiles(it.q, group, R, share), k = at % tiles;
@@ -1035,14 +1040,15 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   Parts P{(unsigned long long *)ws, (float *)((unsigned long long *)ws + kRowBlocks), 0};
   hipError_t e;
   if (chunks) {  // a sequence alone has no other kernel, whatever it turns out to be
-    const Share many{8, A.n_seqs == 1 ? 1 : kChunkLeast, everything};
+    const Share many{8, A.n_seqs == 1 ? 1 : kChunkLeast, everything, 0};
     P.call = next_call();
     e = allow_lds(&k_attend_chunk<TYPE, D, ONE>, lds);
     if (e != hipSuccess) return e;
     k_attend_chunk<TYPE, D, ONE><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
     if (A.n_seqs == 1) return hipGetLastError();
   }
-  const Share few{4, 1, chunks ? kChunkLeast : everything};
+  // about what there is: a sequence has a token at least
+  const int64_t likely = ((int64_t)A.n_seqs * ((group + kRows - 1) / kRows) + std::max(0, A.n_tokens - A.n_seqs) * group / kRows) * A.c.n_heads;
   // Two blocks a CU of four wavefronts, or where there are fewer items than CUs
   // one of eight, which have half the tiles each before the parts are joined.
   // (us a call, four and eight: 4 users of 1000 tokens and 8 heads 14.6 and
@@ -1051,6 +1057,17 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   // items, 27.1 and 29.1, 64 of 512 to 8192 73.5 and 94.7.)
   const auto rows = [&](auto waves_of) {
     constexpr int WAVES = decltype(waves_of)::value, BLOCKS = kRowBlocks * 4 / WAVES;
+    // Where runs of 4, 8 or 16 units are enough for every item to be cut on its
+    // own, they are (us a call, cut evenly and so: 4 users of 4000 tokens and one
+    // head 16.4 and 12.4, 8 heads 20.3 and 16.4, 64 of 4000 and one head 23.7 and
+    // 19.4; with lengths of 1000 to 16000 16 users of one head 21.1 and 25.1, 32 of
+    // up to 8000 20.2 and 18.2).  Longer runs are cut evenly, as lengths differ.
+    Share few{4, 1, chunks ? kChunkLeast : everything, 0};
+    for (int run = 4; run <= 16; run *= 2)
+      if (few.round == 0 && likely * ((tiles - kItemUnits + run - 1) / run) <= BLOCKS) {
+        few.least = run;
+        few.round = run - 1;
+      }
     // parts of an item: by the length of its context, or by its share of the blocks
     const int64_t items = std::max<int64_t>(1, (int64_t)A.n_seqs * A.c.n_heads * ((std::min<int64_t>(most_rows, kChunkLeast) + kRows - 1) / kRows));
     const bool few_parts = std::min((tiles - kItemUnits) / few.least, 2 * BLOCKS / items) < 12;
@@ -1061,8 +1078,6 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
     if (!few_parts) k_join<TYPE, D><<<BLOCKS - 1, 64 * kJoinWaves, lds, s>>>(A, few, BLOCKS, P.floats);
     return hipGetLastError();
   };
-  // about what there is: a sequence has a token at least
-  const int64_t likely = ((int64_t)A.n_seqs * ((group + kRows - 1) / kRows) + std::max(0, A.n_tokens - A.n_seqs) * group / kRows) * A.c.n_heads;
   return likely <= 224 ? rows(std::integral_constant<int, 8>{}) : rows(std::integral_constant<int, 4>{});
 }
 

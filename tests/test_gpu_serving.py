@@ -781,3 +781,10 @@ def test_linear_with_weights_at_any_alignment(env, M, N, K):
     total = torch.round(codes.double() @ w.double().t().contiguous())  # exact: below 2^53
     want = total.float() * scale[:, None] * sw[None] + bias
     assert torch.equal(one, want)
+
+
+@pytest.mark.parametrize("heads,group", [(1, 5), (3, 1), (8, 4), (1, 17)])
+@pytest.mark.parametrize("lengths", [[1000], [4000, 1, 700, 64], [2100, 0, 65, 2049, 1024, 3],
+                                     [300 + 211 * (i % 7) for i in range(24)], [(37 * i) % 1400 for i in range(60)]])
+def test_decode_attention_cut_between_items(env, lengths, heads, group):
+    attention_case(env, lengths, [1] * len(lengths), heads, group, 128 if heads < 8 else 64, 64 if group > 1 else 16, 0, "bf16")
