@@ -162,6 +162,12 @@ __device__ __forceinline__ Item item_at(const AttendArgs &A, int group, const Sh
   return it;
 }
 
+// Blocks of the row kernel: two a CU of four wavefronts or one of eight; of the
+// other: one a CU.
+constexpr int kRowBlocks = 512, kChunkBlocks = 256;
+constexpr int row_blocks(int waves) { return kRowBlocks * 4 / waves; }
+static_assert(kRowBlocks < 4096, "counts of parts have 12 bits");
+
 // A cut costs a block about as much as 16 tiles.  Items that are small beside
 // a run, or where runs are short not much longer, are not cut: a cut within
 // one moves to its nearer end.
@@ -214,8 +220,18 @@ struct Parts {
 };
 
 // Workgroups go round the eight XCDs in turn: each XCD gets neighbouring runs
-// (grids are multiples of eight), so that row tiles of one head meet in its L2.
-__device__ __forceinline__ uint32_t run_of_block() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
+// (grids are multiples of eight), so that row tiles of one head meet in its L2,
+// and the same number of them, however few there are (us a call, with the first
+// XCDs full and so: 24 users of 1000 tokens on 8 heads 15.8 and 14.1, 140 of up to
+// 1000 on two 16.9 and 15.3, 32 of up to 8000 on one 17.9 and 16.9).  A block
+// beyond the runs gets one that starts past the units.
+template <uint32_t BLOCKS>
+__device__ __forceinline__ uint32_t run_of_block(uint32_t total, uint32_t run) {
+  // at least total / run / 8, which is at most BLOCKS / 8 (the factor is for the rounding)
+  const float share = (float)total * __builtin_amdgcn_rcpf((float)run) * (0.125f * 1.00001f);
+  const uint32_t per = min(BLOCKS / 8, (uint32_t)share + 1), at = blockIdx.x >> 3;
+  return at < per ? (blockIdx.x & 7) * per + at : BLOCKS;
+}
 
 // Parts go from block to block, whose L2 may be another XCD's: they are stored
 // and read at the device's scope, two floats at a time, past the L2.  (A fence
@@ -342,7 +358,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
   const Cache &c = A.c;
   const int group = A.n_q_heads / c.n_heads;
   const uint32_t total = list_units<64 * WAVES, kRows>(A, group, share, pre), run = run_length(total, gridDim.x, share);
-  const uint32_t mine = run_of_block();
+  const uint32_t mine = run_of_block<row_blocks(WAVES)>(total, run);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = lane & 15, G = lane >> 4, kg = row >> 2;
   const int PS = ONE ? 64 : 1 << c.page_shift;
@@ -646,7 +662,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
   const Cache &c = A.c;
   const int group = A.n_q_heads / c.n_heads;
   const uint32_t total = list_units<kChunkThreads, kChunkRows>(A, group, share, pre), run = run_length(total, gridDim.x, share);
-  const uint32_t mine = run_of_block(), stop = min((mine + 1) * run, total);
+  const uint32_t mine = run_of_block<kChunkBlocks>(total, run), stop = min((mine + 1) * run, total);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int PS = ONE ? 64 : 1 << c.page_shift;
@@ -1005,11 +1021,6 @@ __global__ void k_check_attention(AttendArgs A, int32_t *flag) {
   }
 }
 
-// Blocks of the row kernel: two a CU, each with four wavefronts of two tiles
-// in flight; of the other: one a CU.
-constexpr int kRowBlocks = 512, kChunkBlocks = 256;
-static_assert(kRowBlocks < 4096, "counts of parts have 12 bits");
-
 // A number that no other call of the process has; the start differs from process
 // to process (a clock and where the program lies; nothing here may throw).
 unsigned long long next_call() {
@@ -1056,7 +1067,7 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   // 16.5, one of 1000 and one head 9.8 and 10.0; 32 of 4000 and 8 heads, 256
   // items, 27.1 and 29.1, 64 of 512 to 8192 73.5 and 94.7.)
   const auto rows = [&](auto waves_of) {
-    constexpr int WAVES = decltype(waves_of)::value, BLOCKS = kRowBlocks * 4 / WAVES;
+    constexpr int WAVES = decltype(waves_of)::value, BLOCKS = row_blocks(WAVES);
     // Where runs of 4, 8 or 16 units are enough for every item to be cut on its
     // own, they are (us a call, cut evenly and so: 4 users of 4000 tokens and one
     // head 16.4 and 12.4, 8 heads 20.3 and 16.4, 64 of 4000 and one head 23.7 and
