@@ -267,8 +267,71 @@ __device__ __forceinline__ bool last_to_arrive(const Parts &P, uint32_t b0, int 
   return last;
 }
 
-// Adds up the parts of an item, four neighbouring elements a lane.  Where
-// there are many the wavefronts share them.
+// Four neighbouring elements of row i from d on, to where they go.
+template <int TYPE, int D>
+__device__ __forceinline__ void store_joined(const AttendArgs &A, const Item &it, const Rows &of, int i, int d, float4v out, float sum) {
+  const int2 to = of(i);
+  uint16_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = bits16<TYPE>(sum == 0.0f ? 0.0f : out[j] / sum);
+  __builtin_memcpy((uint16_t *)A.out + ((int64_t)(it.q.q0 + to.x) * A.n_q_heads + it.h * (int)of.group + to.y) * D + d, w, 8);
+}
+
+// Adds up the parts of an item of many rows: four times four elements a lane and
+// two parts at a time, so that loads enough are under way.  (2048 tokens of 40
+// heads over 8192: 426 us, 438 with the loop for few rows below; two such 667 and
+// 682; 512 of 40 heads over 4096 beside 32 users 134 and 145.)
+template <int TYPE, int D, int R, int WAVES>
+__device__ void join_many(const AttendArgs &A, const Item &it, const Rows &of, int rows, uint32_t b0, int parts, const float *floats) {
+  constexpr int HELD = 4, STEP = 64 * WAVES;
+  const int pieces = rows * (D / 4);
+  for (int at = threadIdx.x; at < pieces; at += HELD * STEP) {
+    float M[HELD], sum[HELD];
+    float4v out[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      M[h] = kFloor;
+      sum[h] = 0.0f;
+      out[h] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (int p0 = 0; p0 < parts; p0 += 2) {
+      float2 ml[2][HELD], v0[2][HELD], v1[2][HELD];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int p = min(p0 + j, parts - 1);
+        const float *const f = floats + part_index(b0 + p, p == 0) * part_floats(R, D);
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+          const int e = min(at + h * STEP, pieces - 1), i = e / (D / 4), d = e % (D / 4) * 4;
+          ml[j][h] = get(f + 2 * i);
+          v0[j][h] = get(f + 2 * R + i * D + d);
+          v1[j][h] = get(f + 2 * R + i * D + d + 2);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (p0 + j >= parts) break;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+          const float m_new = fmaxf(M[h], ml[j][h].x);
+          const float keep = __builtin_amdgcn_exp2f(M[h] - m_new), add = __builtin_amdgcn_exp2f(ml[j][h].x - m_new);
+          sum[h] = sum[h] * keep + ml[j][h].y * add;
+          out[h] = out[h] * keep + float4v{v0[j][h].x, v0[j][h].y, v1[j][h].x, v1[j][h].y} * add;
+          M[h] = m_new;
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      const int e = at + h * STEP;
+      if (e < pieces) store_joined<TYPE, D>(A, it, of, e / (D / 4), e % (D / 4) * 4, out[h], sum[h]);
+    }
+  }
+  __syncthreads();
+}
+
+// The same for an item of few rows, four elements a lane.  Where there are many
+// parts the wavefronts share them.
 template <int TYPE, int D, int R, int WAVES>
 __device__ void join(const AttendArgs &A, const Item &it, const Rows &of, int rows, uint32_t b0, int parts, const float *floats) {
   __shared__ float lm[WAVES][64], ll[WAVES][64];
@@ -319,11 +382,7 @@ __device__ void join(const AttendArgs &A, const Item &it, const Rows &of, int ro
       __syncthreads();
     }
     if (at + lane < pieces && (!together || wave == 0)) {
-      const int2 to = of(i);
-      uint16_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = bits16<TYPE>(sum == 0.0f ? 0.0f : out[j] / sum);
-      __builtin_memcpy((uint16_t *)A.out + ((int64_t)(it.q.q0 + to.x) * A.n_q_heads + it.h * (int)of.group + to.y) * D + d, w, 8);
+      store_joined<TYPE, D>(A, it, of, i, d, out, sum);
     }
   }
   __syncthreads();
@@ -946,7 +1005,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
     if (!whole) {
       const uint32_t b0 = it.start / run, b1 = (it.start + it.units - 1) / run;  // the runs that have parts of it
       if (last_to_arrive(P, b0, (int)(b1 - b0 + 1)))
-        join<TYPE, D, kChunkRows, kChunkThreads / 64>(A, it, of, rows, b0, (int)(b1 - b0 + 1), P.floats);
+        join_many<TYPE, D, kChunkRows, kChunkThreads / 64>(A, it, of, rows, b0, (int)(b1 - b0 + 1), P.floats);
     }
   }
 }
@@ -1033,21 +1092,33 @@ unsigned long long next_call() {
   return n;
 }
 
+// From what the host knows, at most: the units of an item.
+int64_t most_units(const AttendArgs &A) {
+  int64_t tiles = (A.table_width << A.c.page_shift) / kTile;
+  if (A.window) tiles = std::min(tiles, ((int64_t)A.window + A.max_q) / kTile);
+  return tiles + kItemUnits;
+}
+
+// Whether sequences of many rows go to the chunk kernel.  It does about 1700
+// units of 16 rows a us, the row kernel 675, but it takes 30 us more where there
+// is little to do (2 x 2048 tokens of 40 heads over 8192: 1716 us by the row
+// kernel, 680 by this one; 389 tokens of 12 heads in a window of 1000: 25 and
+// 80).  Of the tokens one a sequence is left out: in a step of many users and
+// one prompt they are those that no chunk has.  (120 users, 79 tokens of 24 heads
+// over 3869 among them: 64.8 us, by the chunk kernel 383.)
+bool takes_chunks(const AttendArgs &A) {
+  const int64_t group = A.n_q_heads / A.c.n_heads, tiles = most_units(A) - kItemUnits;
+  const int64_t row_tiles = ((int64_t)std::max(0, A.n_tokens - A.n_seqs) * group / kRows + 1) * A.c.n_heads;
+  return A.max_q * group >= kChunkLeast && row_tiles * std::max<int64_t>(tiles, kItemUnits) >= 32768;
+}
+
 template <int TYPE, int D, bool ONE>
 hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   const size_t lds = sizeof(uint32_t) * A.n_seqs;
   const int64_t group = A.n_q_heads / A.c.n_heads, most_rows = A.max_q * group;
   const int everything = 0x7fffffff;
-  // From what the host knows, at most: row tiles of 16 rows in all, and tiles
-  // of 64 tokens that one sees.
-  const int64_t row_tiles = (A.n_tokens * group / kRows + A.n_seqs) * A.c.n_heads;
-  int64_t tiles = (A.table_width << A.c.page_shift) / kTile + kItemUnits;
-  if (A.window) tiles = std::min(tiles, ((int64_t)A.window + A.max_q) / kTile + kItemUnits);
-  // The chunk kernel does about 1700 units of 16 rows a us, the row kernel 675,
-  // but it takes 30 us more where there is little to do (2 x 2048 tokens of 40
-  // heads over 8192: 1716 us by the row kernel, 680 by this one; 389 tokens of
-  // 12 heads in a window of 1000: 25 and 80).
-  const bool chunks = most_rows >= kChunkLeast && row_tiles * tiles >= 32768;
+  const int64_t tiles = most_units(A);
+  const bool chunks = takes_chunks(A);
   Parts P{(unsigned long long *)ws, (float *)((unsigned long long *)ws + kRowBlocks), 0};
   hipError_t e;
   if (chunks) {  // a sequence alone has no other kernel, whatever it turns out to be
@@ -1101,11 +1172,9 @@ size_t attention_workspace(const Cache &c, int32_t, int64_t, int32_t) {
 }
 
 bool attention_fits(const AttendArgs &A) {
-  const int64_t group = A.n_q_heads / A.c.n_heads, most_rows = A.max_q * group;
-  const int64_t tiles = (A.table_width << A.c.page_shift) / kTile + kItemUnits, limit = 0x7fffffff;
-  const auto fits = [&](int64_t row_tiles) { return row_tiles <= limit / A.c.n_heads / tiles; };
-  const int64_t rows = (int64_t)A.n_tokens * group;
-  if (most_rows < kChunkLeast || rows / kRows + A.n_seqs <= 32768 / tiles) return fits(rows / kRows + A.n_seqs);
+  const int64_t group = A.n_q_heads / A.c.n_heads, rows = (int64_t)A.n_tokens * group;
+  const auto fits = [&](int64_t row_tiles) { return row_tiles <= 0x7fffffff / A.c.n_heads / (most_units(A) + 16); };
+  if (!takes_chunks(A)) return fits(rows / kRows + A.n_seqs);
   return fits(rows / kChunkRows + A.n_seqs) && fits((int64_t)A.n_seqs * (kChunkLeast / kRows));
 }
 

@@ -788,3 +788,14 @@ def test_linear_with_weights_at_any_alignment(env, M, N, K):
                                      [300 + 211 * (i % 7) for i in range(24)], [(37 * i) % 1400 for i in range(60)]])
 def test_decode_attention_cut_between_items(env, lengths, heads, group):
     attention_case(env, lengths, [1] * len(lengths), heads, group, 128 if heads < 8 else 64, 64 if group > 1 else 16, 0, "bf16")
+
+
+@pytest.mark.parametrize("lengths,news,heads,group", [([3900] + [40 + 61 * i for i in range(40)], [79] + [1] * 40, 8, 3),
+                                                      ([2300, 70, 0, 900], [300, 1, 1, 1], 4, 2)])
+def test_one_prompt_beside_users(env, lengths, news, heads, group):
+    attention_case(env, lengths, news, heads, group, 64, 32, 0, "f16")
+
+
+@pytest.mark.parametrize("new,length", [(1100, 9000), (1537, 4100)])
+def test_many_rows_in_many_parts(env, new, length):
+    attention_case(env, [length], [new], 1, 5, 64, 64, 0, "bf16")
