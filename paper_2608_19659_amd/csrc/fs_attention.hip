@@ -1132,10 +1132,11 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   // about what there is: a sequence has a token at least
   const int64_t likely = ((int64_t)A.n_seqs * ((group + kRows - 1) / kRows) + std::max(0, A.n_tokens - A.n_seqs) * group / kRows) * A.c.n_heads;
   // Two blocks a CU of four wavefronts, or where there are fewer items than CUs
-  // one of eight, which have half the tiles each before the parts are joined.
+  // one of eight, which have half the tiles each before the parts are joined (but
+  // not where a CU's share is a few tiles, one for each of the four).
   // (us a call, four and eight: 4 users of 1000 tokens and 8 heads 14.6 and
   // 11.8, 64 of 1000 and one head 15.3 and 12.0, 4 of 4000 and one head 19.8 and
-  // 16.5, one of 1000 and one head 9.8 and 10.0; 32 of 4000 and 8 heads, 256
+  // 16.5, one of 1000 and one head 10.3 and 10.6; 32 of 4000 and 8 heads, 256
   // items, 27.1 and 29.1, 64 of 512 to 8192 73.5 and 94.7.)
   const auto rows = [&](auto waves_of) {
     constexpr int WAVES = decltype(waves_of)::value, BLOCKS = row_blocks(WAVES);
@@ -1160,7 +1161,8 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
     if (!few_parts) k_join<TYPE, D><<<BLOCKS - 1, 64 * kJoinWaves, lds, s>>>(A, few, BLOCKS, P.floats);
     return hipGetLastError();
   };
-  return likely <= 224 ? rows(std::integral_constant<int, 8>{}) : rows(std::integral_constant<int, 4>{});
+  const bool wide = likely <= 224 && likely * ((tiles - kItemUnits + 3) / 4) > 64;
+  return wide ? rows(std::integral_constant<int, 8>{}) : rows(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
