@@ -1099,17 +1099,21 @@ int64_t most_units(const AttendArgs &A) {
   return tiles + kItemUnits;
 }
 
-// Whether sequences of many rows go to the chunk kernel.  It does about 1700
-// units of 16 rows a us, the row kernel 675, but it takes 30 us more where there
-// is little to do (2 x 2048 tokens of 40 heads over 8192: 1716 us by the row
-// kernel, 680 by this one; 389 tokens of 12 heads in a window of 1000: 25 and
-// 80).  Of the tokens one a sequence is left out: in a step of many users and
-// one prompt they are those that no chunk has.  (120 users, 79 tokens of 24 heads
-// over 3869 among them: 64.8 us, by the chunk kernel 383.)
+// Whether sequences of many rows go to the chunk kernel.  By what is measured a
+// call of e units of 16 rows takes the row kernel 8 + e / 650 us and the chunk
+// kernel about 30 us where items are short, 55 + e / 1900 where they are long, as
+// parts of 256 rows are costly to add.  (us, chunk kernel and row kernel: 310
+// tokens of 96 heads in a window of 100, e = 14880, 32.5 and 32.9; 2 x 816 in one
+// of 100, 21216, 30 and 41; 58 tokens of 20 users in one of 1000, 45696, 86 and
+// 109; 147 tokens of 23 users over up to 1277, 16180, 42 and 22; one of 1095 over
+// 1878, 32880, 100 and 73; 4 x 1704 over 1747, 93744, 53 and 100; 2 x 2048 over
+// 8192, 40 heads, 680 and 1716.)  Of the tokens one a sequence is left out: in a
+// step of many users and one prompt they are those that no chunk has (120 users,
+// 79 tokens of 24 heads over 3869 among them: 65 us, by the chunk kernel 383).
 bool takes_chunks(const AttendArgs &A) {
   const int64_t group = A.n_q_heads / A.c.n_heads, tiles = most_units(A) - kItemUnits;
   const int64_t row_tiles = ((int64_t)std::max(0, A.n_tokens - A.n_seqs) * group / kRows + 1) * A.c.n_heads;
-  return A.max_q * group >= kChunkLeast && row_tiles * std::max<int64_t>(tiles, kItemUnits) >= 32768;
+  return A.max_q * group >= kChunkLeast && row_tiles * std::max<int64_t>(tiles, kItemUnits) >= (tiles <= 16 ? 13000 : 45000);
 }
 
 template <int TYPE, int D, bool ONE>
@@ -1127,7 +1131,8 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
     e = allow_lds(&k_attend_chunk<TYPE, D, ONE>, lds);
     if (e != hipSuccess) return e;
     k_attend_chunk<TYPE, D, ONE><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
-    if (A.n_seqs == 1) return hipGetLastError();
+    // no sequence of few rows where the others, at max_q tokens each, leave it many
+    if (A.n_seqs == 1 || (A.n_tokens - (A.n_seqs - 1) * (int64_t)A.max_q) * group >= kChunkLeast) return hipGetLastError();
   }
   // about what there is: a sequence has a token at least
   const int64_t likely = ((int64_t)A.n_seqs * ((group + kRows - 1) / kRows) + std::max(0, A.n_tokens - A.n_seqs) * group / kRows) * A.c.n_heads;

@@ -799,3 +799,11 @@ def test_one_prompt_beside_users(env, lengths, news, heads, group):
 @pytest.mark.parametrize("new,length", [(1100, 9000), (1537, 4100)])
 def test_many_rows_in_many_parts(env, new, length):
     attention_case(env, [length], [new], 1, 5, 64, 64, 0, "bf16")
+
+
+@pytest.mark.parametrize("lengths,news,heads,group,window", [([300, 290, 280], [300, 290, 280], 8, 4, 0),
+                                                             ([700, 650], [600, 580], 8, 3, 100),
+                                                             ([816, 900, 1, 0], [700, 690, 1, 1], 4, 4, 60),
+                                                             ([1200, 1100], [500, 31], 4, 8, 0)])
+def test_many_rows_over_short_contexts(env, lengths, news, heads, group, window):
+    attention_case(env, lengths, news, heads, group, 64, 64, window, "bf16")
