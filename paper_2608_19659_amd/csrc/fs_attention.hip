@@ -514,7 +514,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
       bits = max(bits, __shfl_xor(bits, 32));
       const float largest = value16<TYPE>((uint16_t)bits);
       const float inverse = largest < kTiny ? 0.0f : 32512.0f / largest;
-      q_step = (largest < kTiny ? 0.0f : largest / 32512.0f) * (A.scale * kLog2e);
+      // no code stands for an infinity, whose logits may cancel: as with a NaN all are NaN
+      q_step = (largest < kTiny ? 0.0f : largest / 32512.0f + (largest - largest)) * (A.scale * kLog2e);
 #pragma unroll
       for (int st = 0; st < STEPS; ++st)
 #pragma unroll
