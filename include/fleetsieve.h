@@ -528,7 +528,8 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
  * the tokens of a page adjacent, so that a product over tokens reads whole
  * words.  head_dim is 64 or 128, page_size 16, 32 or 64 (FS_ERR_UNSUPPORTED
  * otherwise); k and v start on multiples of 16 bytes.  Scales are
- * not negative; one below 2^-110 stands for a page of zeros. */
+ * not negative; one below 2^-110 stands for a page of zeros, one that is not
+ * finite for a page of no numbers: a query that sees it gets NaN. */
 typedef struct fs_kv_cache {
   int8_t *k;       /* [n_pages][n_heads][page_size][head_dim] */
   int8_t *v;       /* [n_pages][n_heads][head_dim][page_size] */
@@ -555,7 +556,7 @@ typedef struct fs_kv_cache {
  * first new one.  The page's scale becomes s' = max(s, max |new| / 127); where
  * it grows, the codes held become rint(c * (s / s')); new codes are
  * rint(x * (1 / s')), at most 127 in magnitude (keys from their rotated
- * binary32 values).
+ * binary32 values).  A NaN or an infinity among the new makes s' NaN.
  *
  * With FS_VALIDATE=1 slots outside the cache, positions outside [0,
  * n_positions) and tokens of a page that do not follow one another are

@@ -560,7 +560,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
       const bool zero = vs < kZeroScale;
       const float lift = zero ? -60.0f : __builtin_amdgcn_logf(vs);
       const float per = zero ? 0x1p60f : 1.0f / vs;
-      const float cq = q_step * ks;
+      const float cq = __builtin_fmaf(q_step, ks, ks - ks);  // NaN under an infinite scale, whatever the sum's sign
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = __builtin_fmaf(sc[i], cq, lift);
       if (edge) {
@@ -840,7 +840,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
       }
       if (step == 7 && threadIdx.x < 4) {
         const bool none = scale_v < kZeroScale;
-        scales[buf][threadIdx.x] = float4v{scale_k, none ? -60.0f : __builtin_amdgcn_logf(scale_v),
+        // a NaN for an infinite key scale, whatever the sums' signs
+        scales[buf][threadIdx.x] = float4v{scale_k + (scale_k - scale_k), none ? -60.0f : __builtin_amdgcn_logf(scale_v),
                                            none ? 0x1p60f : __builtin_amdgcn_rcpf(scale_v), 0.0f};
       }
     };

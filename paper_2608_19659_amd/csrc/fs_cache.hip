@@ -134,7 +134,8 @@ __device__ void append_page(const AppendArgs &A, int t, int slot, int head, bool
   if (lane == 0) atomicMax(most, m);
   __syncthreads();
   const float a = __uint_as_float(*most), made = a < kTiny ? 0.0f : a / 127.0f;
-  const float now = old >= made || old != old ? old : made;  // a NaN on either side stays
+  float now = old >= made || old != old ? old : made;  // a NaN on either side stays
+  now += now - now;                                    // and an infinity, which no code can stand beside, becomes one
   const bool grew = first && !(now == old);
   const float inverse = now > 0.0f ? 1.0f / now : 0.0f, ratio = now > 0.0f ? old / now : 0.0f;
 #pragma unroll

@@ -29,3 +29,38 @@ def test_an_infinite_query_gives_no_numbers(env, D, page, length, value, dtype):
     q[0, 1, 5] = value
     got = fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32([length]), i32([0, 1]), 1).cpu()
     assert torch.isnan(got[0, 1]).all() and torch.isfinite(got[0, ::2]).all()
+
+
+@pytest.mark.parametrize("new", [3, 200])
+def test_a_scale_that_is_not_finite_reaches_rows_that_see_it(env, new):
+    """A code of zero under an infinite scale is no number, whatever the sign
+    of the sum that the others make."""
+    fs, ctx = env
+    note(f"scales that are not finite, {new} tokens")
+    for of, scale in (("k_scale", math.inf), ("k_scale", math.nan), ("v_scale", math.inf), ("v_scale", math.nan)):
+        c = wide([300], 1, 64, 16, seed=5) if new > 100 else ref.Paged([300], 1, 64, 16, seed=5)
+        page = int(c.table[0, 299 // 16])  # tokens 288 .. 299
+        c.k[page] = -50
+        c.k[page, ..., 7] = 0
+        getattr(c, of)[page] = scale
+        q = torch.rand(new, 1, 64, generator=gen(2)).to(torch.bfloat16) + 0.5
+        got = fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32([300]), i32([0, new]), new).cpu()
+        sees = torch.arange(300 - new, 300) >= 288
+        assert torch.isnan(got[sees]).all() and torch.isfinite(got[~sees]).all()
+
+
+def test_an_appended_infinity_makes_its_page_no_numbers(env):
+    fs, ctx = env
+    for value in (math.inf, -math.inf):
+        kv = fs.KVCache.empty(4, 2, 64, 16, "cuda:0")
+        k, v = torch.ones(20, 2, 64, device="cuda:0"), torch.ones(20, 2, 64, device="cuda:0")
+        k[18, 1, 3], v[2, 0, 9] = value, value
+        slots = torch.arange(20, dtype=torch.int32, device="cuda:0")
+        fs.cache_append(ctx, kv, k, v, slots)
+        rk, rv = (t.cpu() for t in fs.cache_read(ctx, kv, slots))
+        assert torch.isnan(rk[16:, 1]).all() and torch.isnan(rv[:16, 0]).all()
+        assert torch.isfinite(rk[:, 0]).all() and torch.isfinite(rk[:16]).all()
+        assert torch.isfinite(rv[:, 1]).all() and torch.isfinite(rv[16:]).all()
+        q = torch.ones(1, 2, 64, dtype=torch.float16, device="cuda:0")
+        got = fs.cache_attention(ctx, kv, q, i32([[0, 1]]), i32([20]), i32([0, 1]), 1).cpu()
+        assert torch.isnan(got).all()  # head 0 by a value, head 1 by a key
