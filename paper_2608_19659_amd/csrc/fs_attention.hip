@@ -15,7 +15,7 @@ namespace fs {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kFloor = -1e30f;  // a maximum over no tokens: finite, so differences stay numbers
+constexpr float kFloor = -3.40282347e38f;  // a maximum over no tokens: finite, so differences are no NaN, and above no logit
 constexpr int kTile = 64;         // tokens of one step of a wavefront
 
 // The larger of a lane's value and of the one 32 (or 16) lanes on.

@@ -64,3 +64,19 @@ def test_an_appended_infinity_makes_its_page_no_numbers(env):
         q = torch.ones(1, 2, 64, dtype=torch.float16, device="cuda:0")
         got = fs.cache_attention(ctx, kv, q, i32([[0, 1]]), i32([20]), i32([0, 1]), 1).cpu()
         assert torch.isnan(got).all()  # head 0 by a value, head 1 by a key
+
+
+@pytest.mark.parametrize("new,length", [(1, 1), (1, 150), (3, 4000), (200, 300)])
+def test_logits_far_below_zero(env, new, length):
+    """Logits of about -1.6e34, the same for all tokens: the mean of the values that a row sees."""
+    fs, ctx = env
+    note(f"logits far below zero, {new} of {length}")
+    c = wide([length], 1, 64, 64, seed=9) if new > 100 else ref.Paged([length], 1, 64, 64, seed=9)
+    c.k[:] = 100
+    c.k_scale[:] = 0.02
+    q = torch.full((new, 2, 64), -1e33, dtype=torch.bfloat16)
+    got = fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32([length]), i32([0, new]), new).cpu()
+    _, v = c.values(0)
+    for j in range(new):
+        seen = v[:length - new + 1 + j, 0]
+        assert ((got[j].double() - seen.mean(dim=0)).abs() <= 2.0 ** -8 * seen.mean(dim=0).abs() + 2.0 ** -10 * seen.abs().amax()).all()
