@@ -556,13 +556,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
       if (more) fetch_k(tile + WAVES);
       const bool edge = base < all_low || base + kTile - 1 > all_top;  // some row does not see all of it
       int least = first_seen - base - G * 16, most = last_seen - base - G * 16;
-      if (edge && (most < 0 || least > 15)) ks = vs = 1.0f;  // no page of this row's
+      if (edge && (most < 0 || least > 15)) {  // no page of this row's
+        ks = 1.0f;
+        vs = 0.0f;
+      }
       const bool zero = vs < kZeroScale;
       const float lift = zero ? -60.0f : __builtin_amdgcn_logf(vs);
       const float per = zero ? 0x1p60f : 1.0f / vs;
       const float cq = __builtin_fmaf(q_step, ks, ks - ks);  // NaN under an infinite scale, whatever the sum's sign
+      // Logits may reach 2^29 cq.  From 2^20 on a value scale would be lost in them:
+      // it is added to their differences from the largest.
+      const bool wild = __any(fabsf(cq) > 0x1p-9f);
+      const float with = wild ? 0.0f : lift;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = __builtin_fmaf(sc[i], cq, lift);
+      for (int i = 0; i < 16; ++i) sc[i] = __builtin_fmaf(sc[i], cq, with);
       if (edge) {
         asm volatile("" : "+v"(least), "+v"(most));  // keeps the comparisons in here
 #pragma unroll
@@ -573,7 +580,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
       for (int i = 0; i < 16; ++i) top_s = fmaxf(top_s, sc[i]);
       top_s = max_over_32(max_over_16(top_s));
       const float m_new = fmaxf(m, top_s);
-      const float keep = __builtin_amdgcn_exp2f(m - m_new), add = __builtin_amdgcn_exp2f(top_s - m_new);
+      float below = top_s - m_new;
+      if (wild) {
+        const float most_lift = max_over_32(max_over_16(lift));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = (sc[i] - top_s) + (lift - most_lift);
+        top_s = 0.0f;
+        below += most_lift;
+      }
+      const float keep = __builtin_amdgcn_exp2f(m - m_new), add = __builtin_amdgcn_exp2f(below);
       m = m_new;
       // probabilities against the tile's largest: 15-bit codes, in the low
       // bits of a sum with 2^23 + 128 (the 128 makes the low byte signed)
@@ -916,15 +931,14 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
           asm volatile("" : "+v"(least), "+v"(most));  // keeps the comparisons in here
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            if (g * 16 - half * 8 > most || g * 16 + 15 - half * 8 < least) per[g] = 0.0f;  // no page of this row's
+            if (g * 16 - half * 8 > most || g * 16 + 15 - half * 8 < least) add[g] = per[g] = 0.0f;  // no page of this row's
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int at_i = (g & 1) * 8 + i, place = g * 16 + i;
-              const float v = __builtin_fmaf(sc[g >> 1][at_i], slope[g], add[g]);
+              const float v = sc[g >> 1][at_i] * slope[g];
               sc[g >> 1][at_i] = place >= least && place <= most ? v : -INFINITY;
             }
             slope[g] = 1.0f;
-            add[g] = 0.0f;
           }
         }
         float top_s = kFloor;
@@ -937,17 +951,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
           top_s = fmaxf(top_s, __builtin_fmaf(most, slope[g], add[g]));
         }
         top_s = max_over_32(top_s);
-        if (__any(fabsf(top_s) > 0x1p20f)) {  // logits so large that one rounding less would tell: as they are
+        // Logits so large that a rounding less would tell and a value scale would be
+        // lost in them: as they are, the scale added to their differences from the largest.
+        const bool wild = __any(fabsf(top_s) > 0x1p20f && top_s > kFloor);
+        if (wild) {
+          top_s = kFloor;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int at_i = (g & 1) * 8 + i;
-              sc[g >> 1][at_i] = __builtin_fmaf(sc[g >> 1][at_i], slope[g], add[g]);
+              sc[g >> 1][at_i] *= slope[g];
+              top_s = fmaxf(top_s, sc[g >> 1][at_i] + add[g]);
             }
             slope[g] = 1.0f;
-            add[g] = 0.0f;
           }
+          top_s = max_over_32(top_s);
         }
         if (__any(top_s > m + kLag)) {
           const float m_new = fmaxf(m, top_s), keep = __builtin_amdgcn_exp2f(m - m_new);
@@ -958,9 +977,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[dt][i] *= keep;
         }
+        float less = m - kLift;
+        if (wild) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int at_i = (g & 1) * 8 + i;
+              sc[g >> 1][at_i] = (sc[g >> 1][at_i] - m) + add[g];
+            }
+            add[g] = kLift;
+          }
+          less = 0.0f;
+        }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const float plus = add[g] - (m - kLift);
+          const float plus = add[g] - less;
           float sum = 0.0f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
