@@ -579,9 +579,12 @@ fs_status fs_cache_read(fs_context *ctx, const fs_kv_cache *cache, int64_t n_tok
 
 /* Causal attention of n_seqs sequences' new tokens over the cache.
  *
- * The new tokens of sequence s are rows cu_q[s] .. cu_q[s+1] of q
- * [n_tokens][n_q_heads][head_dim] (token stride q_stride, FS_F16 or FS_BF16);
- * they are the last ones of the ctx_lens[s] tokens that the cache holds for
+ * The new tokens of sequence s are rows cu_q[s] .. cu_q[s+1] - 1 of q
+ * [n_tokens][n_q_heads][head_dim] (token stride q_stride, FS_F16 or FS_BF16),
+ * at most max_q of them; cu_q starts at 0, does not fall, and may end below
+ * n_tokens: rows from cu_q[n_seqs] on belong to no sequence, and `out` is not
+ * written there.  A sequence's new tokens
+ * are the last ones of the ctx_lens[s] tokens that the cache holds for
  * it, in pages block_table[s][0 ..] (row length table_width).  n_q_heads is a
  * multiple of the cache's n_heads, query head i reads cache head
  * i / (n_q_heads / n_heads).  The query at position p sees tokens
@@ -597,7 +600,9 @@ fs_status fs_cache_read(fs_context *ctx, const fs_kv_cache *cache, int64_t n_tok
  * sums are exact or binary32.  Results are equal run to run.
  *
  * With FS_VALIDATE=1 lengths and pages outside their ranges are refused (the
- * call waits for the stream); otherwise they are clamped. */
+ * call waits for the stream); otherwise they are clamped (of a sequence with
+ * more than max_q new tokens the first max_q rows count as all of them, and
+ * the rest of its rows are not written). */
 fs_status fs_cache_attention_workspace_size(const fs_kv_cache *cache, int32_t n_q_heads, int64_t n_tokens,
                                             int32_t n_seqs, size_t *bytes);
 fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const void *d_q, int64_t q_stride,

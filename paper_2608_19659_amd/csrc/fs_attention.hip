@@ -1101,7 +1101,7 @@ __global__ void k_check_attention(AttendArgs A, int32_t *flag) {
   const int s = blockIdx.x;
   const int q0 = A.cu_q[s], q1 = A.cu_q[s + 1], length = A.ctx_lens[s];
   if (threadIdx.x == 0) {
-    if (q0 < 0 || q1 < q0 || q1 > A.n_tokens || (s == 0 && q0 != 0) || (s == A.n_seqs - 1 && q1 != A.n_tokens) ||
+    if (q0 < 0 || q1 < q0 || q1 > A.n_tokens || (s == 0 && q0 != 0) ||
         q1 - q0 > A.max_q || length < 0 || length > (A.table_width << A.c.page_shift))
       atomicAdd(&flag[0], 1);
   }
@@ -1159,14 +1159,17 @@ hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
   const bool chunks = takes_chunks(A);
   Parts P{(unsigned long long *)ws, (float *)((unsigned long long *)ws + kRowBlocks), 0};
   hipError_t e;
-  if (chunks) {  // a sequence alone has no other kernel, whatever it turns out to be
-    const Share many{8, A.n_seqs == 1 ? 1 : kChunkLeast, everything, 0};
+  if (chunks) {
+    // Alone where no sequence has few rows if the others have max_q tokens each and
+    // all rows are someone's.  It takes any that has few all the same: lengths are
+    // the device's, and a buffer may hold more rows than the sequences.
+    const bool alone = A.n_seqs == 1 || (A.n_tokens - (A.n_seqs - 1) * (int64_t)A.max_q) * group >= kChunkLeast;
+    const Share many{8, alone ? 1 : kChunkLeast, everything, 0};
     P.call = next_call();
     e = allow_lds(&k_attend_chunk<TYPE, D, ONE>, lds);
     if (e != hipSuccess) return e;
     k_attend_chunk<TYPE, D, ONE><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
-    // no sequence of few rows where the others, at max_q tokens each, leave it many
-    if (A.n_seqs == 1 || (A.n_tokens - (A.n_seqs - 1) * (int64_t)A.max_q) * group >= kChunkLeast) return hipGetLastError();
+    if (alone) return hipGetLastError();
   }
   // about what there is: a sequence has a token at least
   const int64_t likely = ((int64_t)A.n_seqs * ((group + kRows - 1) / kRows) + std::max(0, A.n_tokens - A.n_seqs) * group / kRows) * A.c.n_heads;

@@ -80,3 +80,32 @@ def test_logits_far_below_zero(env, new, length):
     for j in range(new):
         seen = v[:length - new + 1 + j, 0]
         assert ((got[j].double() - seen.mean(dim=0)).abs() <= 2.0 ** -8 * seen.mean(dim=0).abs() + 2.0 ** -10 * seen.abs().amax()).all()
+
+
+@pytest.mark.parametrize("group,news,length,room", [(5, [300, 10], 4000, 600), (5, [300, 1, 0], 4000, 900), (2, [9, 3], 100, 40)])
+def test_a_buffer_of_more_rows_than_the_sequences_have(env, group, news, length, room, monkeypatch):
+    """All rows of the sequences are computed, and the rows behind them are left as they are."""
+    fs, ctx = env
+    note(f"padded rows {news} in {room}")
+    heads, D, S = 8, 64, len(news)
+    c = ref.Paged([length - 7 * s for s in range(S)], heads, D, 64, seed=room)
+    starts = [sum(news[:s]) for s in range(S + 1)]
+    q = torch.randn(room, heads * group, D, generator=gen(room)).to(torch.bfloat16)
+    out = torch.full((room, heads * group, D), 7.0, dtype=torch.bfloat16, device="cuda:0")
+    fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32(c.lengths), i32(starts), max(news), out=out)
+    got = out.cpu()
+    monkeypatch.setenv("FS_VALIDATE", "1")  # such a buffer is no error
+    fs.cache_attention(ctx, c.device(fs), q.to("cuda:0"), c.table.to("cuda:0"), i32(c.lengths), i32(starts), max(news), out=out)
+    assert torch.equal(bits(out), bits(got))
+    for s, n in enumerate(news):
+        if n == 0:
+            continue
+        k, v = c.values(s)
+        # of a long prompt the first and last tokens
+        for rows in ([range(n)] if n < 20 else [range(4), range(n - 4, n)]):
+            part = q[starts[s] + rows[0]:starts[s] + rows[-1] + 1]
+            first = c.lengths[s] - n + rows[0]
+            want = ref.attend(part, k, v, first, D ** -0.5)
+            bound = ref.attention_bound(part, k, v, first, D ** -0.5, 0, want, STEP["bf16"])
+            assert ((got[starts[s] + rows[0]:starts[s] + rows[-1] + 1].double() - want).abs() <= bound).all()
+    assert (got[starts[-1]:] == 7.0).all()
