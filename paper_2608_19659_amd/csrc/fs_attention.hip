@@ -193,11 +193,17 @@ __device__ __forceinline__ bool take(const Item &it, uint32_t run, uint32_t stop
   return true;
 }
 
+// The first token that a query at position p sees: positions may be negative and
+// windows up to 2^31 - 1, whose difference has no 32 bits.
+__device__ __forceinline__ int first_seen_from(const AttendArgs &A, int p) {
+  return A.window && p >= A.window ? p - A.window + 1 : 0;
+}
+
 // The tiles of units from .. to - 1 of an item whose rows belong to the
 // sequence's new tokens j0 .. j1 that some of them see.
 __device__ __forceinline__ int2 tiles_of(const AttendArgs &A, const Seq &q, int j0, int j1, bool whole, int from, int to) {
   const int first = q.length - q.n, end = min(q.length, first + j1 + 1);
-  const int low = A.window ? max(0, first + j0 - A.window + 1) : 0;
+  const int low = first_seen_from(A, first + j0);
   if (end <= low) return {0, 0};
   const int a = low / kTile, b = (end + kTile - 1) / kTile;
   if (whole) return {a, b};
@@ -438,9 +444,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_rows(AttendArgs A, Sha
     const int token = row < rows ? mine_of.x : 0, q_head = h * group + mine_of.y;
     // what this row sees, what some row sees, what all do
     const int last_seen = row < rows ? first + token : -1;
-    const int first_seen = A.window ? max(0, last_seen - A.window + 1) : 0;
+    const int first_seen = first_seen_from(A, last_seen);
     const int all_top = first + of.token, top = first + j1;
-    const int low = A.window ? max(0, all_top - A.window + 1) : 0, all_low = A.window ? top - A.window + 1 : 0;
+    const int low = first_seen_from(A, all_top), all_low = first_seen_from(A, top);
     const int page_top = max(top, 0) >> c.page_shift, page_low = min(low, max(top, 0)) >> c.page_shift;
     const int32_t *const table = A.table + s * A.table_width;
 
@@ -765,18 +771,18 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
     const bool live = wave * 32 + col < rows;
     const int token = live ? mine_of.x : 0, q_head = h * group + (live ? mine_of.y : 0);
     const int last_seen = live ? first + token : -1;
-    const int first_seen = A.window && live ? max(0, last_seen - A.window + 1) : 0;
+    const int first_seen = first_seen_from(A, last_seen);
     // tiles that some row of this wavefront sees
     const int wave_rows = min(32, rows - wave * 32);
     const int wave_first = of(wave * 32).x, wave_last = of(wave * 32 + max(wave_rows, 1) - 1).x;
     const int wave_top = wave_rows > 0 ? first + wave_last : -1;
-    const int wave_low = A.window && wave_rows > 0 ? max(0, first + wave_first - A.window + 1) : 0;
+    const int wave_low = wave_rows > 0 ? first_seen_from(A, first + wave_first) : 0;
     // tokens that all of its rows see
     const int all_top = wave_rows > 0 ? first + wave_first : -1;
-    const int all_low = A.window && wave_rows > 0 ? wave_top - A.window + 1 : 0;
+    const int all_low = first_seen_from(A, wave_top);
     // pages that some row of the block sees
     const int top = first + j1;
-    const int low = A.window ? max(0, first + of.token - A.window + 1) : 0;
+    const int low = first_seen_from(A, first + of.token);
     const int page_top = max(top, 0) >> c.page_shift, page_low = min(low, max(top, 0)) >> c.page_shift;
     const int32_t *const table = A.table + s * A.table_width;
     const auto entry = [&](int tok) { return table[min(max(tok >> c.page_shift, page_low), page_top)]; };

@@ -109,3 +109,10 @@ def test_a_buffer_of_more_rows_than_the_sequences_have(env, group, news, length,
             bound = ref.attention_bound(part, k, v, first, D ** -0.5, 0, want, STEP["bf16"])
             assert ((got[starts[s] + rows[0]:starts[s] + rows[-1] + 1].double() - want).abs() <= bound).all()
     assert (got[starts[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 3, 2 ** 30])
+def test_windows_near_the_largest_number(env, window):
+    """Also where the cache has fewer tokens than are new, so that positions are negative."""
+    attention_case(env, [5, 40, 0], [10, 3, 4], 1, 2, 64, 16, window, "bf16")
+    attention_case(env, [60], [200], 1, 2, 64, 64, window, "f16", cache=wide([60], 1, 64, 64, seed=3))
