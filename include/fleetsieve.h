@@ -551,7 +551,8 @@ typedef struct fs_kv_cache {
  *
  * Token t enters slot d_slots[t]; a negative slot leaves the cache as it is
  * (its query is rotated all the same).  Tokens of one page must be adjacent
- * in the batch, in slots that follow one another.  A page whose first new
+ * in the batch, in slots that follow one another; of a page for which that is
+ * not so neither scale nor codes are determined.  A page whose first new
  * token is its slot 0 starts empty; otherwise it holds its slots below the
  * first new one.  The page's scale becomes s' = max(s, max |new| / 127); where
  * it grows, the codes held become rint(c * (s / s')); new codes are

@@ -7,7 +7,7 @@
 namespace fs {
 namespace {
 
-__device__ int32_t g_flag[4];  // FS_VALIDATE=1: what the checks counted
+__device__ int32_t g_flag[2];  // FS_VALIDATE=1: what the checks counted
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs A) {
 }
 
 __global__ void k_clear(int32_t *flag) {
-  if (threadIdx.x < 4) flag[threadIdx.x] = 0;
+  if (threadIdx.x < 2) flag[threadIdx.x] = 0;
 }
 
 __global__ void k_check_slots(Cache c, const int32_t *slots, const int32_t *positions, int32_t n_positions, int32_t n,
@@ -325,10 +325,6 @@ __global__ void k_check_slots(Cache c, const int32_t *slots, const int32_t *posi
   const int slot = slots[t];
   if (slot >= n_slots(c) || (slot < 0 && !appending)) atomicAdd(&flag[0], 1);
   if (positions && (positions[t] < 0 || positions[t] >= n_positions)) atomicAdd(&flag[1], 1);
-  if (appending && t > 0 && slot >= 0 && slots[t - 1] >= 0) {
-    const int before = slots[t - 1];
-    if ((before >> c.page_shift) == (slot >> c.page_shift) && before != slot - 1) atomicAdd(&flag[2], 1);
-  }
 }
 
 }  // namespace

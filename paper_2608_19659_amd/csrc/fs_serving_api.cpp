@@ -1,7 +1,9 @@
 // fs_serving_api.cpp -- C entries of the serving operators: argument checks,
 // workspace sizes and launches on the caller's stream.
+#include <algorithm>
 #include <cmath>
 #include <mutex>
+#include <vector>
 
 #include "fs_host.h"
 #include "fs_serving.h"
@@ -64,19 +66,44 @@ fs::Cache to_cache(const fs_kv_cache *c) {
 std::mutex g_checking;  // the counters are the device's
 
 template <class Launch>
-fs_status checked(Launch launch, hipStream_t stream, const char *what, const char *const (&texts)[3]) {
+fs_status checked(Launch launch, hipStream_t stream, const char *what, const char *const (&texts)[2]) {
   std::lock_guard<std::mutex> lock(g_checking);
-  int32_t *flag = nullptr, counted[4] = {0, 0, 0, 0};
+  int32_t *flag = nullptr, counted[2] = {0, 0};
   hipError_t e = fs::flag_address(&flag);
   if (e == hipSuccess) e = fs::launch_clear_flag(flag, stream);
   if (e == hipSuccess) e = launch(flag);
   if (e == hipSuccess) e = hipMemcpyAsync(counted, flag, sizeof(counted), hipMemcpyDeviceToHost, stream);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);
   if (e != hipSuccess) return hip_fail(e, what);
-  for (int i = 0; i < 3; ++i)
+  for (int i = 0; i < 2; ++i)
     if (counted[i])
       return fail(FS_ERR_INVALID_ARGUMENT, std::string(what) + ": " + std::to_string(counted[i]) + " " + texts[i]);
   return FS_OK;
+}
+
+// FS_VALIDATE=1: a page may have one run of tokens.  A block enters a page for
+// each token that does not follow the one before it, so two of them in one page
+// would write its scale and codes at the same time.
+fs_status check_pages(const fs::Cache &c, const int32_t *d_slots, int64_t n_tokens, hipStream_t stream, const char *what) {
+  try {
+    std::vector<int32_t> slots((size_t)n_tokens), pages;
+    hipError_t e = hipMemcpyAsync(slots.data(), d_slots, slots.size() * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(stream);
+    if (e != hipSuccess) return hip_fail(e, what);
+    const int32_t in_page = (1 << c.page_shift) - 1;
+    for (size_t t = 0; t < slots.size(); ++t)
+      if (slots[t] >= 0 && (!(slots[t] & in_page) || t == 0 || slots[t - 1] != slots[t] - 1))
+        pages.push_back(slots[t] >> c.page_shift);
+    const size_t runs = pages.size();
+    std::sort(pages.begin(), pages.end());
+    pages.erase(std::unique(pages.begin(), pages.end()), pages.end());
+    if (runs != pages.size())
+      return fail(FS_ERR_INVALID_ARGUMENT, std::string(what) + ": " + std::to_string(runs - pages.size()) +
+                                               " tokens that do not follow in their page");
+    return FS_OK;
+  } catch (const std::bad_alloc &) {
+    return fail(FS_ERR_INTERNAL, std::string(what) + ": no host memory for the check");
+  }
 }
 
 fs_status matmul(const fs::MatmulArgs &A, void *ws, hipStream_t stream) {
@@ -212,8 +239,8 @@ fs_status fs_cache_append(fs_context *ctx, const fs_kv_cache *cache, const void 
           return fs::launch_check_slots(c, d_slots, rotary_dim ? d_positions : nullptr, n_positions, (int32_t)n_tokens,
                                         1, flag, stream);
         },
-        stream, "fs_cache_append",
-        {"slots outside the cache", "positions outside the tables", "tokens that do not follow in their page"});
+        stream, "fs_cache_append", {"slots outside the cache", "positions outside the tables"});
+    if (st == FS_OK) st = check_pages(c, d_slots, n_tokens, stream, "fs_cache_append");
     if (st != FS_OK) return st;
   }
   const hipError_t e = fs::launch_cache_append(
@@ -242,7 +269,7 @@ fs_status fs_cache_read(fs_context *ctx, const fs_kv_cache *cache, int64_t n_tok
         [&](int32_t *flag) {
           return fs::launch_check_slots(c, d_slots, nullptr, 0, (int32_t)n_tokens, 0, flag, stream);
         },
-        stream, "fs_cache_read", {"slots outside the cache", "", ""});
+        stream, "fs_cache_read", {"slots outside the cache", ""});
     if (st != FS_OK) return st;
   }
   const hipError_t e =
@@ -308,7 +335,7 @@ fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const vo
     return fail(FS_ERR_UNSUPPORTED, "more than 2^31 tiles of rows and tokens: split the call");
   if (fs::env_validate()) {
     st = checked([&](int32_t *flag) { return fs::launch_check_attention(A, flag, stream); }, stream,
-                 "fs_cache_attention", {"sequences with lengths out of range", "pages outside the cache", ""});
+                 "fs_cache_attention", {"sequences with lengths out of range", "pages outside the cache"});
     if (st != FS_OK) return st;
   }
   const hipError_t e = fs::launch_cache_attention(A, d_workspace, stream);

@@ -116,3 +116,20 @@ def test_windows_near_the_largest_number(env, window):
     """Also where the cache has fewer tokens than are new, so that positions are negative."""
     attention_case(env, [5, 40, 0], [10, 3, 4], 1, 2, 64, 16, window, "bf16")
     attention_case(env, [60], [200], 1, 2, 64, 64, window, "f16", cache=wide([60], 1, 64, 64, seed=3))
+
+
+def test_tokens_of_a_page_that_do_not_follow_one_another_are_refused(env, monkeypatch):
+    fs, ctx = env
+    note("tokens that do not follow")
+    monkeypatch.setenv("FS_VALIDATE", "1")
+    kv = fs.KVCache.empty(4, 1, 64, 64, "cuda:0")
+    x = torch.ones(6, 1, 64, device="cuda:0")
+    for slots in ([3, 70, 4], [3, -1, 4], [5, 5], [5, 4], [64, 65, 3, 130, 66], [0, 1, 64, 0], [-1, 9, 10, 12]):
+        with pytest.raises(fs.FleetSieveError) as e:
+            fs.cache_append(ctx, kv, x[:len(slots)], x[:len(slots)], i32(slots))
+        assert e.value.status == fs.FS_ERR_INVALID_ARGUMENT and "do not follow" in str(e.value), slots
+    assert not kv.k.any() and not kv.k_scale.any()
+    for slots in ([3, 4, 70], [3, -1, 70, 71], [62, 63, 64, 65], [127, 128, 5, 6, -1, 200], [-1, -1]):
+        fs.cache_append(ctx, kv, x[:len(slots)], x[:len(slots)], i32(slots))
+        k, _ = fs.cache_read(ctx, kv, i32([s for s in slots if s >= 0]))
+        assert ((k - 1).abs() < 1e-6).all()
