@@ -69,7 +69,11 @@ template <class Launch>
 fs_status checked(Launch launch, hipStream_t stream, const char *what, const char *const (&texts)[2]) {
   std::lock_guard<std::mutex> lock(g_checking);
   int32_t *flag = nullptr, counted[2] = {0, 0};
-  hipError_t e = fs::flag_address(&flag);
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(stream, &capture);
+  if (e == hipSuccess && capture != hipStreamCaptureStatusNone)  // refused while nothing is enqueued
+    return fail(FS_ERR_DEVICE, std::string(what) + ": FS_VALIDATE=1 waits for the stream, which is being captured");
+  if (e == hipSuccess) e = fs::flag_address(&flag);
   if (e == hipSuccess) e = fs::launch_clear_flag(flag, stream);
   if (e == hipSuccess) e = launch(flag);
   if (e == hipSuccess) e = hipMemcpyAsync(counted, flag, sizeof(counted), hipMemcpyDeviceToHost, stream);

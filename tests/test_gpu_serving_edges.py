@@ -133,3 +133,31 @@ def test_tokens_of_a_page_that_do_not_follow_one_another_are_refused(env, monkey
         fs.cache_append(ctx, kv, x[:len(slots)], x[:len(slots)], i32(slots))
         k, _ = fs.cache_read(ctx, kv, i32([s for s in slots if s >= 0]))
         assert ((k - 1).abs() < 1e-6).all()
+
+
+def test_checks_that_wait_are_refused_under_capture(env, monkeypatch):
+    """The capture goes on, and what it recorded before and after replays."""
+    fs, ctx = env
+    note("checks under capture")
+    kv = fs.KVCache.empty(2, 1, 64, 16, "cuda:0")
+    x, slots = torch.ones(3, 1, 64, device="cuda:0"), i32([1, 2, 3])
+    q, table, lens, cu = torch.ones(1, 1, 64, device="cuda:0").half(), i32([[0]]), i32([4]), i32([0, 1])
+    side = torch.cuda.Stream()
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda:0")
+    plans = [fs.AppendPlan(ctx, kv, x, x, slots, stream=side), fs.ReadPlan(ctx, kv, slots, stream=side),
+             fs.AttentionPlan(ctx, kv, q, table, lens, cu, 1, stream=side, workspace=ws)]
+    y = torch.zeros(4, device="cuda:0")
+    torch.cuda.synchronize()
+    monkeypatch.setenv("FS_VALIDATE", "1")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        y.add_(1.0)
+        for plan in plans:
+            with pytest.raises(fs.FleetSieveError) as e:
+                plan.run()
+            assert e.value.status == fs.FS_ERR_DEVICE and "captured" in str(e.value)
+        y.add_(1.0)
+    for i in range(1, 4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (y == 2.0 * i).all()
