@@ -603,7 +603,8 @@ fs_status fs_cache_read(fs_context *ctx, const fs_kv_cache *cache, int64_t n_tok
  * With FS_VALIDATE=1 lengths and pages outside their ranges are refused (the
  * call waits for the stream); otherwise they are clamped (of a sequence with
  * more than max_q new tokens the first max_q rows count as all of them, and
- * the rest of its rows are not written). */
+ * the rest of its rows are not written; where cu_q falls, out is not
+ * determined). */
 fs_status fs_cache_attention_workspace_size(const fs_kv_cache *cache, int32_t n_q_heads, int64_t n_tokens,
                                             int32_t n_seqs, size_t *bytes);
 fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const void *d_q, int64_t q_stride,

@@ -98,7 +98,9 @@ __device__ __forceinline__ int row_tiles(const Seq &q, int group, int R, const S
 }
 
 // Prefix sums of the sequences' units (pre, in LDS) and their total; all
-// threads of the block call it.
+// threads of the block call it.  Where cu_q falls sequences overlap and may have
+// more units than launch_cache_attention allows for: sums that pass 32 bits stay
+// at their largest, and such a call does nothing.
 template <int THREADS, int R>
 __device__ uint32_t list_units(const AttendArgs &A, int group, const Share &share, uint32_t *pre) {
   __shared__ uint32_t carry[THREADS / 64];
@@ -114,19 +116,19 @@ __device__ uint32_t list_units(const AttendArgs &A, int group, const Share &shar
     uint32_t sum = v;
     for (int o = 1; o < 64; o <<= 1) {
       const uint32_t x = (uint32_t)__shfl_up((int)sum, o);
-      if (lane >= o) sum += x;
+      if (lane >= o) sum = __builtin_elementwise_add_sat(sum, x);
     }
     if (lane == 63) carry[wave] = sum;
     __syncthreads();
     uint32_t before = base;
     for (int i = 0; i < THREADS / 64; ++i) {
       if (i < wave) before += carry[i];
-      base += carry[i];
+      base = __builtin_elementwise_add_sat(base, carry[i]);
     }
     if (s < A.n_seqs) pre[s] = before + sum - v;
     __syncthreads();
   }
-  return base;
+  return base > 0x7fffffffu ? 0 : base;
 }
 
 __device__ __forceinline__ uint32_t run_length(uint32_t total, uint32_t blocks, const Share &share) {

@@ -161,3 +161,20 @@ def test_checks_that_wait_are_refused_under_capture(env, monkeypatch):
         graph.replay()
         torch.cuda.synchronize()
         assert (y == 2.0 * i).all()
+
+
+@pytest.mark.parametrize("T,max_q,width", [(16384, 16384, 2048), (25, 25, 16384)])
+def test_sequences_that_overlap_end_without_harm(env, T, max_q, width):
+    """Rows 0 .. T - 1 given to 2048 sequences: more units of work than 32 bits count."""
+    fs, ctx = env
+    note(f"overlapping sequences, {T} rows")
+    S, heads, group, D = 4096, 8, 5, 64
+    c = ref.Paged([70], heads, D, 64, seed=1)
+    kv = c.device(fs)
+    q = torch.zeros(T, heads * group, D, dtype=torch.bfloat16, device="cuda:0")
+    table = torch.zeros(S, width, dtype=torch.int32, device="cuda:0")
+    lens = torch.full((S,), width * 64, dtype=torch.int32, device="cuda:0")
+    cu = i32([0, T] * (S // 2) + [0])
+    fs.cache_attention(ctx, kv, q, table, lens, cu, max_q)
+    torch.cuda.synchronize()
+    attention_case(env, [70, 300], [3, 1], 1, 2, 64, 16, 0, "bf16")
