@@ -29,14 +29,14 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds) {
   return v;
 }
 
-// Eight neighbouring elements of a row, zeros from `cols` on; `whole`: rows
-// start on multiples of 16 bytes.
+// Eight neighbouring elements of a row from c <= cols on, zeros from `cols` on;
+// `whole`: rows start on multiples of 16 bytes.  (c + 8 may have no 32 bits.)
 template <int TYPE>
 __device__ __forceinline__ void load8_of(const void *x, int64_t row, int c, int cols, bool whole, float (&v)[8]) {
-  if (c + 8 <= cols) {
+  if (cols - c >= 8) {
     load8<TYPE>(x, row + c, whole, v);
   } else {
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? load_value<TYPE>(x, row + c + i) : 0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = i < cols - c ? load_value<TYPE>(x, row + c + i) : 0.0f;
   }
 }
 
@@ -56,12 +56,12 @@ __device__ __forceinline__ int2 codes8(const float (&v)[8], float inverse) {
 
 __device__ __forceinline__ void store_codes8(int8_t *out, int c, int cols, const float (&v)[8], float inverse) {
   const int2 word = codes8(v, inverse);
-  if (c + 8 <= cols) {
+  if (cols - c >= 8) {
     __builtin_memcpy(out + c, &word, 8);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < cols) out[c + i] = (int8_t)((i < 4 ? word.x : word.y) >> (8 * (i & 3)));
+      if (i < cols - c) out[c + i] = (int8_t)((i < 4 ? word.x : word.y) >> (8 * (i & 3)));
   }
 }
 
@@ -144,7 +144,7 @@ __device__ __forceinline__ void store_products(const MatmulArgs &A, int m, int n
     y[i] = (float)acc[i] * sa * sw[i];
     if (A.bias) y[i] += bias[i];
   }
-  if (n + 4 <= A.N) {  // one store at any alignment
+  if (A.N - n >= 4) {  // one store at any alignment
     if constexpr (TYPE == kF32) {
       __builtin_memcpy((float *)A.out + at, y, 16);
     } else {
@@ -156,7 +156,7 @@ __device__ __forceinline__ void store_products(const MatmulArgs &A, int m, int n
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (n + i < A.N) store_value<TYPE>(A.out, at + i, y[i]);
+      if (i < A.N - n) store_value<TYPE>(A.out, at + i, y[i]);
   }
 }
 

@@ -178,3 +178,25 @@ def test_sequences_that_overlap_end_without_harm(env, T, max_q, width):
     fs.cache_attention(ctx, kv, q, table, lens, cu, max_q)
     torch.cuda.synchronize()
     attention_case(env, [70, 300], [3, 1], 1, 2, 64, 16, 0, "bf16")
+
+
+def test_a_row_of_nearly_two_to_the_31_elements(env):
+    """Its last eight pass 2^31 - 1; nothing behind the row is read or written."""
+    fs, ctx = env
+    cols = 2 ** 31 - 1
+    note(f"quantize 1x{cols}")
+    x = torch.zeros(cols + 65, dtype=torch.float16, device="cuda:0")
+    for at in range(0, cols, 1 << 28):
+        n = min(1 << 28, cols - at)
+        x[at:at + n] = (torch.arange(at, at + n, dtype=torch.int64, device="cuda:0") % 201 - 100).half()
+    x[cols:] = 5000.0
+    codes = torch.full((cols + 65,), 77, dtype=torch.int8, device="cuda:0")
+    scale = torch.empty(1, device="cuda:0")
+    fs._check(fs.load_library().fs_quantize_rows(ctx.handle, x.data_ptr(), fs.F16, 1, cols, cols + 65, codes.data_ptr(), cols + 65,
+                                                 scale.data_ptr(), fs._stream(x.device, None)))
+    assert scale.item() == float(torch.tensor(100.0) / 127.0)
+    inverse = torch.tensor(127.0, device="cuda:0") / torch.tensor(100.0, device="cuda:0")
+    for at in (0, 1 << 30, cols - (1 << 20)):
+        want = torch.round(x[at:min(at + (1 << 20), cols)].float() * inverse).to(torch.int8)
+        assert torch.equal(codes[at:at + want.numel()], want)
+    assert (codes[cols:] == 77).all()
