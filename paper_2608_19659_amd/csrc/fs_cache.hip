@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A, int span) {
   // the order of tokens a few of the CUs had them all: 33 us instead of 17 for
   // 8192 tokens of 8 heads).
   const int at_run = blockIdx.x * gridDim.z + blockIdx.z;
-  if (at_run >= (A.n_tokens + span - 1) / span) return;
+  if (at_run > (A.n_tokens - 1) / span) return;
   const int t0 = at_run * span, t1 = min(t0 + span, A.n_tokens);
   const int first_q = 2 * A.c.n_heads, part = blockIdx.y, lane = threadIdx.x & 63;
   if (part < first_q) {
@@ -320,7 +320,7 @@ __global__ void k_clear(int32_t *flag) {
 
 __global__ void k_check_slots(Cache c, const int32_t *slots, const int32_t *positions, int32_t n_positions, int32_t n,
                               int appending, int32_t *flag) {
-  const int t = blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x;
   if (t >= n) return;
   const int slot = slots[t];
   if (slot >= n_slots(c) || (slot < 0 && !appending)) atomicAdd(&flag[0], 1);
@@ -338,7 +338,7 @@ hipError_t launch_clear_flag(int32_t *flag, hipStream_t s) {
 
 hipError_t launch_check_slots(const Cache &c, const int32_t *slots, const int32_t *positions, int32_t n_positions,
                               int32_t n_tokens, int appending, int32_t *flag, hipStream_t s) {
-  k_check_slots<<<(n_tokens + 255) / 256, 256, 0, s>>>(c, slots, positions, n_positions, n_tokens, appending, flag);
+  k_check_slots<<<(n_tokens - 1) / 256 + 1, 256, 0, s>>>(c, slots, positions, n_positions, n_tokens, appending, flag);
   return hipGetLastError();
 }
 
@@ -347,8 +347,8 @@ static hipError_t append_as(const AppendArgs &A, hipStream_t s) {
   // few tokens a block while that is few blocks: each may be a page of its own
   const int span = A.n_tokens <= 512 ? 1 : A.n_tokens <= 2048 ? 4 : 16;
   const int q_blocks = A.q ? std::min(16, (span * A.n_q_heads * (D / 16) + 511) / 512) : 0;
-  const int runs = (A.n_tokens + span - 1) / span;
-  const int fold = std::max((1 << A.c.page_shift) / span, 1);
+  const int runs = (A.n_tokens - 1) / span + 1;
+  const int fold = std::max({(1 << A.c.page_shift) / span, 1, (int)((runs - 1) / kMostBlocks) + 1});
   const dim3 grid((runs + fold - 1) / fold, 2 * A.c.n_heads + q_blocks, fold);
   const bool whole = starts_whole<TYPE>(A.k, A.k_stride) && starts_whole<TYPE>(A.v, A.v_stride) &&
                      (!A.q || starts_whole<TYPE>(A.q, A.q_stride));
@@ -370,10 +370,20 @@ hipError_t launch_cache_append(const AppendArgs &A, hipStream_t s) {
 
 template <int TYPE>
 static hipError_t read_of(const ReadArgs &A, hipStream_t s) {
-  const dim3 grid((A.n_tokens + 15) / 16, A.c.n_heads);
-  if (A.c.head_dim == 64) k_read<TYPE, 64><<<grid, 256, 0, s>>>(A);
-  else k_read<TYPE, 128><<<grid, 256, 0, s>>>(A);
-  return hipGetLastError();
+  const int64_t element = TYPE == kF32 ? 4 : 2, token = A.c.n_heads * (int64_t)A.c.head_dim * element;
+  for (int64_t t = 0; t < A.n_tokens; t += kMostBlocks * 16) {
+    ReadArgs part = A;
+    part.slots = A.slots + t;
+    part.n_tokens = (int32_t)std::min(kMostBlocks * 16, A.n_tokens - t);
+    if (A.k_out) part.k_out = (uint8_t *)A.k_out + t * token;
+    if (A.v_out) part.v_out = (uint8_t *)A.v_out + t * token;
+    const dim3 grid((part.n_tokens + 15) / 16, A.c.n_heads);
+    if (A.c.head_dim == 64) k_read<TYPE, 64><<<grid, 256, 0, s>>>(part);
+    else k_read<TYPE, 128><<<grid, 256, 0, s>>>(part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_cache_read(const ReadArgs &A, hipStream_t s) {

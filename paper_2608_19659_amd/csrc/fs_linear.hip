@@ -567,8 +567,18 @@ __global__ __launch_bounds__(S::THREADS) void k_linear_few(QuantizeArgs X, Matmu
 
 template <int TYPE, int THREADS, int HELD>
 hipError_t quantize_as(const QuantizeArgs &A, hipStream_t s) {
-  k_quantize_rows<TYPE, THREADS, HELD><<<A.rows, THREADS, 0, s>>>(A);
-  return hipGetLastError();
+  constexpr int64_t MOST = kMostBlocks / 2;  // blocks have up to 1024 threads
+  for (int64_t r = 0; r < A.rows; r += MOST) {
+    QuantizeArgs part = A;
+    part.x = (const uint8_t *)A.x + r * A.x_stride * (TYPE == kF32 ? 4 : 2);
+    part.codes = A.codes + r * A.code_stride;
+    part.scale = A.scale + r;
+    part.rows = (int32_t)std::min(MOST, A.rows - r);
+    k_quantize_rows<TYPE, THREADS, HELD><<<part.rows, THREADS, 0, s>>>(part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <int TYPE>
@@ -583,14 +593,13 @@ hipError_t quantize_of(const QuantizeArgs &A, hipStream_t s) {
 template <int TYPE, int BM, int BN, int WM, int WN, int BK, int WK, int NS>
 hipError_t matmul_as(const MatmulArgs &A, hipStream_t s) {
   using S = Shape<TYPE, BM, BN, WM, WN, BK, WK, NS>;
-  const int tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
-  const int64_t total = (int64_t)tm * tn, grid = (total + 7) / 8 * 8;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const int tm = (A.M - 1) / BM + 1, tn = (A.N - 1) / BN + 1;
+  const int grid = (tm * tn + 7) / 8 * 8;  // see matmul_fits
   const auto whole = [](const int8_t *p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)stride) & 15) == 0 && stride <= 1 << 23; };
   const bool a = whole(A.a, A.a_stride), w = whole(A.w, A.w_stride);
-  if (a && w) k_matmul<S, kBoth><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
-  else if (a && (A.a_padded || A.K % 16 == 0)) k_matmul<S, kCodes><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
-  else k_matmul<S, kNone><<<(int)grid, S::THREADS, 0, s>>>(A, tm, tn);
+  if (a && w) k_matmul<S, kBoth><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else if (a && (A.a_padded || A.K % 16 == 0)) k_matmul<S, kCodes><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else k_matmul<S, kNone><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
   return hipGetLastError();
 }
 
@@ -663,7 +672,7 @@ bool few_of(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_
   const int64_t bytes = A.M * ((A.K * size + load - 1) / load * load + (A.K + 511) / 512 * 512 + 64);
   if (A.N <= 256 * 16 && 6 * 8192 + bytes <= kFewBytes) *e = few_as<TYPE, 16, 8, 6>(X, A, bytes, s);
   else if (A.N <= 256 * 32 && 4 * 16384 + bytes <= kFewBytes) *e = few_as<TYPE, 32, 4, 4>(X, A, bytes, s);
-  else if (A.M == 1 && 3 * 16384 + bytes <= 80 << 10) *e = few_as<TYPE, 32, 4, 3>(X, A, bytes, s);
+  else if (A.M == 1 && 3 * 16384 + bytes <= 80 << 10 && A.N <= kMostBlocks * 32) *e = few_as<TYPE, 32, 4, 3>(X, A, bytes, s);
   else return false;
   return true;
 }
@@ -683,6 +692,11 @@ hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s) {
 }
 
 size_t matmul_workspace(int32_t, int32_t, int32_t) { return 0; }
+
+bool matmul_fits(int32_t M, int32_t N, int32_t K) {
+  const Tile &t = kTiles[best_tile(M, N, K)];
+  return ((int64_t)(M - 1) / t.bm + 1) * ((N - 1) / t.bn + 1) <= kMostBlocks;
+}
 
 hipError_t launch_scaled_matmul(const MatmulArgs &A, void *, hipStream_t s) {
   return A.out_type == kF32 ? matmul_of<kF32>(A, s) : A.out_type == kF16 ? matmul_of<kF16>(A, s) : matmul_of<kBF16>(A, s);

@@ -24,6 +24,10 @@ struct QuantizeArgs {
 };
 hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s);
 
+// A launch has fewer than 2^32 threads along its grid's first dimension: blocks
+// of up to 512 threads, in multiples of eight, are at most this many.
+constexpr int64_t kMostBlocks = (1 << 23) - 8;
+
 struct MatmulArgs {
   const int8_t *a, *w;
   const float *a_scale, *w_scale, *bias;
@@ -33,6 +37,8 @@ struct MatmulArgs {
   int32_t a_padded;  // rows of a may be read (not their values used) to the next multiple of 16
 };
 size_t matmul_workspace(int32_t M, int32_t N, int32_t K);
+// Whether the product's tiles are few enough for one launch.
+bool matmul_fits(int32_t M, int32_t N, int32_t K);
 hipError_t launch_scaled_matmul(const MatmulArgs &A, void *ws, hipStream_t s);
 
 // Both steps in one launch where there are few rows (codes and scales stay

@@ -110,6 +110,8 @@ fs_status check_pages(const fs::Cache &c, const int32_t *d_slots, int64_t n_toke
   }
 }
 
+fs_status too_many_tiles() { return fail(FS_ERR_UNSUPPORTED, "the product has more tiles than a launch: split the call"); }
+
 fs_status matmul(const fs::MatmulArgs &A, void *ws, hipStream_t stream) {
   const hipError_t e = fs::launch_scaled_matmul(A, ws, stream);
   return e == hipSuccess ? FS_OK : hip_fail(e, "matrix product launch");
@@ -161,6 +163,7 @@ fs_status fs_scaled_matmul(fs_context *ctx, const int8_t *d_a, int64_t a_stride,
   if (need && !d_workspace) return fail(FS_ERR_INVALID_ARGUMENT, "workspace is NULL");
   if (workspace_bytes < need)
     return fail(FS_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(need) + " bytes");
+  if (!fs::matmul_fits((int32_t)M, (int32_t)N, (int32_t)K)) return too_many_tiles();
   DeviceGuard dg(ctx->device);
   if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
   return matmul({d_a, d_w, d_a_scale, d_w_scale, d_bias, d_out, a_stride, w_stride, out_stride, (int32_t)M, (int32_t)N,
@@ -192,6 +195,7 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
   if (workspace_bytes < need)
     return fail(FS_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(need) + " bytes");
   if ((uintptr_t)d_workspace & 15) return fail(FS_ERR_INVALID_ARGUMENT, "the workspace must start on a multiple of 16 bytes");
+  if (!fs::matmul_fits((int32_t)M, (int32_t)N, (int32_t)K)) return too_many_tiles();
   DeviceGuard dg(ctx->device);
   if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
   int8_t *const codes = (int8_t *)d_workspace;

@@ -200,3 +200,66 @@ def test_a_row_of_nearly_two_to_the_31_elements(env):
         want = torch.round(x[at:min(at + (1 << 20), cols)].float() * inverse).to(torch.int8)
         assert torch.equal(codes[at:at + want.numel()], want)
     assert (codes[cols:] == 77).all()
+
+
+def test_more_rows_than_a_launch_has_blocks(env):
+    fs, ctx = env
+    rows, cols = 2 ** 24 + 5, 4
+    note(f"quantize {rows}x{cols}")
+    x = torch.randn(rows, cols, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(3)).half()
+    codes, scale = fs.quantize_rows(ctx, x)
+    a = x.float().abs().amax(dim=1, keepdim=True)
+    assert torch.equal(scale, a[:, 0] / torch.full_like(a[:, 0], 127.0))
+    assert torch.equal(codes, torch.round(x.float() * (torch.full_like(a, 127.0) / a)).to(torch.int8))
+
+
+def test_more_channels_than_a_launch_of_one_row_has_tiles(env):
+    fs, ctx = env
+    N, K = 2 ** 28 + 5, 16
+    note(f"linear 1x{N}x{K}")
+    g = torch.Generator("cuda:0").manual_seed(4)
+    w = torch.randint(-127, 128, (N, K), generator=g, dtype=torch.int8, device="cuda:0")
+    sw = torch.full((N,), 0.01, device="cuda:0")
+    x = torch.randn(1, K, generator=g, device="cuda:0").bfloat16()
+    y = fs.linear(ctx, x, w, sw)
+    codes, scale = fs.quantize_rows(ctx, x)
+    for at in (0, N // 2, N - 4096):
+        total = (w[at:at + 4096].double() * codes.double()).sum(dim=1)  # exact: below 2^53
+        assert torch.equal(y[0, at:at + 4096], (total.float() * scale * sw[:4096]).bfloat16())
+
+
+def test_products_of_nearly_two_to_the_31_channels(env):
+    fs, ctx = env
+    g = torch.Generator("cuda:0").manual_seed(5)
+    most = 2 ** 31 - 1
+    w = torch.empty(most, 1, dtype=torch.int8, device="cuda:0")
+    w.view(torch.uint8).random_(0, 256, generator=g)
+    sw = torch.full((most,), 0.5, device="cuda:0")
+    a, sa = torch.full((1, 1), 3, dtype=torch.int8, device="cuda:0"), torch.ones(1, device="cuda:0")
+    N = (2 ** 23 - 8) * 256
+    note(f"matmul 1x{N}x1")
+    y = fs.scaled_matmul(ctx, a, sa, w[:N], sw[:N], out_dtype=torch.float16)
+    for at in (0, N // 2 - 300, N - 5000):
+        assert torch.equal(y[0, at:at + 5000], (w[at:at + 5000, 0].float() * 1.5).half()[:min(5000, N - at)])
+    del y
+    with pytest.raises(fs.FleetSieveError) as e:
+        fs.scaled_matmul(ctx, a, sa, w, sw, out_dtype=torch.float16)
+    assert e.value.status == fs.FS_ERR_UNSUPPORTED
+
+
+def test_more_tokens_than_a_launch_reads(env):
+    fs, ctx = env
+    T = 2 ** 28 + 20
+    note(f"read of {T} tokens")
+    c = ref.Paged([640], 1, 64, 16, seed=2)
+    kv = c.device(fs)
+    kv.k_scale.fill_(0.01)
+    slots = torch.arange(T, dtype=torch.int32, device="cuda:0") % 637
+    out = torch.empty(T, 1, 64, dtype=torch.float16, device="cuda:0")
+    cache = kv._struct()
+    import ctypes
+    fs._check(fs.load_library().fs_cache_read(ctx.handle, ctypes.byref(cache), T, slots.data_ptr(), out.data_ptr(), None, fs.F16,
+                                              fs._stream(out.device, None)))
+    for at in (0, 2 ** 27 - 100, T - 4000):
+        s = slots[at:at + 4000].long()
+        assert torch.equal(out[at:at + 4000], (kv.k[s // 16, :, s % 16].float() * kv.k_scale[s // 16][:, :, None]).half())
