@@ -159,7 +159,12 @@ typedef enum fs_option {
    * patterns; 1 = stepping, then bisection; 2 = bisection only.  Every value
    * gives identical results (a test knob for the later stages, which the
    * window leaves unused on ordinary inputs). */
-  FS_OPT_THRESHOLD_SEARCH = 9
+  FS_OPT_THRESHOLD_SEARCH = 9,
+  /* fs_cache_attention: 0 (default) = the kernel of 16 rows or of 256 by the
+   * call's sizes and each sequence's rows; 1 = the kernel of 16 rows, 2 = that
+   * of 256, for all sequences.  All keep the call's bounds; their roundings
+   * differ (a test knob: what a call takes by itself may change). */
+  FS_OPT_ATTENTION_KERNEL = 10
 } fs_option;
 
 typedef enum fs_objective { FS_OBJECTIVE_MAXMIN = 0, FS_OBJECTIVE_LEXICOGRAPHIC = 1 } fs_objective;

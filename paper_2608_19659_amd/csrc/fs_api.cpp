@@ -141,7 +141,7 @@ fs_status fs_context_create(int hip_device, fs_context **out) {
     (void)hipHostFree(pinned);
     return hip_fail(e, "second stream of the stage-wise score");
   }
-  *out = new fs_context{hip_device, 0, 0, 0, 0, 0, 0, 0, 0, pinned, scratch, side, fork, join, {}};
+  *out = new fs_context{hip_device, 0, 0, 0, 0, 0, 0, 0, 0, 0, pinned, scratch, side, fork, join, {}};
   return FS_OK;
 }
 
@@ -213,6 +213,11 @@ fs_status fs_context_set_option(fs_context *ctx, fs_option option, int64_t value
   if (option == FS_OPT_THRESHOLD_SEARCH) {
     if (value < 0 || value > 2) return fail(FS_ERR_INVALID_ARGUMENT, "threshold search must be 0, 1 or 2");
     ctx->thr_search = (int)value;
+    return FS_OK;
+  }
+  if (option == FS_OPT_ATTENTION_KERNEL) {
+    if (value < 0 || value > 2) return fail(FS_ERR_INVALID_ARGUMENT, "attention kernel must be 0, 1 or 2");
+    ctx->attention = (int)value;
     return FS_OK;
   }
   if (option == FS_OPT_SETUP) {

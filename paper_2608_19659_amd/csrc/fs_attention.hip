@@ -1152,26 +1152,27 @@ int64_t most_units(const AttendArgs &A) {
 // 8192, 40 heads, 680 and 1716.)  Of the tokens one a sequence is left out: in a
 // step of many users and one prompt they are those that no chunk has (120 users,
 // 79 tokens of 24 heads over 3869 among them: 65 us, by the chunk kernel 383).
-bool takes_chunks(const AttendArgs &A) {
+bool takes_chunks(const AttendArgs &A, int kernel) {
+  if (kernel) return kernel == 2;
   const int64_t group = A.n_q_heads / A.c.n_heads, tiles = most_units(A) - kItemUnits;
   const int64_t row_tiles = ((int64_t)std::max(0, A.n_tokens - A.n_seqs) * group / kRows + 1) * A.c.n_heads;
   return A.max_q * group >= kChunkLeast && row_tiles * std::max<int64_t>(tiles, kItemUnits) >= (tiles <= 16 ? 13000 : 45000);
 }
 
 template <int TYPE, int D, bool ONE>
-hipError_t attend_as(const AttendArgs &A, void *ws, hipStream_t s) {
+hipError_t attend_as(const AttendArgs &A, int kernel, void *ws, hipStream_t s) {
   const size_t lds = sizeof(uint32_t) * A.n_seqs;
   const int64_t group = A.n_q_heads / A.c.n_heads, most_rows = A.max_q * group;
   const int everything = 0x7fffffff;
   const int64_t tiles = most_units(A);
-  const bool chunks = takes_chunks(A);
+  const bool chunks = takes_chunks(A, kernel);
   Parts P{(unsigned long long *)ws, (float *)((unsigned long long *)ws + kRowBlocks), 0};
   hipError_t e;
   if (chunks) {
     // Alone where no sequence has few rows if the others have max_q tokens each and
     // all rows are someone's.  It takes any that has few all the same: lengths are
     // the device's, and a buffer may hold more rows than the sequences.
-    const bool alone = A.n_seqs == 1 || (A.n_tokens - (A.n_seqs - 1) * (int64_t)A.max_q) * group >= kChunkLeast;
+    const bool alone = kernel == 2 || A.n_seqs == 1 || (A.n_tokens - (A.n_seqs - 1) * (int64_t)A.max_q) * group >= kChunkLeast;
     const Share many{8, alone ? 1 : kChunkLeast, everything, 0};
     P.call = next_call();
     e = allow_lds(&k_attend_chunk<TYPE, D, ONE>, lds);
@@ -1223,21 +1224,21 @@ size_t attention_workspace(const Cache &c, int32_t, int64_t, int32_t) {
          2 * sizeof(float) * std::max(kRowBlocks * part_floats(kRows, c.head_dim), kChunkBlocks * part_floats(kChunkRows, c.head_dim));
 }
 
-bool attention_fits(const AttendArgs &A) {
+bool attention_fits(const AttendArgs &A, int kernel) {
   const int64_t group = A.n_q_heads / A.c.n_heads, rows = (int64_t)A.n_tokens * group;
   const auto fits = [&](int64_t row_tiles) { return row_tiles <= 0x7fffffff / A.c.n_heads / (most_units(A) + 16); };
-  if (!takes_chunks(A)) return fits(rows / kRows + A.n_seqs);
+  if (!takes_chunks(A, kernel)) return fits(rows / kRows + A.n_seqs);
   return fits(rows / kChunkRows + A.n_seqs) && fits((int64_t)A.n_seqs * (kChunkLeast / kRows));
 }
 
 template <int TYPE>
-static hipError_t attend_of(const AttendArgs &A, void *ws, hipStream_t s) {
-  if (A.c.page_shift == 6) return A.c.head_dim == 64 ? attend_as<TYPE, 64, true>(A, ws, s) : attend_as<TYPE, 128, true>(A, ws, s);
-  return A.c.head_dim == 64 ? attend_as<TYPE, 64, false>(A, ws, s) : attend_as<TYPE, 128, false>(A, ws, s);
+static hipError_t attend_of(const AttendArgs &A, int kernel, void *ws, hipStream_t s) {
+  if (A.c.page_shift == 6) return A.c.head_dim == 64 ? attend_as<TYPE, 64, true>(A, kernel, ws, s) : attend_as<TYPE, 128, true>(A, kernel, ws, s);
+  return A.c.head_dim == 64 ? attend_as<TYPE, 64, false>(A, kernel, ws, s) : attend_as<TYPE, 128, false>(A, kernel, ws, s);
 }
 
-hipError_t launch_cache_attention(const AttendArgs &A, void *ws, hipStream_t s) {
-  return A.type == kF16 ? attend_of<kF16>(A, ws, s) : attend_of<kBF16>(A, ws, s);
+hipError_t launch_cache_attention(const AttendArgs &A, int kernel, void *ws, hipStream_t s) {
+  return A.type == kF16 ? attend_of<kF16>(A, kernel, ws, s) : attend_of<kBF16>(A, kernel, ws, s);
 }
 
 hipError_t launch_check_attention(const AttendArgs &A, int32_t *flag, hipStream_t s) {

@@ -20,6 +20,7 @@ struct fs_context {
   int loop_objective;  // profiling loop certificate: 0 max-min, 1 whole objective
   int loop_refit;      // profiling loop fit step: 0 off, 1 interval refit every round
   int thr_search;      // exclusion set-up: capacity-threshold search start (0 window, 1 stepping, 2 bisection)
+  int attention;       // cache attention: 0 by size, 1 the kernel of 16 rows, 2 that of 256
   int32_t *pinned;   // pinned host word: running trajectories read back by fs_profile_loop
   void *scratch;     // this device's address of the static scratch of fs_score_candidates_noalloc
   // a second stream (default priority) and the fork / join events of the

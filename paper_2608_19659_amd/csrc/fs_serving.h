@@ -80,10 +80,11 @@ struct AttendArgs {
   float scale;
   uint32_t per_group;  // 2^32 / query heads of a group, rounded up (of no account for 1)
 };
+// `kernel`: 0 by size, 1 the kernel of 16 rows, 2 that of 256.
 // Whether the call's units of work can be counted in 32 bits.
-bool attention_fits(const AttendArgs &A);
+bool attention_fits(const AttendArgs &A, int kernel);
 size_t attention_workspace(const Cache &c, int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs);
-hipError_t launch_cache_attention(const AttendArgs &A, void *ws, hipStream_t s);
+hipError_t launch_cache_attention(const AttendArgs &A, int kernel, void *ws, hipStream_t s);
 
 // FS_VALIDATE=1: counts what is out of range into the validation words
 // (flag_address) of the current device, which the caller cleared.

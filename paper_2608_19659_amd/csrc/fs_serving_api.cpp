@@ -339,14 +339,14 @@ fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const vo
   const fs::AttendArgs A{to_cache(cache), d_q, d_out, d_cu_q, d_ctx_lens, d_block_table, q_stride, table_width,
                          (int32_t)n_tokens, n_seqs, n_q_heads, max_q, window, (int32_t)type, scale,
                          (uint32_t)((0x100000000ull + (uint64_t)group - 1) / (uint64_t)group)};
-  if (!fs::attention_fits(A))
+  if (!fs::attention_fits(A, ctx->attention))
     return fail(FS_ERR_UNSUPPORTED, "more than 2^31 tiles of rows and tokens: split the call");
   if (fs::env_validate()) {
     st = checked([&](int32_t *flag) { return fs::launch_check_attention(A, flag, stream); }, stream,
                  "fs_cache_attention", {"sequences with lengths out of range", "pages outside the cache"});
     if (st != FS_OK) return st;
   }
-  const hipError_t e = fs::launch_cache_attention(A, d_workspace, stream);
+  const hipError_t e = fs::launch_cache_attention(A, ctx->attention, d_workspace, stream);
   return e == hipSuccess ? FS_OK : hip_fail(e, "attention launch");
 }
 

@@ -31,6 +31,7 @@ OPT_SETUP = 6
 OPT_LOOP_OBJECTIVE = 7
 OPT_LOOP_REFIT = 8
 OPT_THRESHOLD_SEARCH = 9
+OPT_ATTENTION_KERNEL = 10
 OBJECTIVE_MAXMIN, OBJECTIVE_LEXICOGRAPHIC = 0, 1
 KERNEL_AUTO, KERNEL_WAVE, KERNEL_LANE, KERNEL_EXCLUSION = 0, 1, 2, 3
 

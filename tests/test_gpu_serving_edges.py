@@ -263,3 +263,56 @@ def test_more_tokens_than_a_launch_reads(env):
     for at in (0, 2 ** 27 - 100, T - 4000):
         s = slots[at:at + 4000].long()
         assert torch.equal(out[at:at + 4000], (kv.k[s // 16, :, s % 16].float() * kv.k_scale[s // 16][:, :, None]).half())
+
+
+# ------------------------------------------------ each attention kernel by itself --
+@pytest.fixture(params=[1, 2], ids=["16rows", "256rows"])
+def one_kernel(env, request):
+    """Every sequence by the kernel of 16 rows, or by that of 256, whatever the sizes."""
+    fs, ctx = env
+    ctx.set_option(fs.OPT_ATTENTION_KERNEL, request.param)
+    yield request.param
+    ctx.set_option(fs.OPT_ATTENTION_KERNEL, 0)
+
+
+def test_kernels_that_are_none(env):
+    fs, ctx = env
+    for value in (-1, 3):
+        with pytest.raises(fs.FleetSieveError) as e:
+            ctx.set_option(fs.OPT_ATTENTION_KERNEL, value)
+        assert e.value.status == fs.FS_ERR_INVALID_ARGUMENT
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [0, 1, 40, 300])
+@pytest.mark.parametrize("D,page,heads,group", [(128, 64, 2, 5), (128, 32, 1, 3), (128, 16, 1, 8), (64, 64, 2, 2), (64, 32, 3, 4),
+                                                (64, 16, 1, 1)])
+def test_windows(env, one_kernel, D, page, heads, group, window, dtype):
+    lengths, news = [200, 33, 530, 1, 130, 0, 90, 64, 65], [200, 1, 137, 1, 16, 2, 90, 64, 63]
+    attention_case(env, lengths, news, heads, group, D, page, window, dtype, seed=window)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lengths,news,heads,group,window", [([3000, 2900], [150, 700], 1, 2, 1000), ([2600], [300], 2, 1, 0),
+                                                             ([4100], [1537], 1, 1, 700), ([260] * 12, [256] * 12, 2, 1, 100),
+                                                             ([100, 300], [250, 200], 1, 2, 70)])
+def test_windows_over_cut_contexts(env, one_kernel, D, lengths, news, heads, group, window):
+    attention_case(env, lengths, news, heads, group, D, 64 if D == 128 else 32, window, "bf16" if D == 128 else "f16")
+
+
+@pytest.mark.parametrize("D,page", [(128, 64), (128, 16), (64, 32), (64, 64)])
+def test_pages_below_the_window_may_be_anything(env, one_kernel, D, page):
+    """Entries that are no pages, and pages whose scales are no numbers."""
+    lengths, new, window = [900], 290, 100
+    c = ref.Paged(lengths, 1, D, page, seed=6)
+    good = ref.Paged(lengths, 1, D, page, seed=6)
+    first = 900 - new - window + 1  # of the tokens that are seen
+    for i in range(first // page):
+        if i % 3 == 0:
+            c.k_scale[int(c.table[0, i])] = math.nan
+            c.v_scale[int(c.table[0, i])] = math.inf
+        else:
+            c.table[0, i] = -1 if i % 3 == 1 else 1 << 30
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(c, "values", good.values)
+        attention_case(env, lengths, [new], 1, 2, D, page, window, "f16", cache=c)
