@@ -316,3 +316,59 @@ def test_pages_below_the_window_may_be_anything(env, one_kernel, D, page):
     with pytest.MonkeyPatch.context() as m:
         m.setattr(c, "values", good.values)
         attention_case(env, lengths, [new], 1, 2, D, page, window, "f16", cache=c)
+
+
+def counted_plans(fs, ctx, kernel, make_workspace):
+    """Plans whose blocks count the parts of the items that they cut: items of 24
+    and 15 tiles in runs of 4 (the kernel of 16 rows) or 8, fewer than twelve
+    parts each."""
+    c = ref.Paged([1500, 900], 1, 128, 64, seed=1)
+    kv, table, lens = c.device(fs), c.table.to("cuda:0"), i32([1500, 900])
+    for n, group in ((1, 5), (3, 4)) if kernel == 1 else ((1, 5), (300, 2)):
+        q = torch.randn(2 * n, group, 128, generator=gen(n)).to(torch.bfloat16).to("cuda:0")
+        yield c, q, fs.AttentionPlan(ctx, kv, q, table, lens, i32([0, n, 2 * n]), n, workspace=make_workspace())
+
+
+def test_counts_of_parts_in_workspaces_of_any_contents(env, one_kernel):
+    """Words that look like counts, with any number of arrivals in their low 12
+    bits: results are the same, and what was counted is left at zero."""
+    fs, ctx = env
+    note(f"counts of parts, kernel {one_kernel}")
+    g = torch.Generator().manual_seed(7)
+    any_word = torch.randint(-2 ** 62, 2 ** 62, (512,), generator=g)
+    contents = [torch.full((512,), 1), torch.full((512,), -1), (torch.arange(512) << 12) + torch.arange(512) % 13 + 1,
+                (any_word & ~0xfff) + torch.arange(512) % 13 + 1]
+    results = {}
+    for words in contents:
+        assert (words != 0).all()
+
+        def workspace():
+            ws = torch.full((80 << 20,), 255, dtype=torch.uint8, device="cuda:0")
+            ws[:4096] = words.contiguous().view(torch.uint8).to("cuda:0")
+            return ws
+        for c, q, plan in counted_plans(fs, ctx, one_kernel, workspace):
+            n = q.shape[0] // 2
+            ws = plan._keep[-1]
+            for _ in range(3):
+                got = plan.run().clone()
+                assert torch.equal(bits(got), bits(results.setdefault(n, got)))
+                # parts were counted: a counter that came back at zero, and none left in between
+                counters = ws[:4096].view(torch.int64).cpu()
+                assert (counters == 0).any() and ((counters == 0) | (counters == words)).all()
+    for n, got in results.items():
+        k, v = c.values(0)
+        q = next(q for _, q, _ in counted_plans(fs, ctx, one_kernel, workspace) if q.shape[0] == 2 * n).cpu()
+        want = ref.attend(q[:n], k, v, 1500 - n, 128 ** -0.5)
+        bound = ref.attention_bound(q[:n], k, v, 1500 - n, 128 ** -0.5, 0, want, STEP["bf16"])
+        assert ((got.cpu()[:n].double() - want).abs() <= bound).all()
+
+
+def test_cut_items_are_the_same_on_every_run(env, one_kernel):
+    """Whichever block arrives last adds the parts in their order."""
+    fs, ctx = env
+    note(f"every run, kernel {one_kernel}")
+    ws = torch.zeros(80 << 20, dtype=torch.uint8, device="cuda:0")
+    for _, _, plan in counted_plans(fs, ctx, one_kernel, lambda: ws):
+        first = plan.run().clone()
+        for _ in range(40):
+            assert torch.equal(bits(plan.run()), bits(first))
