@@ -744,7 +744,7 @@ def _rows(t, shape, name, dtype=None):
 
 def _same_device(ctx, **tensors):
     for name, t in tensors.items():
-        if t is not None and t.is_cuda and t.device.index != ctx.device:
+        if getattr(t, "is_cuda", False) and t.device.index != ctx.device:  # what is no device tensor is refused by name
             raise _invalid(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
 
 
@@ -753,8 +753,8 @@ def quantize_rows(ctx: Context, x, stream=None):
     scale for each row (fs_quantize_rows)."""
     torch = _torch()
     p, stride = _rows(x, (None, None), "x")
-    _same_device(ctx, x=x)
     rows, cols = (int(n) for n in x.shape)
+    _same_device(ctx, x=x)
     codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
     scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(load_library().fs_quantize_rows(ctx.handle, p, _element_type(x.dtype), rows, cols, stride, codes.data_ptr(),
@@ -792,15 +792,16 @@ class MatmulPlan(_Plan):
         if out is None:
             out = torch.empty((M, N), dtype=out_dtype or torch.bfloat16, device=a.device)
         po, so = _rows(out, (M, N), "out", out_dtype)
-        _same_device(ctx, a=a, w=w, out=out)
         lib = load_library()
         need = _size(lib.fs_scaled_matmul_workspace_size, M, N, K)
         ws = workspace if workspace is not None else ctx.workspace(need)
+        _same_device(ctx, a=a, a_scale=a_scale, w=w, w_scale=w_scale, bias=bias, out=out, workspace=ws)
         self.out, self._keep = out, (a, a_scale, w, w_scale, bias, ws)
         self._fn = lib.fs_scaled_matmul
         self._args = (ctx.handle, pa, sa, _dev_ptr(a_scale, torch.float32, (M,), "a_scale"), pw, sw,
                       _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
-                      M, N, K, po, _element_type(out.dtype), so, ws.data_ptr(), ws.numel(), _stream(a.device, stream))
+                      M, N, K, po, _element_type(out.dtype), so, _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(),
+                      _stream(a.device, stream))
 
 
 def scaled_matmul(ctx: Context, a, a_scale, w, w_scale, bias=None, out_dtype=None, out=None, stream=None,
@@ -822,15 +823,16 @@ class LinearPlan(_Plan):
         if out is None:
             out = torch.empty((M, N), dtype=out_dtype or x.dtype, device=x.device)
         po, so = _rows(out, (M, N), "out", out_dtype)
-        _same_device(ctx, x=x, w=w, out=out)
         lib = load_library()
         need = _size(lib.fs_linear_workspace_size, M, N, K)
         ws = workspace if workspace is not None else ctx.workspace(need)
+        _same_device(ctx, x=x, w=w, w_scale=w_scale, bias=bias, out=out, workspace=ws)
         self.out, self._keep = out, (x, w, w_scale, bias, ws)
         self._fn = lib.fs_linear
         self._args = (ctx.handle, px, _element_type(x.dtype), sx, pw, sw,
                       _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
-                      M, N, K, po, _element_type(out.dtype), so, ws.data_ptr(), ws.numel(), _stream(x.device, stream))
+                      M, N, K, po, _element_type(out.dtype), so, _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(),
+                      _stream(x.device, stream))
 
 
 def linear(ctx: Context, x, w, w_scale, bias=None, out_dtype=None, out=None, stream=None, workspace=None):
@@ -867,6 +869,9 @@ class KVCache:
     @property
     def head_dim(self) -> int:
         return int(self.k.shape[3])
+
+    def _tensors(self):
+        return dict(k_codes=self.k, v_codes=self.v, k_scale=self.k_scale, v_scale=self.v_scale)
 
     def _struct(self):
         torch = _torch()
@@ -907,7 +912,7 @@ class AppendPlan(_Plan):
             if cos.dim() != 2:
                 raise _invalid("cos must be [positions, rotary_dim / 2]")
             reach, half = (int(n) for n in cos.shape)
-        _same_device(ctx, k=k, v=v, q=q, slots=slots, cache=cache.k)
+        _same_device(ctx, k=k, v=v, q=q, slots=slots, positions=positions, cos=cos, sin=sin, q_out=q_out, **cache._tensors())
         self.out, self._keep = (q_out if q is not None else None), (cache, k, v, q, slots, positions, cos, sin)
         self._fn = load_library().fs_cache_append
         self._args = (ctx.handle, ctypes.byref(self._cache), pk, sk, pv, sv, pq, sq, heads, _element_type(k.dtype), T,
@@ -935,7 +940,7 @@ class ReadPlan(_Plan):
         dtype = dtype or torch.float32
         if out is None:
             out = tuple(torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
-        _same_device(ctx, slots=slots, cache=cache.k)
+        _same_device(ctx, slots=slots, k_out=out[0], v_out=out[1], **cache._tensors())
         self.out, self._keep = out, (cache, slots)
         self._fn = load_library().fs_cache_read
         self._args = (ctx.handle, ctypes.byref(self._cache), T, _dev_ptr(slots, torch.int32, (T,), "slots"),
@@ -969,17 +974,17 @@ class AttentionPlan(_Plan):
         if out is None:
             out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
         po = _dev_ptr(out, q.dtype, (T, heads, cache.head_dim), "out")
-        _same_device(ctx, q=q, block_table=block_table, ctx_lens=ctx_lens, cu_q=cu_q, cache=cache.k)
         lib = load_library()
         need = _size(lib.fs_cache_attention_workspace_size, ctypes.byref(self._cache), heads, T, S)
         ws = workspace if workspace is not None else ctx.workspace(need)
+        _same_device(ctx, q=q, block_table=block_table, ctx_lens=ctx_lens, cu_q=cu_q, out=out, workspace=ws, **cache._tensors())
         self.out, self._keep = out, (cache, q, block_table, ctx_lens, cu_q, ws)
         self._fn = lib.fs_cache_attention
         self._args = (ctx.handle, ctypes.byref(self._cache), pq, sq, _element_type(q.dtype), heads, T, S,
                       _dev_ptr(cu_q, torch.int32, (S + 1,), "cu_q"), _dev_ptr(ctx_lens, torch.int32, (S,), "ctx_lens"),
                       _dev_ptr(block_table, torch.int32, (S, width), "block_table"), width, int(max_q),
-                      float(cache.head_dim ** -0.5 if scale is None else scale), int(window), po, ws.data_ptr(),
-                      ws.numel(), _stream(q.device, stream))
+                      float(cache.head_dim ** -0.5 if scale is None else scale), int(window), po,
+                      _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(), _stream(q.device, stream))
 
 
 def cache_attention(ctx: Context, cache: KVCache, q, block_table, ctx_lens, cu_q, max_q: int, scale=None,

@@ -372,3 +372,55 @@ def test_cut_items_are_the_same_on_every_run(env, one_kernel):
         first = plan.run().clone()
         for _ in range(40):
             assert torch.equal(bits(plan.run()), bits(first))
+
+
+# ------------------------------------------------------ tensors and streams --
+def every_plan(fs, ctx, stream=None, workspace=None):
+    """(call, the tensors that it is given) for every serving call."""
+    dev = "cuda:0"
+    i8 = lambda *s: torch.ones(*s, dtype=torch.int8, device=dev)  # noqa: E731
+    f = lambda *s: torch.ones(*s, device=dev)  # noqa: E731
+    h = lambda *s: torch.ones(*s, device=dev, dtype=torch.float16)  # noqa: E731
+    kv = fs.KVCache.empty(4, 2, 64, 16, dev)
+    cache = [kv.k, kv.v, kv.k_scale, kv.v_scale]
+    t = dict(a=i8(2, 64), a_scale=f(2), w=i8(3, 64), w_scale=f(3), bias=f(3), out=h(2, 3))
+    yield lambda: fs.scaled_matmul(ctx, **t, stream=stream, workspace=workspace), list(t.values())
+    u = dict(x=h(2, 64), w=i8(3, 64), w_scale=f(3), bias=f(3), out=h(2, 3))
+    yield lambda: fs.linear(ctx, **u, stream=stream, workspace=workspace), list(u.values())
+    n = dict(k=h(2, 2, 64), v=h(2, 2, 64), slots=i32([0, 1]), q=h(2, 4, 64), positions=i32([0, 1]), cos=f(3, 32), sin=f(3, 32),
+             q_out=h(2, 4, 64))
+    yield lambda: fs.cache_append(ctx, kv, **n, stream=stream), list(n.values()) + cache
+    slots, outs = i32([0, 1]), (h(2, 2, 64), h(2, 2, 64))
+    yield lambda: fs.cache_read(ctx, kv, slots, torch.float16, outs, stream=stream), [slots, *outs] + cache
+    s = dict(q=h(2, 4, 64), block_table=i32([[0]]), ctx_lens=i32([2]), cu_q=i32([0, 2]), max_q=2, out=h(2, 4, 64))
+    yield (lambda: fs.cache_attention(ctx, kv, **s, stream=stream, workspace=workspace),
+           [x for x in s.values() if isinstance(x, torch.Tensor)] + cache)
+    x = h(2, 64)
+    yield lambda: fs.quantize_rows(ctx, x, stream=stream), [x]
+
+
+def test_every_tensor_is_held_against_the_context_device(env, monkeypatch):
+    fs, ctx = env
+    seen, check = [], fs._same_device
+
+    def record(ctx, **tensors):
+        seen.extend(t for t in tensors.values() if t is not None)
+        check(ctx, **tensors)
+    monkeypatch.setattr(fs, "_same_device", record)
+    for call, tensors in every_plan(fs, ctx, workspace=torch.empty(80 << 20, dtype=torch.uint8, device="cuda:0")):
+        seen.clear()
+        call()
+        assert {t.data_ptr() for t in tensors} <= {t.data_ptr() for t in seen}
+
+
+def test_workspaces_that_are_refused(env):
+    fs, ctx = env
+    size = 80 << 20
+    for ws in (torch.empty(size, dtype=torch.uint8), torch.empty(size // 4, dtype=torch.float32, device="cuda:0"),
+               torch.empty(2 * size, dtype=torch.uint8, device="cuda:0")[::2]):
+        for i, (call, _) in enumerate(every_plan(fs, ctx, workspace=ws)):
+            if i not in (0, 1, 4):  # calls without a workspace
+                continue
+            with pytest.raises(fs.FleetSieveError) as e:
+                call()
+            assert e.value.status == fs.FS_ERR_INVALID_ARGUMENT and "workspace" in str(e.value)
