@@ -748,6 +748,38 @@ def _same_device(ctx, **tensors):
             raise _invalid(f"{name} is on {t.device}, the context on cuda:{ctx.device}")
 
 
+def _empty(shape, dtype, device, stream):
+    """A new output.  For a stream other than the current one its memory is
+    that stream's own: what the current one still has to do with memory of its
+    own is not waited for."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    out.record_stream(current)
+    return out
+
+
+def _workspace(ctx, workspace, need, stream):
+    torch = _torch()
+    if workspace is not None:
+        return workspace
+    ws = ctx.workspace(need)
+    # a larger one may take its place while this stream works on it
+    ws.record_stream(stream if stream is not None else torch.cuda.current_stream(ctx.device))
+    return ws
+
+
+def _keep_for(stream, *tensors):
+    """Memory given back while `stream` still works on it waits for it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def quantize_rows(ctx: Context, x, stream=None):
     """(codes int8 [rows, cols], scale float32 [rows]) of a matrix with a
     scale for each row (fs_quantize_rows)."""
@@ -755,10 +787,11 @@ def quantize_rows(ctx: Context, x, stream=None):
     p, stride = _rows(x, (None, None), "x")
     rows, cols = (int(n) for n in x.shape)
     _same_device(ctx, x=x)
-    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    codes = _empty((rows, cols), torch.int8, x.device, stream)
+    scale = _empty(rows, torch.float32, x.device, stream)
     _check(load_library().fs_quantize_rows(ctx.handle, p, _element_type(x.dtype), rows, cols, stride, codes.data_ptr(),
                                            cols, scale.data_ptr(), _stream(x.device, stream)))
+    _keep_for(stream, x)
     return codes, scale
 
 
@@ -771,7 +804,10 @@ def _size(fn, *args):
 class _Plan:
     """A call with its arguments checked and marshalled once; run() enqueues
     it again on the same device buffers, whose contents may change between
-    runs, and returns its output."""
+    runs, and returns its output.  It does so on `stream`, or on the stream that
+    is current when the plan is made.  Without a workspace it takes the
+    context's, which all its calls share: plans whose runs may overlap need
+    workspaces of their own."""
 
     def run(self):
         _check(self._fn(*self._args))
@@ -790,11 +826,11 @@ class MatmulPlan(_Plan):
         pw, sw = _rows(w, (None, K), "w", torch.int8)
         N = int(w.shape[0])
         if out is None:
-            out = torch.empty((M, N), dtype=out_dtype or torch.bfloat16, device=a.device)
+            out = _empty((M, N), out_dtype or torch.bfloat16, a.device, stream)
         po, so = _rows(out, (M, N), "out", out_dtype)
         lib = load_library()
         need = _size(lib.fs_scaled_matmul_workspace_size, M, N, K)
-        ws = workspace if workspace is not None else ctx.workspace(need)
+        ws = _workspace(ctx, workspace, need, stream)
         _same_device(ctx, a=a, a_scale=a_scale, w=w, w_scale=w_scale, bias=bias, out=out, workspace=ws)
         self.out, self._keep = out, (a, a_scale, w, w_scale, bias, ws)
         self._fn = lib.fs_scaled_matmul
@@ -802,6 +838,7 @@ class MatmulPlan(_Plan):
                       _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
                       M, N, K, po, _element_type(out.dtype), so, _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(),
                       _stream(a.device, stream))
+        _keep_for(stream, out, *self._keep)
 
 
 def scaled_matmul(ctx: Context, a, a_scale, w, w_scale, bias=None, out_dtype=None, out=None, stream=None,
@@ -821,11 +858,11 @@ class LinearPlan(_Plan):
         pw, sw = _rows(w, (None, K), "w", torch.int8)
         N = int(w.shape[0])
         if out is None:
-            out = torch.empty((M, N), dtype=out_dtype or x.dtype, device=x.device)
+            out = _empty((M, N), out_dtype or x.dtype, x.device, stream)
         po, so = _rows(out, (M, N), "out", out_dtype)
         lib = load_library()
         need = _size(lib.fs_linear_workspace_size, M, N, K)
-        ws = workspace if workspace is not None else ctx.workspace(need)
+        ws = _workspace(ctx, workspace, need, stream)
         _same_device(ctx, x=x, w=w, w_scale=w_scale, bias=bias, out=out, workspace=ws)
         self.out, self._keep = out, (x, w, w_scale, bias, ws)
         self._fn = lib.fs_linear
@@ -833,6 +870,7 @@ class LinearPlan(_Plan):
                       _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
                       M, N, K, po, _element_type(out.dtype), so, _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(),
                       _stream(x.device, stream))
+        _keep_for(stream, out, *self._keep)
 
 
 def linear(ctx: Context, x, w, w_scale, bias=None, out_dtype=None, out=None, stream=None, workspace=None):
@@ -903,7 +941,7 @@ class AppendPlan(_Plan):
             pq, sq = _rows(q, (T, None, cache.head_dim), "q", k.dtype)
             heads = int(q.shape[1])
             if q_out is None:
-                q_out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+                q_out = _empty((T, heads, cache.head_dim), q.dtype, q.device, stream)
             po = _dev_ptr(q_out, q.dtype, (T, heads, cache.head_dim), "q_out")
         reach = half = 0
         if cos is not None:
@@ -920,6 +958,7 @@ class AppendPlan(_Plan):
                       _dev_ptr(cos, torch.float32, (reach, half), "cos"),
                       _dev_ptr(sin, torch.float32, (reach, half), "sin") if cos is not None else None, reach, 2 * half,
                       po, _stream(k.device, stream))
+        _keep_for(stream, self.out, *self._keep[1:], *cache._tensors().values())
 
 
 def cache_append(ctx: Context, cache: KVCache, k, v, slots, q=None, positions=None, cos=None, sin=None, q_out=None,
@@ -939,13 +978,14 @@ class ReadPlan(_Plan):
         shape = (T, cache.n_heads, cache.head_dim)
         dtype = dtype or torch.float32
         if out is None:
-            out = tuple(torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+            out = tuple(_empty(shape, dtype, cache.k.device, stream) for _ in range(2))
         _same_device(ctx, slots=slots, k_out=out[0], v_out=out[1], **cache._tensors())
         self.out, self._keep = out, (cache, slots)
         self._fn = load_library().fs_cache_read
         self._args = (ctx.handle, ctypes.byref(self._cache), T, _dev_ptr(slots, torch.int32, (T,), "slots"),
                       _dev_ptr(out[0], dtype, shape, "k_out"), _dev_ptr(out[1], dtype, shape, "v_out"),
                       _element_type(dtype), _stream(cache.k.device, stream))
+        _keep_for(stream, *out, slots, *cache._tensors().values())
 
 
 def cache_read(ctx: Context, cache: KVCache, slots, dtype=None, out=None, stream=None):
@@ -972,11 +1012,11 @@ class AttentionPlan(_Plan):
             raise _invalid("block_table must be [sequences, width]")
         width = int(block_table.shape[1])
         if out is None:
-            out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+            out = _empty((T, heads, cache.head_dim), q.dtype, q.device, stream)
         po = _dev_ptr(out, q.dtype, (T, heads, cache.head_dim), "out")
         lib = load_library()
         need = _size(lib.fs_cache_attention_workspace_size, ctypes.byref(self._cache), heads, T, S)
-        ws = workspace if workspace is not None else ctx.workspace(need)
+        ws = _workspace(ctx, workspace, need, stream)
         _same_device(ctx, q=q, block_table=block_table, ctx_lens=ctx_lens, cu_q=cu_q, out=out, workspace=ws, **cache._tensors())
         self.out, self._keep = out, (cache, q, block_table, ctx_lens, cu_q, ws)
         self._fn = lib.fs_cache_attention
@@ -985,6 +1025,7 @@ class AttentionPlan(_Plan):
                       _dev_ptr(block_table, torch.int32, (S, width), "block_table"), width, int(max_q),
                       float(cache.head_dim ** -0.5 if scale is None else scale), int(window), po,
                       _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(), _stream(q.device, stream))
+        _keep_for(stream, out, *self._keep[1:], *cache._tensors().values())
 
 
 def cache_attention(ctx: Context, cache: KVCache, q, block_table, ctx_lens, cu_q, max_q: int, scale=None,

@@ -424,3 +424,52 @@ def test_workspaces_that_are_refused(env):
             with pytest.raises(fs.FleetSieveError) as e:
                 call()
             assert e.value.status == fs.FS_ERR_INVALID_ARGUMENT and "workspace" in str(e.value)
+
+
+def later(stream):
+    """Work of some tens of milliseconds ahead of what `stream` is given next."""
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(50_000_000)
+
+
+def test_outputs_for_another_stream_are_not_memory_that_the_current_one_still_reads(env):
+    fs, ctx = env
+    note("outputs for another stream")
+    n = 1 << 11
+    w, sw = torch.ones(n, 64, dtype=torch.int8, device="cuda:0"), torch.ones(n, device="cuda:0")
+    x = torch.ones(n, 64, dtype=torch.bfloat16, device="cuda:0")
+    side, current = torch.cuda.Stream(), torch.cuda.current_stream()
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda:0")
+    for _ in range(2):  # the second time both pools hold memory
+        read = torch.full((n, n), 7.0, dtype=torch.bfloat16, device="cuda:0")
+        torch.cuda.synchronize()
+        later(current)
+        copy = torch.empty_like(read)
+        copy.copy_(read)
+        del read  # its memory is the current stream's again, which has yet to copy it
+        out = fs.linear(ctx, x, w, sw, stream=side, workspace=ws)
+        torch.cuda.synchronize()
+        assert (copy == 7.0).all() and torch.isfinite(out).all() and not (out == 7.0).any()
+        del out, copy
+
+
+def test_inputs_and_workspaces_given_back_while_another_stream_works_on_them(env):
+    fs, ctx = env
+    note("inputs for another stream")
+    n, K = 1 << 10, 1 << 11
+    w, sw = torch.ones(64, K, dtype=torch.int8, device="cuda:0"), torch.ones(64, device="cuda:0")
+    side = torch.cuda.Stream()
+    own = fs.Context(0)
+    x = torch.ones(n, K, dtype=torch.bfloat16, device="cuda:0")
+    want = fs.linear(ctx, x, w, sw)
+    torch.cuda.synchronize()
+    later(side)
+    got = fs.linear(own, x, w, sw, stream=side)
+    old = own.workspace(0).numel()
+    del x
+    own.workspace(4 * old)  # another workspace: the one in use is given back
+    filler = [torch.full((n, K), 3.0, dtype=torch.bfloat16, device="cuda:0"), torch.full((old,), 255, dtype=torch.uint8, device="cuda:0")]
+    torch.cuda.synchronize()
+    assert torch.equal(bits(got), bits(want))
+    del filler
+    own.close()
