@@ -202,6 +202,32 @@ def settle(load: float, answer: int, prefill: float, steps):
     return served, UNSERVED
 
 
+def settle_between(load: float, answer: int, prefill, steps):
+    """((least, largest) capacity, (least, largest) tail) of `settle` over all
+    times between (fast, slow): prefill a pair, steps {batch: a pair}.
+
+    Between the two sides the cell may run with any batch from the fast side's to
+    the slow side's, or, where the slow side does not serve the load, with none.
+    A batch that runs serves the load, so its rate lies between the larger of its
+    slow rate and the load, and its fast rate."""
+    rate = lambda n, side: 1.0 / (prefill[side] + answer * steps[n][side] / n)  # noqa: E731
+
+    def tail(n, side):
+        free = 1.0 - load * prefill[side]
+        return min((prefill[side] + answer * steps[n][side]) / free, UNSERVED) if free > 0.0 else UNSERVED
+    caps, tails = [], []
+    for n in sorted(steps):
+        if rate(n, 0) >= load:
+            caps += [max(rate(n, 1), load), rate(n, 0)]
+            tails += [tail(n, 0), tail(n, 1)]
+        if rate(n, 1) >= load:  # no larger batch is needed, whatever the times
+            break
+    else:  # at the slow times no batch serves the load
+        caps += [max(rate(n, 1) for n in steps), min(max(rate(n, 0) for n in steps), load)]
+        tails.append(UNSERVED)
+    return (min(caps), max(caps)), (min(tails), max(tails))
+
+
 @dataclass
 class Times:
     """Seconds by TP degree and class: prefill (fast, slow), and for every
@@ -211,25 +237,21 @@ class Times:
 
 
 def intervals(problem: Problem, classes, times: Times) -> Intervals:
-    """Every cell's intervals, one order, none measured.  The slow sides give
-    the lower capacity and the upper tail.  Capacities lie on the 1/64 grid,
-    rounded away from the interval's inside."""
+    """Every cell's intervals, one order, none measured: all that `settle` gives
+    for times between the fast and the slow ones.  Capacities lie on the 1/64 grid,
+    rounded away from the interval's inside (but to one step of it at least)."""
     N = problem.n_cells
     cap, tail = np.zeros((2, N)), np.zeros((2, N))
     for cell in range(N):
         i, t, b = problem.cell_coords(cell)
         key = (int(problem.tp[t]), classes[i].name)
-        for side in (0, 1):  # fast, slow
-            steps = {n: s[side] for n, s in times.step[key].items()}
-            cap[side, cell], tail[side, cell] = settle(float(problem.levels[b]), classes[i].answer,
-                                                       times.prefill[key][side], steps)
-    # a slower replica may need a larger batch, whose rate may be above the
-    # faster one's: the interval holds both
-    lo, hi = cap.min(axis=0), cap.max(axis=0)
+        cap[:, cell], tail[:, cell] = settle_between(float(problem.levels[b]), classes[i].answer, times.prefill[key],
+                                                     times.step[key])
+    lo, hi = cap
     lo = np.maximum(np.floor(lo / QUANTUM), 1.0) * QUANTUM
     hi = np.maximum(np.ceil(hi / QUANTUM) * QUANTUM, lo)
     one = lambda x: np.ascontiguousarray(x[None], dtype=np.float32)  # noqa: E731
-    return Intervals(one(lo), one(hi), one(tail.min(axis=0)), one(tail.max(axis=0)), np.zeros((1, N), np.uint8))
+    return Intervals(one(lo), one(hi), one(tail[0]), one(tail[1]), np.zeros((1, N), np.uint8))
 
 
 def measure(ctx, decoder: Decoder, tps, batches, classes, layers: int = 8, link_gbs: float = 153.0, hop_us: float = 2.0,
