@@ -514,6 +514,7 @@ fs_status fs_quantize_rows(fs_context *ctx, const void *d_x, fs_dtype type, int6
  * [M][K], w [N][K] (both rows contiguous, strides >= K), out [M][N] of
  * out_type with stride >= N.  Any alignment is accepted; rows that start on
  * multiples of 16 bytes are faster.  Bitwise equal run to run.
+ * The workspace is not used at present (its size is 0).
  * FS_ERR_UNSUPPORTED where the product has more than 2^23 - 8 tiles (2^31 - 2048
  * channels of few rows, 5 * 10^11 results of many). */
 fs_status fs_scaled_matmul_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);

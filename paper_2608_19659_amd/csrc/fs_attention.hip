@@ -1167,7 +1167,6 @@ hipError_t attend_as(const AttendArgs &A, int kernel, void *ws, hipStream_t s) {
   const int64_t tiles = most_units(A);
   const bool chunks = takes_chunks(A, kernel);
   Parts P{(unsigned long long *)ws, (float *)((unsigned long long *)ws + kRowBlocks), 0};
-  hipError_t e;
   if (chunks) {
     // Alone where no sequence has few rows if the others have max_q tokens each and
     // all rows are someone's.  It takes any that has few all the same: lengths are
@@ -1175,8 +1174,6 @@ hipError_t attend_as(const AttendArgs &A, int kernel, void *ws, hipStream_t s) {
     const bool alone = kernel == 2 || A.n_seqs == 1 || (A.n_tokens - (A.n_seqs - 1) * (int64_t)A.max_q) * group >= kChunkLeast;
     const Share many{8, alone ? 1 : kChunkLeast, everything, 0};
     P.call = next_call();
-    e = allow_lds(&k_attend_chunk<TYPE, D, ONE>, lds);
-    if (e != hipSuccess) return e;
     k_attend_chunk<TYPE, D, ONE><<<kChunkBlocks, kChunkThreads, lds, s>>>(A, many, P);
     if (alone) return hipGetLastError();
   }
@@ -1206,8 +1203,6 @@ hipError_t attend_as(const AttendArgs &A, int kernel, void *ws, hipStream_t s) {
     const int64_t items = std::max<int64_t>(1, (int64_t)A.n_seqs * A.c.n_heads * ((std::min<int64_t>(most_rows, kChunkLeast) + kRows - 1) / kRows));
     const bool few_parts = std::min((tiles - kItemUnits) / few.least, 2 * BLOCKS / items) < 12;
     P.call = few_parts ? next_call() : 0;
-    hipError_t e = allow_lds(&k_attend_rows<TYPE, D, WAVES, ONE>, lds);
-    if (e != hipSuccess) return e;
     k_attend_rows<TYPE, D, WAVES, ONE><<<BLOCKS, 64 * WAVES, lds, s>>>(A, few, P);
     if (!few_parts) k_join<TYPE, D><<<BLOCKS - 1, 64 * kJoinWaves, lds, s>>>(A, few, BLOCKS, P.floats);
     return hipGetLastError();

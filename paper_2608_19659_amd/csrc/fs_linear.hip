@@ -653,7 +653,8 @@ hipError_t few_as(const QuantizeArgs &X, const MatmulArgs &A, int64_t rows_bytes
   constexpr int RING = S::NS * S::BN * S::BK;
   static_assert(RING >= S::WAVES * S::NT * 1024, "the parts' sums fit the ring");
   static_assert(S::THREADS == kFewThreads, "whole loads of a row");
-  const hipError_t e = allow_lds(&k_linear_few<S>, kFewBytes);
+  // more than 64 KB of LDS asked for at the launch
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_linear_few<S>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewBytes);
   if (e != hipSuccess) return e;
   const int tiles = (A.N + BN - 1) / BN;
   k_linear_few<S><<<(tiles + 7) / 8 * 8, S::THREADS, (size_t)(RING + rows_bytes), s>>>(X, A, tiles);
@@ -691,14 +692,12 @@ hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s) {
   return A.type == kF32 ? quantize_of<kF32>(A, s) : A.type == kF16 ? quantize_of<kF16>(A, s) : quantize_of<kBF16>(A, s);
 }
 
-size_t matmul_workspace(int32_t, int32_t, int32_t) { return 0; }
-
 bool matmul_fits(int32_t M, int32_t N, int32_t K) {
   const Tile &t = kTiles[best_tile(M, N, K)];
   return ((int64_t)(M - 1) / t.bm + 1) * ((N - 1) / t.bn + 1) <= kMostBlocks;
 }
 
-hipError_t launch_scaled_matmul(const MatmulArgs &A, void *, hipStream_t s) {
+hipError_t launch_scaled_matmul(const MatmulArgs &A, hipStream_t s) {
   return A.out_type == kF32 ? matmul_of<kF32>(A, s) : A.out_type == kF16 ? matmul_of<kF16>(A, s) : matmul_of<kBF16>(A, s);
 }
 

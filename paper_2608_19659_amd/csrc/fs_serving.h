@@ -36,10 +36,9 @@ struct MatmulArgs {
   int32_t M, N, K, out_type;
   int32_t a_padded;  // rows of a may be read (not their values used) to the next multiple of 16
 };
-size_t matmul_workspace(int32_t M, int32_t N, int32_t K);
 // Whether the product's tiles are few enough for one launch.
 bool matmul_fits(int32_t M, int32_t N, int32_t K);
-hipError_t launch_scaled_matmul(const MatmulArgs &A, void *ws, hipStream_t s);
+hipError_t launch_scaled_matmul(const MatmulArgs &A, hipStream_t s);
 
 // Both steps in one launch where there are few rows (codes and scales stay
 // unset); false: not for this call, nothing done.
@@ -95,12 +94,6 @@ hipError_t launch_check_slots(const Cache &c, const int32_t *slots, const int32_
 hipError_t launch_check_attention(const AttendArgs &A, int32_t *flag, hipStream_t s);
 
 #ifdef __HIPCC__
-template <class Kernel>
-inline hipError_t allow_lds(Kernel kernel, size_t bytes) {  // beyond 64 KB with the static part
-  if (bytes <= 16384) return hipSuccess;
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
-
 using half8 = _Float16 __attribute__((ext_vector_type(8)));
 using float4v = float __attribute__((ext_vector_type(4)));
 using float16v = float __attribute__((ext_vector_type(16)));

@@ -112,8 +112,8 @@ fs_status check_pages(const fs::Cache &c, const int32_t *d_slots, int64_t n_toke
 
 fs_status too_many_tiles() { return fail(FS_ERR_UNSUPPORTED, "the product has more tiles than a launch: split the call"); }
 
-fs_status matmul(const fs::MatmulArgs &A, void *ws, hipStream_t stream) {
-  const hipError_t e = fs::launch_scaled_matmul(A, ws, stream);
+fs_status matmul(const fs::MatmulArgs &A, hipStream_t stream) {
+  const hipError_t e = fs::launch_scaled_matmul(A, stream);
   return e == hipSuccess ? FS_OK : hip_fail(e, "matrix product launch");
 }
 
@@ -142,17 +142,16 @@ fs_status fs_scaled_matmul_workspace_size(int64_t M, int64_t N, int64_t K, size_
   if (!bytes) return fail(FS_ERR_INVALID_ARGUMENT, "bytes is NULL");
   const fs_status st = check_product(M, N, K);
   if (st != FS_OK) return st;
-  *bytes = align256(fs::matmul_workspace((int32_t)M, (int32_t)N, (int32_t)K));
+  *bytes = 0;  // no product has parts
   return FS_OK;
 }
 
 fs_status fs_scaled_matmul(fs_context *ctx, const int8_t *d_a, int64_t a_stride, const float *d_a_scale,
                            const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
                            int64_t M, int64_t N, int64_t K, void *d_out, fs_dtype out_type, int64_t out_stride,
-                           void *d_workspace, size_t workspace_bytes, hipStream_t stream) {
+                           void *, size_t, hipStream_t stream) {
   if (!ctx) return fail(FS_ERR_INVALID_ARGUMENT, "context is NULL");
-  size_t need = 0;
-  const fs_status st = fs_scaled_matmul_workspace_size(M, N, K, &need);
+  const fs_status st = check_product(M, N, K);
   if (st != FS_OK) return st;
   if (!element_type(out_type)) return fail(FS_ERR_INVALID_ARGUMENT, "unknown element type");
   if (a_stride < K || w_stride < K || out_stride < N)
@@ -160,21 +159,18 @@ fs_status fs_scaled_matmul(fs_context *ctx, const int8_t *d_a, int64_t a_stride,
   if (M == 0 || N == 0) return FS_OK;
   if (!d_a_scale || !d_w_scale || !d_out || (K > 0 && (!d_a || !d_w)))
     return fail(FS_ERR_INVALID_ARGUMENT, "array is NULL");
-  if (need && !d_workspace) return fail(FS_ERR_INVALID_ARGUMENT, "workspace is NULL");
-  if (workspace_bytes < need)
-    return fail(FS_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(need) + " bytes");
   if (!fs::matmul_fits((int32_t)M, (int32_t)N, (int32_t)K)) return too_many_tiles();
   DeviceGuard dg(ctx->device);
   if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
   return matmul({d_a, d_w, d_a_scale, d_w_scale, d_bias, d_out, a_stride, w_stride, out_stride, (int32_t)M, (int32_t)N,
                  (int32_t)K, (int32_t)out_type, 0},
-                d_workspace, stream);
+                stream);
 }
 
 fs_status fs_linear_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes) {
   const fs_status st = fs_scaled_matmul_workspace_size(M, N, K, bytes);
   if (st != FS_OK) return st;
-  *bytes += linear_codes(M, K) + align256(4 * (size_t)M);
+  *bytes = linear_codes(M, K) + align256(4 * (size_t)M);
   return FS_OK;
 }
 
@@ -208,7 +204,7 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
     return e == hipSuccess ? FS_OK : hip_fail(e, "linear launch");
   e = fs::launch_quantize_rows(rows, stream);
   if (e != hipSuccess) return hip_fail(e, "quantize launch");
-  return matmul(product, (uint8_t *)scale + align256(4 * (size_t)M), stream);
+  return matmul(product, stream);
 }
 
 fs_status fs_cache_append(fs_context *ctx, const fs_kv_cache *cache, const void *d_k, int64_t k_stride,

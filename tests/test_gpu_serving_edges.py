@@ -473,3 +473,8 @@ def test_inputs_and_workspaces_given_back_while_another_stream_works_on_them(env
     assert torch.equal(bits(got), bits(want))
     del filler
     own.close()
+
+
+def test_the_most_sequences_of_a_call(env, one_kernel):
+    lengths = [(13 * s) % 90 for s in range(4096)]
+    attention_case(env, lengths, [1 + s % 2 if s % 500 == 0 else 1 for s in range(4096)], 1, 1, 128, 64, 0, "bf16")
