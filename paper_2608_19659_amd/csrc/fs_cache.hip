@@ -270,10 +270,10 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs A) {
       if (i >= n) continue;
       const int64_t to = ((int64_t)(t0 + i) * c.n_heads + head) * D + d;
       if constexpr (TYPE == kF32) {
-        *(float4v *)((float *)A.k_out + to) = float4v{v[0], v[1], v[2], v[3]};
+        __builtin_memcpy((float *)A.k_out + to, v, 16);
       } else {
         const uint2 w = {bits16<TYPE>(v[0]) | (uint32_t)bits16<TYPE>(v[1]) << 16, bits16<TYPE>(v[2]) | (uint32_t)bits16<TYPE>(v[3]) << 16};
-        *(uint2 *)((uint16_t *)A.k_out + to) = w;
+        __builtin_memcpy((uint16_t *)A.k_out + to, &w, 8);
       }
     }
     return;

@@ -171,7 +171,7 @@ __device__ __forceinline__ void load8(const void *x, int64_t at, bool whole, flo
     for (int i = 0; i < 8; ++i) v[i] = value16<TYPE>((uint16_t)(raw[i >> 1] >> 16 * (i & 1)));
   }
 }
-// Eight to a place that is a multiple of 16 bytes.
+// Eight neighbouring elements to any place.
 template <int TYPE>
 __device__ __forceinline__ void store8(void *x, int64_t at, const float (&v)[8]) {
   if constexpr (TYPE == kF32) {
@@ -180,7 +180,7 @@ __device__ __forceinline__ void store8(void *x, int64_t at, const float (&v)[8])
     int4v raw;
 #pragma unroll
     for (int i = 0; i < 4; ++i) raw[i] = (int)(bits16<TYPE>(v[2 * i]) | (uint32_t)bits16<TYPE>(v[2 * i + 1]) << 16);
-    *(int4v *)((uint16_t *)x + at) = raw;
+    __builtin_memcpy((uint16_t *)x + at, &raw, 16);
   }
 }
 #endif

@@ -478,3 +478,38 @@ def test_inputs_and_workspaces_given_back_while_another_stream_works_on_them(env
 def test_the_most_sequences_of_a_call(env, one_kernel):
     lengths = [(13 * s) % 90 for s in range(4096)]
     attention_case(env, lengths, [1 + s % 2 if s % 500 == 0 else 1 for s in range(4096)], 1, 1, 128, 64, 0, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("offset", [1, 3, 4])
+def test_outputs_that_start_anywhere(env, dtype, offset):
+    """Outputs from any element of their memory on: the same bits, and nothing beside them."""
+    fs, ctx = env
+    note(f"outputs at +{offset} {dtype}")
+    ty = TYPES[dtype]
+
+    def place(*shape, of=ty):
+        flat = torch.full((offset + math.prod(shape) + 9,), 5, dtype=of, device="cuda:0")
+        return flat, flat[offset:offset + math.prod(shape)].view(shape)
+
+    def untouched(flat, view):
+        return (flat[:offset] == 5).all() and (flat[offset + view.numel():] == 5).all()
+    T, heads, group, D = 37, 2, 3, 64
+    c = ref.Paged([60], heads, D, 16, seed=4)
+    x = torch.randn(T, heads * (group + 2), D, generator=gen(3)).to(ty).to("cuda:0")
+    q, k, v = x[:, :heads * group], x[:, heads * group:heads * (group + 1)], x[:, heads * (group + 1):]
+    angle = torch.rand(60, 16, generator=gen(5)).to("cuda:0")
+    slots = i32(c.slots(0, 60 - T, 60))
+    turn = dict(positions=i32(list(range(60 - T, 60))), cos=angle.cos(), sin=angle.sin())
+    flat, out = place(T, heads * group, D)
+    got = fs.cache_append(ctx, c.device(fs), k, v, slots, q=q, q_out=out, **turn)
+    assert torch.equal(bits(got), bits(fs.cache_append(ctx, c.device(fs), k, v, slots, q=q, **turn))) and untouched(flat, out)
+    kv = c.device(fs)
+    both = [place(T, heads, D) for _ in range(2)]
+    fs.cache_read(ctx, kv, slots, ty, tuple(view for _, view in both))
+    for (flat, view), want in zip(both, fs.cache_read(ctx, kv, slots, ty)):
+        assert torch.equal(bits(view), bits(want)) and untouched(flat, view)
+    if dtype != "f32":
+        flat, out = place(T, heads * group, D)
+        call = lambda **kw: fs.cache_attention(ctx, kv, q, c.table.to("cuda:0"), i32([60]), i32([0, T]), T, **kw)  # noqa: E731
+        assert torch.equal(bits(call(out=out)), bits(call())) and untouched(flat, out)
