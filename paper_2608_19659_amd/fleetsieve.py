@@ -951,14 +951,14 @@ class AppendPlan(_Plan):
                 raise _invalid("cos must be [positions, rotary_dim / 2]")
             reach, half = (int(n) for n in cos.shape)
         _same_device(ctx, k=k, v=v, q=q, slots=slots, positions=positions, cos=cos, sin=sin, q_out=q_out, **cache._tensors())
-        self.out, self._keep = (q_out if q is not None else None), (cache, k, v, q, slots, positions, cos, sin)
+        self.out, self._keep = (q_out if q is not None else None), (*cache._tensors().values(), k, v, q, slots, positions, cos, sin)
         self._fn = load_library().fs_cache_append
         self._args = (ctx.handle, ctypes.byref(self._cache), pk, sk, pv, sv, pq, sq, heads, _element_type(k.dtype), T,
                       _dev_ptr(slots, torch.int32, (T,), "slots"), _dev_ptr(positions, torch.int32, (T,), "positions"),
                       _dev_ptr(cos, torch.float32, (reach, half), "cos"),
                       _dev_ptr(sin, torch.float32, (reach, half), "sin") if cos is not None else None, reach, 2 * half,
                       po, _stream(k.device, stream))
-        _keep_for(stream, self.out, *self._keep[1:], *cache._tensors().values())
+        _keep_for(stream, self.out, *self._keep)
 
 
 def cache_append(ctx: Context, cache: KVCache, k, v, slots, q=None, positions=None, cos=None, sin=None, q_out=None,
@@ -980,12 +980,12 @@ class ReadPlan(_Plan):
         if out is None:
             out = tuple(_empty(shape, dtype, cache.k.device, stream) for _ in range(2))
         _same_device(ctx, slots=slots, k_out=out[0], v_out=out[1], **cache._tensors())
-        self.out, self._keep = out, (cache, slots)
+        self.out, self._keep = out, (*cache._tensors().values(), slots)
         self._fn = load_library().fs_cache_read
         self._args = (ctx.handle, ctypes.byref(self._cache), T, _dev_ptr(slots, torch.int32, (T,), "slots"),
                       _dev_ptr(out[0], dtype, shape, "k_out"), _dev_ptr(out[1], dtype, shape, "v_out"),
                       _element_type(dtype), _stream(cache.k.device, stream))
-        _keep_for(stream, *out, slots, *cache._tensors().values())
+        _keep_for(stream, *out, *self._keep)
 
 
 def cache_read(ctx: Context, cache: KVCache, slots, dtype=None, out=None, stream=None):
@@ -1018,14 +1018,14 @@ class AttentionPlan(_Plan):
         need = _size(lib.fs_cache_attention_workspace_size, ctypes.byref(self._cache), heads, T, S)
         ws = _workspace(ctx, workspace, need, stream)
         _same_device(ctx, q=q, block_table=block_table, ctx_lens=ctx_lens, cu_q=cu_q, out=out, workspace=ws, **cache._tensors())
-        self.out, self._keep = out, (cache, q, block_table, ctx_lens, cu_q, ws)
+        self.out, self._keep = out, (*cache._tensors().values(), q, block_table, ctx_lens, cu_q, ws)
         self._fn = lib.fs_cache_attention
         self._args = (ctx.handle, ctypes.byref(self._cache), pq, sq, _element_type(q.dtype), heads, T, S,
                       _dev_ptr(cu_q, torch.int32, (S + 1,), "cu_q"), _dev_ptr(ctx_lens, torch.int32, (S,), "ctx_lens"),
                       _dev_ptr(block_table, torch.int32, (S, width), "block_table"), width, int(max_q),
                       float(cache.head_dim ** -0.5 if scale is None else scale), int(window), po,
                       _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(), _stream(q.device, stream))
-        _keep_for(stream, out, *self._keep[1:], *cache._tensors().values())
+        _keep_for(stream, out, *self._keep)
 
 
 def cache_attention(ctx: Context, cache: KVCache, q, block_table, ctx_lens, cu_q, max_q: int, scale=None,

@@ -513,3 +513,22 @@ def test_outputs_that_start_anywhere(env, dtype, offset):
         flat, out = place(T, heads * group, D)
         call = lambda **kw: fs.cache_attention(ctx, kv, q, c.table.to("cuda:0"), i32([60]), i32([0, T]), T, **kw)  # noqa: E731
         assert torch.equal(bits(call(out=out)), bits(call())) and untouched(flat, out)
+
+
+def test_plans_hold_the_memory_that_they_run_on(env):
+    """Also where a cache's tensors are exchanged for others."""
+    import gc
+    import weakref
+    fs, ctx = env
+    for make in (lambda kv, x, i: fs.AppendPlan(ctx, kv, x, x, i), lambda kv, x, i: fs.ReadPlan(ctx, kv, i),
+                 lambda kv, x, i: fs.AttentionPlan(ctx, kv, x, i[None], i + 1, i32([0, 1]), 1)):
+        kv = fs.KVCache.empty(2, 1, 64, 16, "cuda:0")
+        x, i = torch.ones(1, 1, 64, dtype=torch.float16, device="cuda:0"), i32([0])
+        plan = make(kv, x, i)
+        held = [weakref.ref(t) for t in (kv.k, kv.v, kv.k_scale, kv.v_scale)]
+        for name in ("k", "v", "k_scale", "v_scale"):
+            setattr(kv, name, getattr(kv, name).clone())
+        gc.collect()
+        assert all(r() is not None for r in held)
+        plan.run()
+    torch.cuda.synchronize()
