@@ -178,7 +178,7 @@ __device__ __forceinline__ int turn(int r) {
 // `to` on, in lane order.  Counted like any load; the compiler does not know
 // of it, so arrive() waits.
 __device__ __forceinline__ void load_to_lds(const int8_t *base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory", "m0");
 }
 
 // Waits until at most LOADS of this wavefront's loads are under way and its
