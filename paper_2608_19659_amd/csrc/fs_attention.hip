@@ -1141,15 +1141,17 @@ int64_t most_units(const AttendArgs &A) {
   return tiles + kItemUnits;
 }
 
-// Whether sequences of many rows go to the chunk kernel.  By what is measured a
-// call of e units of 16 rows takes the row kernel 8 + e / 650 us and the chunk
-// kernel about 30 us where items are short, 55 + e / 1900 where they are long, as
-// parts of 256 rows are costly to add.  (us, chunk kernel and row kernel: 310
-// tokens of 96 heads in a window of 100, e = 14880, 32.5 and 32.9; 2 x 816 in one
-// of 100, 21216, 30 and 41; 58 tokens of 20 users in one of 1000, 45696, 86 and
-// 109; 147 tokens of 23 users over up to 1277, 16180, 42 and 22; one of 1095 over
-// 1878, 32880, 100 and 73; 4 x 1704 over 1747, 93744, 53 and 100; 2 x 2048 over
-// 8192, 40 heads, 680 and 1716.)  Of the tokens one a sequence is left out: in a
+// Whether sequences of many rows go to the chunk kernel: from so many units of 16
+// rows, e, on, earlier where items are short, as parts of 256 rows are costly to
+// add.  Neither kernel's time follows from e alone (at the same e they are up to a
+// factor of two apart from call to call); 13000 and 45000 are what parts the calls
+// measured.  (us, chunk kernel and row kernel.  Up to 16 tiles: 310 tokens of 96
+// heads in a window of 100, e = 14880, 32.5 and 32.9; 2 x 816 in one of 100,
+// 21216, 30 and 41.  Longer: 147 tokens of 23 users over up to 1277, 16180, 42 and
+// 22; one of 1095 over 1878, 32880, 100 and 73; 58 tokens of 20 users in a window
+// of 1000, 45696, 86 and 109; 4 x 1704 over 1747, 93744, 53 and 100; 2 x 2048 over
+// 8192, 40 heads, 680 and 1716.)  Both counts are upper bounds, from the table's
+// width.  Of the tokens one a sequence is left out: in a
 // step of many users and one prompt they are those that no chunk has (120 users,
 // 79 tokens of 24 heads over 3869 among them: 65 us, by the chunk kernel 383).
 bool takes_chunks(const AttendArgs &A, int kernel) {

@@ -316,8 +316,8 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
     // a stage or two ahead, behind the codes of the same stage.  The last stage's
     // weights end in zeros, so whatever codes stand beside them are of no account:
     // places beyond the row take its last piece.  (us a call, so and with
-    // both operands through registers: 333 x 1001 x 1999 11.8 and 14.6, 64 x 5001 x
-    // 5119 17.4 and 23.1, 3000 x 5001 x 2999 78 and 90.)
+    // both operands through registers: 333 x 1001 x 1999 11.8 and 14.5, 64 x 5001 x
+    // 5119 18.2 and 23.3, 3000 x 5001 x 2999 76 and 89.)
     constexpr int AHEAD = S::NS >= 3 && S::MT * S::NT <= 8 ? 2 : 1;
     const int stages = (A.K + S::BK - 1) / S::BK;
     const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)lds + wave * 1024;
@@ -605,11 +605,11 @@ hipError_t matmul_as(const MatmulArgs &A, hipStream_t s) {
 
 // The tile whose rounds over the 256 CUs take least: a round's time is about
 // 1.5 us and, for each 5120 inner elements, what is measured with the tile at
-// one block a CU.  (K = 5120, us: 64 tokens x 5120 channels 9.6 with tiles of
-// 64 x 32, 11.0 with 32 x 32, 12.7 with 64 x 64; 64 x 896 4.2 with 16 x 16 and
-// 7.4 with 32 x 32; 128 x 5120 12.6 with 64 x 64, 16.4 with 64 x 32; 2048 x
-// 5120 70 with 128 x 64, 78 with 256 x 256; 8192 x 20480 831 with 256 x 256,
-// 951 with 256 x 128.)
+// one block a CU.  (K = 5120, us of the product alone, one call after another:
+// 64 tokens x 5120 channels 9.0 with tiles of 64 x 32, 12.1 with 32 x 32, 11.1
+// with 64 x 64; 64 x 896 4.3 with 16 x 16 and 6.2 with 32 x 32; 128 x 5120 11.3
+// with 64 x 64, 15.9 with 64 x 32; 2048 x 5120 70 with 128 x 64 and with 256 x
+// 256; 8192 x 20480 743 with 256 x 256, 847 with 256 x 128.)
 struct Tile {
   int bm, bn;
   double us;
@@ -662,11 +662,11 @@ hipError_t few_as(const QuantizeArgs &X, const MatmulArgs &A, int64_t rows_bytes
 }
 
 // Where one launch is faster than two: a block a CU or less, or a single row
-// and two blocks a CU.  (bfloat16, us of one launch and of two: 1 x 7168 x 5120
-// 9.5 and 12.5, 4 rows 11.3 and 12.7; 1 x 896 x 5120 5.9 and 8.2; 1 x 5120 x 640
-// 4.6 and 8.2; 1 x 5120 x 20480 23.8 and 28.9; 1 x 10240 x 5120 13.2 and 16.1;
-// 4 x 10240 x 5120 18.9 and 16.5, where every CU makes the codes twice.  896
-// channels in tiles of 32: 7.1.)
+// and two blocks a CU.  (bfloat16, eight sets of weights in turn, us of one
+// launch and of two: 1 x 7168 x 5120 8.9 and 11.6, 4 rows 10.4 and 11.6; 1 x 896
+// x 5120 5.3 and 7.3; 1 x 5120 x 640 4.1 and 7.3; 1 x 5120 x 20480 23.5 and 28.6;
+// 1 x 10240 x 5120 12.9 and 16.2; 4 x 10240 x 5120 18.9 and 16.2, where every CU
+// makes the codes twice.)
 template <int TYPE>
 bool few_of(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_t *e) {
   const int64_t size = X.type == kF32 ? 4 : 2, load = kFewThreads * 16;

@@ -30,8 +30,9 @@ fs_status check_product(int64_t M, int64_t N, int64_t K) {
 
 // Codes of M rows for fs_linear: rows an odd number of lines of 128 bytes apart,
 // so that the same columns of neighbouring rows, which all tiles read together,
-// do not meet in a few channels of L2.  (2048 x 5120 x 5120 80 us a call, with
-// rows of 5120 bytes 84; 64 rows 12.0 either way.)
+// do not meet in a few channels of L2.  (2048 x 5120 x 5120 78 to 80 us a call
+// and 79 with rows of 5120 bytes on one card, 80 and 84 on another; 64 rows 12.3
+// either way.)
 int64_t padded(int64_t K) { return ((K + 127) / 128 | 1) * 128; }
 
 size_t linear_codes(int64_t M, int64_t K) { return align256((size_t)(M * padded(K))); }
