@@ -606,7 +606,11 @@ fs_status fs_cache_read(fs_context *ctx, const fs_kv_cache *cache, int64_t n_tok
  *
  * Queries and probabilities enter the products as pairs of 8-bit integers
  * (15 bits against the row's or block's largest) or as binary16 values, the
- * sums are exact or binary32.  Results are equal run to run.
+ * sums are exact or binary32.  Results are equal run to run.  A query with a
+ * NaN or an infinity gets NaN.  Value scales of the pages that a query sees may
+ * differ by a factor of 2^100; tokens of a page of smaller scale still lose
+ * their weight.  table_width counts as the longest context where work is dealt
+ * out: tables far wider than the contexts cost time.
  *
  * With FS_VALIDATE=1 lengths and pages outside their ranges are refused (the
  * call waits for the stream); otherwise they are clamped (of a sequence with
