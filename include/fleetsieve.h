@@ -490,8 +490,10 @@ fs_status fs_profile_loop(fs_context *ctx, const fs_problem *p, fs_intervals iv,
  * s stands for c * s.  Elements are FS_F32, FS_F16 or FS_BF16; sums, softmax
  * statistics and scales are binary32 or 32-bit integers, results are rounded
  * once, to nearest even, when they are stored.  No size may exceed 2^31 - 1;
- * offsets are 64-bit.  A call with nothing to do (no rows, no tokens) returns
- * FS_OK and enqueues nothing. */
+ * offsets are 64-bit.  Outputs and workspaces may not overlap inputs.  A call
+ * with nothing to do (no rows, no tokens) returns FS_OK and enqueues nothing.
+ * Checks under FS_VALIDATE=1 wait for the stream: while it is being captured
+ * the cache's calls are refused with FS_ERR_DEVICE. */
 typedef enum fs_dtype { FS_F32 = 0, FS_F16 = 1, FS_BF16 = 2 } fs_dtype;
 
 /* Codes of each row of x [rows][cols] (row stride x_stride >= cols), with one
