@@ -961,6 +961,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_attend_chunk(AttendArgs A,
         top_s = max_over_32(top_s);
         // Logits so large that a rounding less would tell and a value scale would be
         // lost in them: as they are, the scale added to their differences from the largest.
+        // (Past 2^27 the maximum holds none of the scale, and probabilities, with 2^14 over
+        // one, hold value scales up to 2.)
         const bool wild = __any(fabsf(top_s) > 0x1p20f && top_s > kFloor);
         if (wild) {
           top_s = kFloor;
