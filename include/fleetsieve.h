@@ -533,6 +533,49 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
                     void *d_out, fs_dtype out_type, int64_t out_stride, void *d_workspace, size_t workspace_bytes,
                     hipStream_t stream);
 
+/* What stands before a projection of a decoder layer: the RMS norm of the rows,
+ * x[m][k] * gain[k] / sqrt(mean_k x[m][k]^2 + eps), binary32 (gain NULL: ones;
+ * eps in [2^-80, 2^80]).  The codes are those of x * gain (each product rounded),
+ * the row's factor goes into the row's scale. */
+typedef struct fs_norm {
+  const float *gain; /* [K], device memory, or NULL */
+  float eps;
+} fs_norm;
+
+/* What stands behind it: gelu(t) = t (1 + erf(t / sqrt 2)) / 2, or with its tanh
+ * form; silu(t) = t / (1 + e^-t). */
+typedef enum fs_activation {
+  FS_ACT_NONE = 0,
+  FS_ACT_RELU = 1,
+  FS_ACT_GELU = 2,
+  FS_ACT_GELU_TANH = 3,
+  FS_ACT_SILU = 4
+} fs_activation;
+
+/* out[m][n] = act(y[m][n]) + residual[m][n], with y the projection of fs_linear
+ * behind the norm (norm NULL: none), its bias (NULL: none) among it.  residual
+ * [M][N] is of out_type (NULL: none); it may be out itself, with out's stride, and
+ * may not overlap it otherwise.  All in binary32, rounded once; without norm,
+ * activation and residual the bits of fs_linear.  Activations are off by less than
+ * 2^-20 (1 + |y|) |act(y)| + 2^-22 |y|.  A row with a NaN or an infinity, in x or
+ * x * gain, gives NaN. */
+fs_status fs_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
+fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
+                     const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
+                     fs_activation activation, const void *d_residual, int64_t residual_stride, int64_t M, int64_t N,
+                     int64_t K, void *d_out, fs_dtype out_type, int64_t out_stride, void *d_workspace,
+                     size_t workspace_bytes, hipStream_t stream);
+
+/* The first half of a gated feed-forward block, out[m][n] = act(g[m][n]) u[m][n]:
+ * g and u are the projections of the (normed) rows by w's rows 0 .. N - 1 and
+ * N .. 2 N - 1, with w_scale and bias [2 N] likewise (2 N < 2^31).  Gates and values
+ * stay in registers: one launch behind the codes', or one in all for few rows. */
+fs_status fs_gated_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
+fs_status fs_gated_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
+                           const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
+                           fs_activation activation, int64_t M, int64_t N, int64_t K, void *d_out, fs_dtype out_type,
+                           int64_t out_stride, void *d_workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* A paged cache of keys and values in 8 bits with one scale for each page and
  * head.  Slot number = page * page_size + place in the page.  Values lie with
  * the tokens of a page adjacent, so that a product over tokens reads whole

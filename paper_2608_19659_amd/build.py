@@ -17,7 +17,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfleetsieve.so")
-SOURCES = [os.path.join(CSRC, n) for n in ("fs_kernels.hip", "fs_linear.hip", "fs_cache.hip", "fs_attention.hip",
+SOURCES = [os.path.join(CSRC, n) for n in ("fs_kernels.hip", "fs_linear.hip", "fs_project.hip", "fs_cache.hip", "fs_attention.hip",
                                            "fs_api.cpp", "fs_serving_api.cpp")]
 
 HIP_FLAGS = [

@@ -1,0 +1,40 @@
+// fs_project.hip -- projections with what stands before and behind them in a
+// decoder layer: the rows' RMS norm in front of the quantisation; an activation
+// and the residual stream behind the product, or the product of the activated
+// gate and the value, while the sums are in registers.
+//
+// Bounds: up to a few hundred rows the weights' bytes, then the matrix units.
+// Against the separate calls a layer saves the norms', the activation's and the
+// sums' launches and their passes over the rows, and a gated block's gates and
+// values are never stored.
+#include "fs_product.h"
+
+namespace fs {
+namespace {
+
+constexpr int kAnyType = -1;  // the output's type is looked at when a tile is stored
+
+template <Finish FINISH>
+bool few_finished(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_t *e) {
+  return X.normed ? few_of<kAnyType, FINISH, true>(X, A, s, e) : few_of<kAnyType, FINISH, false>(X, A, s, e);
+}
+
+}  // namespace
+
+bool launch_project_few(const QuantizeArgs &X, const MatmulArgs &A, bool gated, hipStream_t s, hipError_t *e) {
+  if (!few_rows(X, A)) return false;
+  if (gated && A.N * A.w_stride > (int64_t)1 << 31) return false;  // both rows of a channel: in 32 bits from the first on
+  return gated ? few_finished<kGated>(X, A, s, e) : few_finished<kFinished>(X, A, s, e);
+}
+
+hipError_t launch_quantize_normed(const QuantizeArgs &A, hipStream_t s) {
+  return A.type == kF32   ? quantize_of<kF32, true>(A, s)
+         : A.type == kF16 ? quantize_of<kF16, true>(A, s)
+                          : quantize_of<kBF16, true>(A, s);
+}
+
+hipError_t launch_project(const MatmulArgs &A, bool gated, hipStream_t s) {
+  return gated ? matmul_of<kAnyType, kGated>(A, s) : matmul_of<kAnyType, kFinished>(A, s);
+}
+
+}  // namespace fs

@@ -21,8 +21,13 @@ struct QuantizeArgs {
   float *scale;
   int64_t x_stride, code_stride;
   int32_t rows, cols, type;
+  int32_t normed;     // the rows' RMS norm first:
+  const float *gain;  // factor of each column, NULL for ones
+  float eps;
 };
 hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s);
+
+enum Activation : int32_t { kNoActivation = 0, kRelu = 1, kGelu = 2, kGeluTanh = 3, kSilu = 4 };
 
 // A launch has fewer than 2^32 threads along its grid's first dimension: blocks
 // of up to 512 threads, in multiples of eight, are at most this many.
@@ -35,6 +40,10 @@ struct MatmulArgs {
   int64_t a_stride, w_stride, out_stride;
   int32_t M, N, K, out_type;
   int32_t a_padded;  // rows of a may be read (not their values used) to the next multiple of 16
+  // launch_project only:
+  int32_t activation;
+  const void *residual;  // of out's type, or NULL; may be out
+  int64_t residual_stride;
 };
 // Whether the product's tiles are few enough for one launch.
 bool matmul_fits(int32_t M, int32_t N, int32_t K);
@@ -43,6 +52,12 @@ hipError_t launch_scaled_matmul(const MatmulArgs &A, hipStream_t s);
 // Both steps in one launch where there are few rows (codes and scales stay
 // unset); false: not for this call, nothing done.
 bool launch_linear_few(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s, hipError_t *e);
+
+// The same with an RMS norm before and an activation and a residual behind, or
+// gated: w has 2 N rows, the gates' and then the values'.
+hipError_t launch_quantize_normed(const QuantizeArgs &A, hipStream_t s);
+hipError_t launch_project(const MatmulArgs &A, bool gated, hipStream_t s);
+bool launch_project_few(const QuantizeArgs &X, const MatmulArgs &A, bool gated, hipStream_t s, hipError_t *e);
 
 struct Cache {
   int8_t *k, *v;

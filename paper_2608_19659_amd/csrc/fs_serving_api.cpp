@@ -118,6 +118,57 @@ fs_status matmul(const fs::MatmulArgs &A, hipStream_t stream) {
   return e == hipSuccess ? FS_OK : hip_fail(e, "matrix product launch");
 }
 
+// fs_project and fs_gated_project.
+fs_status project(fs_context *ctx, const fs_norm *norm, int64_t w_rows, bool gated, fs::QuantizeArgs rows,
+                  fs::MatmulArgs product, int64_t M, int64_t N, int64_t K, void *d_workspace, size_t workspace_bytes,
+                  hipStream_t stream) {
+  if (!ctx) return fail(FS_ERR_INVALID_ARGUMENT, "context is NULL");
+  size_t need = 0;
+  const fs_status st = fs_linear_workspace_size(M, w_rows, K, &need);
+  if (st != FS_OK) return st;
+  if (!element_type((fs_dtype)rows.type) || !element_type((fs_dtype)product.out_type))
+    return fail(FS_ERR_INVALID_ARGUMENT, "unknown element type");
+  if (product.activation < FS_ACT_NONE || product.activation > FS_ACT_SILU)
+    return fail(FS_ERR_INVALID_ARGUMENT, "unknown activation");
+  if (norm && !(norm->eps >= 0x1p-80f && norm->eps <= 0x1p80f))
+    return fail(FS_ERR_INVALID_ARGUMENT, "the norm's eps must be in [2^-80, 2^80]");
+  if (rows.x_stride < K || product.w_stride < K || product.out_stride < N || (product.residual && product.residual_stride < N))
+    return fail(FS_ERR_INVALID_ARGUMENT, "row strides must be at least the rows' lengths");
+  if (M == 0 || N == 0) return FS_OK;
+  if (!product.w_scale || !product.out || (K > 0 && (!rows.x || !product.w)))
+    return fail(FS_ERR_INVALID_ARGUMENT, "array is NULL");
+  if (K > 0 && rows.x == product.out) return fail(FS_ERR_INVALID_ARGUMENT, "out may not be x");
+  if (product.residual == product.out && product.residual_stride != product.out_stride)
+    return fail(FS_ERR_INVALID_ARGUMENT, "a residual that is out must have out's stride");
+  if (!d_workspace) return fail(FS_ERR_INVALID_ARGUMENT, "workspace is NULL");
+  if (workspace_bytes < need)
+    return fail(FS_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(need) + " bytes");
+  if ((uintptr_t)d_workspace & 15) return fail(FS_ERR_INVALID_ARGUMENT, "the workspace must start on a multiple of 16 bytes");
+  if (!fs::matmul_fits((int32_t)M, (int32_t)w_rows, (int32_t)K)) return too_many_tiles();
+  DeviceGuard dg(ctx->device);
+  if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
+  rows.codes = (int8_t *)d_workspace;
+  rows.scale = (float *)(rows.codes + linear_codes(M, K));
+  rows.code_stride = product.a_stride = padded(K);
+  rows.rows = product.M = (int32_t)M;
+  rows.cols = product.K = (int32_t)K;
+  product.N = (int32_t)N;
+  product.a = rows.codes;
+  product.a_scale = rows.scale;
+  product.a_padded = 1;
+  if (norm) {
+    rows.normed = 1;
+    rows.gain = norm->gain;
+    rows.eps = norm->eps;
+  }
+  hipError_t e = hipSuccess;
+  if (fs::launch_project_few(rows, product, gated, stream, &e)) return e == hipSuccess ? FS_OK : hip_fail(e, "projection launch");
+  e = norm ? fs::launch_quantize_normed(rows, stream) : fs::launch_quantize_rows(rows, stream);
+  if (e != hipSuccess) return hip_fail(e, "quantize launch");
+  e = fs::launch_project(product, gated, stream);
+  return e == hipSuccess ? FS_OK : hip_fail(e, "projection launch");
+}
+
 }  // namespace
 
 extern "C" {
@@ -206,6 +257,59 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
   e = fs::launch_quantize_rows(rows, stream);
   if (e != hipSuccess) return hip_fail(e, "quantize launch");
   return matmul(product, stream);
+}
+
+fs_status fs_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes) {
+  return fs_linear_workspace_size(M, N, K, bytes);
+}
+
+fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
+                     const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
+                     fs_activation activation, const void *d_residual, int64_t residual_stride, int64_t M, int64_t N,
+                     int64_t K, void *d_out, fs_dtype out_type, int64_t out_stride, void *d_workspace,
+                     size_t workspace_bytes, hipStream_t stream) {
+  fs::QuantizeArgs rows{};
+  rows.x = d_x;
+  rows.type = (int32_t)type;
+  rows.x_stride = x_stride;
+  fs::MatmulArgs product{};
+  product.w = d_w;
+  product.w_stride = w_stride;
+  product.w_scale = d_w_scale;
+  product.bias = d_bias;
+  product.activation = (int32_t)activation;
+  product.residual = d_residual;
+  product.residual_stride = residual_stride;
+  product.out = d_out;
+  product.out_type = (int32_t)out_type;
+  product.out_stride = out_stride;
+  return project(ctx, norm, N, false, rows, product, M, N, K, d_workspace, workspace_bytes, stream);
+}
+
+fs_status fs_gated_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes) {
+  if (N < 0 || N > kMost / 2) return fail(FS_ERR_INVALID_ARGUMENT, "2 N must be in [0, 2^31)");
+  return fs_linear_workspace_size(M, 2 * N, K, bytes);
+}
+
+fs_status fs_gated_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
+                           const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
+                           fs_activation activation, int64_t M, int64_t N, int64_t K, void *d_out, fs_dtype out_type,
+                           int64_t out_stride, void *d_workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (N < 0 || N > kMost / 2) return fail(FS_ERR_INVALID_ARGUMENT, "2 N must be in [0, 2^31)");
+  fs::QuantizeArgs rows{};
+  rows.x = d_x;
+  rows.type = (int32_t)type;
+  rows.x_stride = x_stride;
+  fs::MatmulArgs product{};
+  product.w = d_w;
+  product.w_stride = w_stride;
+  product.w_scale = d_w_scale;
+  product.bias = d_bias;
+  product.activation = (int32_t)activation;
+  product.out = d_out;
+  product.out_type = (int32_t)out_type;
+  product.out_stride = out_stride;
+  return project(ctx, norm, 2 * N, true, rows, product, M, N, K, d_workspace, workspace_bytes, stream);
 }
 
 fs_status fs_cache_append(fs_context *ctx, const fs_kv_cache *cache, const void *d_k, int64_t k_stride,

@@ -42,7 +42,8 @@ EXPORTED = ("fs_context_create", "fs_context_destroy", "fs_context_set_option", 
             "fs_solve_batch_lex", "fs_certify_lex", "fs_refit_intervals", "fs_loop_refit_workspace_size",
             "fs_score_lex_workspace_size", "fs_score_candidates_lex", "fs_clamp_samples",
             "fs_score_candidates_noalloc", "fs_quantize_rows", "fs_scaled_matmul_workspace_size", "fs_scaled_matmul",
-            "fs_linear_workspace_size", "fs_linear", "fs_cache_append", "fs_cache_read",
+            "fs_linear_workspace_size", "fs_linear", "fs_project_workspace_size", "fs_project",
+            "fs_gated_project_workspace_size", "fs_gated_project", "fs_cache_append", "fs_cache_read",
             "fs_cache_attention_workspace_size", "fs_cache_attention")
 POLICY_SCORE, POLICY_ORDER = 0, 1
 CELL_SECONDS = 300.0
@@ -131,6 +132,9 @@ def load_library():
     lib.fs_scaled_matmul.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     lib.fs_linear_workspace_size.argtypes = [i64, i64, i64, psz]
     lib.fs_linear.argtypes = [vp, vp, i32, i64, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.fs_project_workspace_size.argtypes = lib.fs_gated_project_workspace_size.argtypes = [i64, i64, i64, psz]
+    lib.fs_project.argtypes = [vp, vp, i32, i64, vp, vp, i64, vp, vp, i32, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.fs_gated_project.argtypes = [vp, vp, i32, i64, vp, vp, i64, vp, vp, i32, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     lib.fs_cache_append.argtypes = [vp, C, vp, i64, vp, i64, vp, i64, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp]
     lib.fs_cache_read.argtypes = [vp, C, i64, vp, vp, vp, i32, vp]
     lib.fs_cache_attention_workspace_size.argtypes = [C, i32, i64, i32, psz]
@@ -876,6 +880,108 @@ class LinearPlan(_Plan):
 def linear(ctx: Context, x, w, w_scale, bias=None, out_dtype=None, out=None, stream=None, workspace=None):
     """fs_linear, one call (see LinearPlan)."""
     return LinearPlan(ctx, x, w, w_scale, bias, out_dtype, out, stream, workspace).run()
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("gain", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+@dataclass
+class Norm:
+    """The RMS norm of a projection's rows, x * gain / sqrt(mean x^2 + eps):
+    gain float32 [K], None for ones."""
+    gain: object = None
+    eps: float = 1e-6
+
+    def _struct(self, K):
+        torch = _torch()
+        return _Norm(_dev_ptr(self.gain, torch.float32, (K,), "gain"), float(self.eps))
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise _invalid(f"activation must be one of {', '.join(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+class ProjectPlan(_Plan):
+    """act(y) + residual, y the projection of x [M, K] (LinearPlan) behind the
+    rows' norm (fs_project).  residual [M, N] has out's type and may be out
+    itself: then the call adds to it."""
+
+    def __init__(self, ctx: Context, x, w, w_scale, norm: Norm | None = None, bias=None, activation: str = "none",
+                 residual=None, out_dtype=None, out=None, stream=None, workspace=None):
+        torch = _torch()
+        px, sx = _rows(x, (None, None), "x")
+        M, K = (int(n) for n in x.shape)
+        pw, sw = _rows(w, (None, K), "w", torch.int8)
+        N = int(w.shape[0])
+        if out is None:
+            out = _empty((M, N), out_dtype or x.dtype, x.device, stream)
+        po, so = _rows(out, (M, N), "out", out_dtype)
+        pr, sr = _rows(residual, (M, N), "residual", out.dtype) if residual is not None else (None, 0)
+        lib = load_library()
+        need = _size(lib.fs_project_workspace_size, M, N, K)
+        ws = _workspace(ctx, workspace, need, stream)
+        gain = norm.gain if norm is not None else None
+        _same_device(ctx, x=x, gain=gain, w=w, w_scale=w_scale, bias=bias, residual=residual, out=out, workspace=ws)
+        self._norm = norm._struct(K) if norm is not None else None
+        self.out, self._keep = out, (x, gain, w, w_scale, bias, residual, ws)
+        self._fn = lib.fs_project
+        self._args = (ctx.handle, px, _element_type(x.dtype), sx, None if norm is None else ctypes.byref(self._norm), pw, sw,
+                      _dev_ptr(w_scale, torch.float32, (N,), "w_scale"), _dev_ptr(bias, torch.float32, (N,), "bias"),
+                      _activation(activation), pr, sr, M, N, K, po, _element_type(out.dtype), so,
+                      _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(), _stream(x.device, stream))
+        _keep_for(stream, out, *self._keep)
+
+
+def project(ctx: Context, x, w, w_scale, norm: Norm | None = None, bias=None, activation: str = "none", residual=None,
+            out_dtype=None, out=None, stream=None, workspace=None):
+    """fs_project, one call (see ProjectPlan)."""
+    return ProjectPlan(ctx, x, w, w_scale, norm, bias, activation, residual, out_dtype, out, stream, workspace).run()
+
+
+class GatedProjectPlan(_Plan):
+    """act(g) * u, g and u the projections of x [M, K] behind the rows' norm by
+    w int8 [2 N, K]: the gates' N rows, then the values' (fs_gated_project);
+    w_scale and bias [2 N]."""
+
+    def __init__(self, ctx: Context, x, w, w_scale, norm: Norm | None = None, bias=None, activation: str = "silu",
+                 out_dtype=None, out=None, stream=None, workspace=None):
+        torch = _torch()
+        px, sx = _rows(x, (None, None), "x")
+        M, K = (int(n) for n in x.shape)
+        pw, sw = _rows(w, (None, K), "w", torch.int8)
+        rows = int(w.shape[0])
+        if rows % 2:
+            raise _invalid(f"w must have a gate's and a value's row for each channel, got {rows} rows")
+        N = rows // 2
+        if out is None:
+            out = _empty((M, N), out_dtype or x.dtype, x.device, stream)
+        po, so = _rows(out, (M, N), "out", out_dtype)
+        lib = load_library()
+        need = _size(lib.fs_gated_project_workspace_size, M, N, K)
+        ws = _workspace(ctx, workspace, need, stream)
+        gain = norm.gain if norm is not None else None
+        _same_device(ctx, x=x, gain=gain, w=w, w_scale=w_scale, bias=bias, out=out, workspace=ws)
+        self._norm = norm._struct(K) if norm is not None else None
+        self.out, self._keep = out, (x, gain, w, w_scale, bias, ws)
+        self._fn = lib.fs_gated_project
+        self._args = (ctx.handle, px, _element_type(x.dtype), sx, None if norm is None else ctypes.byref(self._norm), pw, sw,
+                      _dev_ptr(w_scale, torch.float32, (rows,), "w_scale"),
+                      _dev_ptr(bias, torch.float32, (rows,), "bias"), _activation(activation), M, N, K, po,
+                      _element_type(out.dtype), so, _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(),
+                      _stream(x.device, stream))
+        _keep_for(stream, out, *self._keep)
+
+
+def gated_project(ctx: Context, x, w, w_scale, norm: Norm | None = None, bias=None, activation: str = "silu",
+                  out_dtype=None, out=None, stream=None, workspace=None):
+    """fs_gated_project, one call (see GatedProjectPlan)."""
+    return GatedProjectPlan(ctx, x, w, w_scale, norm, bias, activation, out_dtype, out, stream, workspace).run()
 
 
 @dataclass

@@ -1,0 +1,87 @@
+"""Plain 64-bit statements, on the CPU, of what a decoder layer does around its
+products and of state attention, with bounds of the results' errors."""
+import math
+
+import torch
+
+TINY = 2.0 ** -100
+STEP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+# half the least spacing, which is 2^-149, 2^-24 and 2^-133: what rounding moves a result below the normal numbers
+SMALLEST = {torch.float32: 2.0 ** -150, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}
+
+
+def activate(y, name):
+    if name == "none":
+        return y
+    if name == "relu":
+        return torch.where(y < 0, torch.zeros_like(y), y)
+    if name == "silu":
+        return y / (1.0 + torch.exp(-y))
+    if name == "gelu":
+        return 0.5 * y * torch.special.erfc(-y * math.sqrt(0.5))
+    return y / (1.0 + torch.exp(-2.0 * math.sqrt(2.0 / math.pi) * (y + 0.044715 * y ** 3)))
+
+
+def codes(x, gain=None, eps=None):
+    """(codes, row scales): the codes by their definition's binary32 steps, the
+    scale in binary64."""
+    v = x.float() if gain is None else x.float() * gain
+    a = v.abs().amax(dim=1) if v.shape[1] else torch.zeros(v.shape[0])
+    live = ~(a < TINY)
+    made = torch.where(live[:, None], torch.round(v * (torch.full_like(a, 127.0) / a)[:, None]), torch.zeros_like(v))
+    scale = a.double() / 127.0
+    if eps is not None:
+        scale = scale / torch.sqrt(x.double().pow(2).mean(dim=1) + float(torch.tensor(eps, dtype=torch.float32))) if x.shape[1] else scale
+    return made.double(), torch.where(live, scale, torch.zeros_like(scale))
+
+
+def projection(x, w, w_scale, gain=None, eps=None, bias=None):
+    """(y, what its products alone are): the projection behind the norm."""
+    c, s = codes(x, gain, eps)
+    y = (c @ w.double().t()) * s[:, None] * w_scale.double()[None]
+    return (y if bias is None else y + bias.double()), y
+
+
+def projection_room(y, product, normed):
+    """How far binary32 may be from y: the sum's rounding, two scales and what
+    multiplies them, the bias, a step each.  Behind a norm the mean of squares: a
+    thread adds up to 80 of a row of 20480 elements at most, wavefronts and blocks
+    a dozen sums more, all of one sign, and the factor is its root: 46 steps; with
+    the root, the quotients and the product under 64."""
+    return product.abs() * ((64 if normed else 0) + 6) * 2.0 ** -24 + y.abs() * 2.0 ** -24
+
+
+def activation_room(y, name, room):
+    """An activation moves by at most 1.13 of its argument's error (the largest
+    slope, of gelu; silu's is 1.1), beside what the header allows it itself."""
+    own = 0.0 if name in ("none", "relu") else 2.0 ** -20 * (1 + y.abs()) * activate(y, name).abs() + 2.0 ** -22 * y.abs()
+    return 1.13 * room + own
+
+
+def stored_room(want, room, dtype):
+    """One rounding to the output's type, of a value that is off by `room`, and of
+    the sums before it one step of binary32."""
+    return room + (want.abs() + room) * (STEP[dtype] + 2.0 ** -23) + SMALLEST[dtype]
+
+
+def project(x, w, w_scale, norm=None, bias=None, act="none", residual=None, dtype=torch.float32):
+    """(result, bound of the error)."""
+    gain, eps = norm if norm else (None, None)
+    y, product = projection(x, w, w_scale, gain, eps, bias)
+    room = activation_room(y, act, projection_room(y, product, norm is not None))
+    want = activate(y, act)
+    if residual is not None:
+        want = want + residual.double()
+        room = room + activate(y, act).abs() * 2.0 ** -24
+    return want, stored_room(want, room, dtype)
+
+
+def gated(x, w, w_scale, norm=None, bias=None, act="silu", dtype=torch.float32):
+    gain, eps = norm if norm else (None, None)
+    y, product = projection(x, w, w_scale, gain, eps, bias)
+    room = projection_room(y, product, norm is not None)
+    N = w.shape[0] // 2
+    g, u = activate(y[:, :N], act), y[:, N:]
+    rg, ru = activation_room(y[:, :N], act, room[:, :N]), room[:, N:]
+    want = g * u
+    return want, stored_room(want, rg * u.abs() + ru * g.abs() + rg * ru, dtype)
