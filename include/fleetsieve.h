@@ -670,6 +670,50 @@ fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const vo
                              int64_t table_width, int32_t max_q, float scale, int32_t window, void *d_out,
                              void *d_workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* A pool of states, the past of a head whose attention keeps one matrix: head_dim
+ * (64 or 128) rows, a key's elements, of head_dim columns, a value's. */
+typedef struct fs_state_pool {
+  float *s; /* [n_states][n_heads][head_dim][head_dim], from a multiple of 16 bytes on */
+  int32_t n_states, n_heads, head_dim;
+} fs_state_pool;
+
+/* Attention of n_seqs sequences' new tokens over a state that decays with every
+ * token and takes its key and value in:
+ *   S = exp(log_decay[h]) S + k v^T,   out = scale * S^T q,   token by token.
+ *
+ * q [n_tokens][n_q_heads][head_dim], k, v [n_tokens][n_heads][head_dim] with token
+ * strides (heads adjacent), FS_F16 or FS_BF16; n_q_heads is a multiple of n_heads,
+ * query head i reads state head i / (n_q_heads / n_heads).  log_decay [n_heads] is
+ * at most 0 (-infinity: nothing is kept).  The new tokens of sequence s are rows
+ * cu_q[s] .. cu_q[s+1] - 1 as in fs_cache_attention, at most max_q of them; rows
+ * from cu_q[n_seqs] on are not written.  Its state is number state_index[s] of the
+ * pool, updated in place; ctx_lens[s] counts its tokens with the new ones: where
+ * that is no more than the new ones it starts from zeros, whatever the pool holds.
+ * A negative index: it starts from zeros and its state is not kept.  A sequence
+ * without new tokens leaves its state as it is.  No two sequences with new tokens
+ * may have one state.  out: [n_tokens][n_q_heads][head_dim] contiguous, of q's type.
+ *
+ * Sums and states are binary32.  Sequences of up to 8 new tokens go token by token.
+ * Longer ones go in chunks of 64, where states, decayed values and decayed products
+ * of queries and keys enter the products as pairs of bfloat16 values, 16 bits of
+ * each: results are off by about 2^-17 of the sums' terms before they are rounded.
+ * Equal run to run.  What a NaN or an infinity reaches by the formula (its own
+ * token's outputs and later ones, the state) is not finite, and nothing else; a
+ * state beyond 2^127 counts as infinite.
+ *
+ * With FS_VALIDATE=1 lengths, states and decays outside their ranges and states that
+ * two sequences share are refused (the call waits for the stream); otherwise lengths
+ * are clamped as in fs_cache_attention, an index beyond the pool counts as negative,
+ * a positive log_decay as 0. */
+fs_status fs_state_attention_workspace_size(const fs_state_pool *pool, int32_t n_q_heads, int64_t n_tokens,
+                                            int32_t n_seqs, size_t *bytes);
+fs_status fs_state_attention(fs_context *ctx, const fs_state_pool *pool, const void *d_q, int64_t q_stride,
+                             const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride, fs_dtype type,
+                             int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs, const int32_t *d_cu_q,
+                             const int32_t *d_ctx_lens, const int32_t *d_state_index, int32_t max_q,
+                             const float *d_log_decay, float scale, void *d_out, void *d_workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

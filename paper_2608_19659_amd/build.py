@@ -17,7 +17,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfleetsieve.so")
-SOURCES = [os.path.join(CSRC, n) for n in ("fs_kernels.hip", "fs_linear.hip", "fs_project.hip", "fs_cache.hip", "fs_attention.hip",
+SOURCES = [os.path.join(CSRC, n) for n in ("fs_kernels.hip", "fs_linear.hip", "fs_project.hip", "fs_cache.hip", "fs_attention.hip", "fs_state.hip",
                                            "fs_api.cpp", "fs_serving_api.cpp")]
 
 HIP_FLAGS = [
@@ -43,7 +43,7 @@ def build_library(extra_flags=(), out: str = LIB, verbose: bool = False) -> str:
         if verbose:
             for cmd in (*compiles, link):
                 print(" ".join(cmd), file=sys.stderr)
-        with ThreadPoolExecutor(max_workers=4) as pool:
+        with ThreadPoolExecutor(max_workers=8) as pool:
             list(pool.map(lambda cmd: subprocess.run(cmd, check=True, cwd=HERE), compiles))
         subprocess.run(link, check=True, cwd=HERE)
     os.replace(tmp, out)

@@ -100,6 +100,22 @@ bool attention_fits(const AttendArgs &A, int kernel);
 size_t attention_workspace(const Cache &c, int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs);
 hipError_t launch_cache_attention(const AttendArgs &A, int kernel, void *ws, hipStream_t s);
 
+struct StateArgs {
+  float *states;  // [n_states][n_heads][head_dim][head_dim]: keys' elements, then values'
+  const void *q, *k, *v;
+  void *out;
+  const int32_t *cu_q, *ctx_lens, *index;
+  const float *log_decay;
+  float *local;  // workspace
+  int64_t q_stride, k_stride, v_stride;
+  int32_t n_states, n_heads, head_dim, n_q_heads, n_tokens, n_seqs, max_q, type;
+  float scale;
+  int32_t step_most, segment, n_places;  // set by the launcher
+};
+size_t state_workspace(int32_t n_heads, int32_t head_dim, int64_t n_tokens);
+hipError_t launch_state_attention(const StateArgs &A, hipStream_t s);
+hipError_t launch_check_state(const StateArgs &A, int32_t *flag, hipStream_t s);
+
 // FS_VALIDATE=1: counts what is out of range into the validation words
 // (flag_address) of the current device, which the caller cleared.
 hipError_t flag_address(int32_t **flag);

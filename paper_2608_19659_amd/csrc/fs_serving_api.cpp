@@ -451,4 +451,71 @@ fs_status fs_cache_attention(fs_context *ctx, const fs_kv_cache *cache, const vo
   return e == hipSuccess ? FS_OK : hip_fail(e, "attention launch");
 }
 
+static fs_status check_pool(const fs_state_pool *pool, int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs) {
+  if (!pool) return fail(FS_ERR_INVALID_ARGUMENT, "pool is NULL");
+  if (pool->n_states < 0 || pool->n_heads < 1)
+    return fail(FS_ERR_INVALID_ARGUMENT, "the pool's heads must be positive (n_states >= 0)");
+  if (pool->head_dim != 64 && pool->head_dim != 128) return fail(FS_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (pool->n_heads > 4096) return fail(FS_ERR_UNSUPPORTED, "n_heads must be at most 4096");
+  if (n_q_heads < 1 || n_q_heads % pool->n_heads)
+    return fail(FS_ERR_INVALID_ARGUMENT, "n_q_heads must be a positive multiple of the pool's heads");
+  if (n_q_heads > 65536 / 2) return fail(FS_ERR_UNSUPPORTED, "n_q_heads must be at most 32768");
+  if (n_tokens < 0 || n_tokens > kMost || n_tokens * n_q_heads > kMost)
+    return fail(FS_ERR_INVALID_ARGUMENT, "n_tokens * n_q_heads must be in [0, 2^31)");
+  if (n_seqs < 0) return fail(FS_ERR_INVALID_ARGUMENT, "n_seqs must be >= 0");
+  if (n_seqs > FS_MAX_SEQUENCES)
+    return fail(FS_ERR_UNSUPPORTED, "n_seqs must be at most " + std::to_string(FS_MAX_SEQUENCES));
+  return FS_OK;
+}
+
+fs_status fs_state_attention_workspace_size(const fs_state_pool *pool, int32_t n_q_heads, int64_t n_tokens,
+                                            int32_t n_seqs, size_t *bytes) {
+  if (!bytes) return fail(FS_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  const fs_status st = check_pool(pool, n_q_heads, n_tokens, n_seqs);
+  if (st != FS_OK) return st;
+  *bytes = align256(fs::state_workspace(pool->n_heads, pool->head_dim, n_tokens));
+  return FS_OK;
+}
+
+fs_status fs_state_attention(fs_context *ctx, const fs_state_pool *pool, const void *d_q, int64_t q_stride,
+                             const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride, fs_dtype type,
+                             int32_t n_q_heads, int64_t n_tokens, int32_t n_seqs, const int32_t *d_cu_q,
+                             const int32_t *d_ctx_lens, const int32_t *d_state_index, int32_t max_q,
+                             const float *d_log_decay, float scale, void *d_out, void *d_workspace,
+                             size_t workspace_bytes, hipStream_t stream) {
+  if (!ctx) return fail(FS_ERR_INVALID_ARGUMENT, "context is NULL");
+  size_t need = 0;
+  fs_status st = fs_state_attention_workspace_size(pool, n_q_heads, n_tokens, n_seqs, &need);
+  if (st != FS_OK) return st;
+  if (type != FS_F16 && type != FS_BF16) return fail(FS_ERR_UNSUPPORTED, "queries, keys and values must be FS_F16 or FS_BF16");
+  const int64_t width = (int64_t)pool->n_heads * pool->head_dim;
+  if (q_stride < (int64_t)n_q_heads * pool->head_dim || k_stride < width || v_stride < width)
+    return fail(FS_ERR_INVALID_ARGUMENT, "token strides must be at least the rows' lengths");
+  if (max_q < 0) return fail(FS_ERR_INVALID_ARGUMENT, "max_q must be >= 0");
+  if (!std::isfinite(scale)) return fail(FS_ERR_INVALID_ARGUMENT, "scale must be finite");
+  if (n_tokens == 0 || n_seqs == 0 || max_q == 0) return FS_OK;
+  if (!d_q || !d_k || !d_v || !d_cu_q || !d_ctx_lens || !d_state_index || !d_log_decay || !d_out ||
+      (pool->n_states > 0 && !pool->s))
+    return fail(FS_ERR_INVALID_ARGUMENT, "array is NULL");
+  if ((uintptr_t)pool->s & 15) return fail(FS_ERR_INVALID_ARGUMENT, "the pool must start on a multiple of 16 bytes");
+  if (need && !d_workspace) return fail(FS_ERR_INVALID_ARGUMENT, "workspace is NULL");
+  if (workspace_bytes < need)
+    return fail(FS_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(need) + " bytes");
+  if ((uintptr_t)d_workspace & 15) return fail(FS_ERR_INVALID_ARGUMENT, "the workspace must start on a multiple of 16 bytes");
+  DeviceGuard dg(ctx->device);
+  if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
+  const fs::StateArgs A{pool->s,      d_q,          d_k,           d_v,      d_out,          d_cu_q,
+                        d_ctx_lens,   d_state_index, d_log_decay,  (float *)d_workspace,     q_stride,
+                        k_stride,     v_stride,     pool->n_states, pool->n_heads,           pool->head_dim,
+                        n_q_heads,    (int32_t)n_tokens, n_seqs,   max_q,    (int32_t)type,  scale,
+                        0,            0,            0};
+  if (fs::env_validate()) {
+    st = checked([&](int32_t *flag) { return fs::launch_check_state(A, flag, stream); }, stream, "fs_state_attention",
+                 {"sequences with lengths or states out of range", "decays that are not at most 0"});
+    if (st != FS_OK) return st;
+  }
+  const hipError_t e = fs::launch_state_attention(A, stream);
+  return e == hipSuccess ? FS_OK : hip_fail(e, "state attention launch");
+}
+
 }  // extern "C"

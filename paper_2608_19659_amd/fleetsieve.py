@@ -44,7 +44,8 @@ EXPORTED = ("fs_context_create", "fs_context_destroy", "fs_context_set_option", 
             "fs_score_candidates_noalloc", "fs_quantize_rows", "fs_scaled_matmul_workspace_size", "fs_scaled_matmul",
             "fs_linear_workspace_size", "fs_linear", "fs_project_workspace_size", "fs_project",
             "fs_gated_project_workspace_size", "fs_gated_project", "fs_cache_append", "fs_cache_read",
-            "fs_cache_attention_workspace_size", "fs_cache_attention")
+            "fs_cache_attention_workspace_size", "fs_cache_attention", "fs_state_attention_workspace_size",
+            "fs_state_attention")
 POLICY_SCORE, POLICY_ORDER = 0, 1
 CELL_SECONDS = 300.0
 
@@ -132,6 +133,9 @@ def load_library():
     lib.fs_scaled_matmul.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     lib.fs_linear_workspace_size.argtypes = [i64, i64, i64, psz]
     lib.fs_linear.argtypes = [vp, vp, i32, i64, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz, vp]
+    lib.fs_state_attention_workspace_size.argtypes = [vp, i32, i64, i32, psz]
+    lib.fs_state_attention.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, i32, i32, i64, i32, vp, vp, vp, i32, vp,
+                                       ctypes.c_float, vp, vp, sz, vp]
     lib.fs_project_workspace_size.argtypes = lib.fs_gated_project_workspace_size.argtypes = [i64, i64, i64, psz]
     lib.fs_project.argtypes = [vp, vp, i32, i64, vp, vp, i64, vp, vp, i32, vp, i64, i64, i64, i64, vp, i32, i64, vp, sz, vp]
     lib.fs_gated_project.argtypes = [vp, vp, i32, i64, vp, vp, i64, vp, vp, i32, i64, i64, i64, vp, i32, i64, vp, sz, vp]
@@ -1138,3 +1142,54 @@ def cache_attention(ctx: Context, cache: KVCache, q, block_table, ctx_lens, cu_q
                     window: int = 0, out=None, stream=None, workspace=None):
     """fs_cache_attention, one call (see AttentionPlan)."""
     return AttentionPlan(ctx, cache, q, block_table, ctx_lens, cu_q, max_q, scale, window, out, stream, workspace).run()
+
+
+class _StatePool(ctypes.Structure):
+    _fields_ = [("s", ctypes.c_void_p), ("n_states", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class StateAttentionPlan(_Plan):
+    """Attention of packed new tokens over one decaying matrix a head
+    (fs_state_attention).  states float32 [states, heads, head_dim, head_dim] is
+    the pool, updated in place; q [T, query heads, head_dim], k and v [T, heads,
+    head_dim] may be parts of wider rows; state_index int32 [sequences] (negative:
+    starts from zeros, not kept), ctx_lens, cu_q and max_q as in AttentionPlan (a
+    sequence whose ctx_lens is its number of new tokens starts from zeros);
+    log_decay float32 [heads], at most 0.  scale defaults to head_dim ** -0.5."""
+
+    def __init__(self, ctx: Context, states, q, k, v, state_index, ctx_lens, cu_q, max_q: int, log_decay, scale=None,
+                 out=None, stream=None, workspace=None):
+        torch = _torch()
+        if states.dim() != 4:
+            raise _invalid("states must be [states, heads, head_dim, head_dim]")
+        P, H, D = (int(n) for n in states.shape[:3])
+        self._pool = _StatePool(_dev_ptr(states, torch.float32, (P, H, D, D), "states"), P, H, D)
+        pq, sq = _rows(q, (None, None, D), "q")
+        T, heads = int(q.shape[0]), int(q.shape[1])
+        pk, sk = _rows(k, (T, H, D), "k", q.dtype)
+        pv, sv = _rows(v, (T, H, D), "v", q.dtype)
+        S = int(state_index.shape[0])
+        if out is None:
+            out = _empty((T, heads, D), q.dtype, q.device, stream)
+        po = _dev_ptr(out, q.dtype, (T, heads, D), "out")
+        lib = load_library()
+        need = _size(lib.fs_state_attention_workspace_size, ctypes.byref(self._pool), heads, T, S)
+        ws = _workspace(ctx, workspace, need, stream)
+        _same_device(ctx, states=states, q=q, k=k, v=v, state_index=state_index, ctx_lens=ctx_lens, cu_q=cu_q,
+                     log_decay=log_decay, out=out, workspace=ws)
+        self.out, self._keep = out, (states, q, k, v, state_index, ctx_lens, cu_q, log_decay, ws)
+        self._fn = lib.fs_state_attention
+        self._args = (ctx.handle, ctypes.byref(self._pool), pq, sq, pk, sk, pv, sv, _element_type(q.dtype), heads, T, S,
+                      _dev_ptr(cu_q, torch.int32, (S + 1,), "cu_q"), _dev_ptr(ctx_lens, torch.int32, (S,), "ctx_lens"),
+                      _dev_ptr(state_index, torch.int32, (S,), "state_index"), int(max_q),
+                      _dev_ptr(log_decay, torch.float32, (H,), "log_decay"), float(D ** -0.5 if scale is None else scale),
+                      po, _dev_ptr(ws, torch.uint8, None, "workspace"), ws.numel(), _stream(q.device, stream))
+        _keep_for(stream, out, *self._keep)
+
+
+def state_attention(ctx: Context, states, q, k, v, state_index, ctx_lens, cu_q, max_q: int, log_decay, scale=None,
+                    out=None, stream=None, workspace=None):
+    """fs_state_attention, one call (see StateAttentionPlan)."""
+    return StateAttentionPlan(ctx, states, q, k, v, state_index, ctx_lens, cu_q, max_q, log_decay, scale, out, stream,
+                              workspace).run()

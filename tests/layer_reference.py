@@ -85,3 +85,35 @@ def gated(x, w, w_scale, norm=None, bias=None, act="silu", dtype=torch.float32):
     rg, ru = activation_room(y[:, :N], act, room[:, :N]), room[:, N:]
     want = g * u
     return want, stored_room(want, rg * u.abs() + ru * g.abs() + rg * ru, dtype)
+
+
+# ------------------------------------------------------------ state attention --
+def state_attend(q, k, v, state, log_decay, scale):
+    """(outputs, state, bound of the outputs' errors, bound of the state's), token
+    by token in binary64.  q [n, heads, D], k, v [n, state heads, D], state
+    [state heads, D, D], log_decay [state heads].
+
+    The bounds: every decayed product of a key and a value enters the state with
+    2^-17 of itself lost where it is held as two bfloat16 values (2^-9 of the first's
+    rounding, 2^-9 of that of the rest, half a step each); its decay is 2 to a power
+    below 128 where anything is left, which is off by 2^-24 of itself: 2^-17 again;
+    and each of up to n additions and decays rounds by 2^-24 of the sum of the terms'
+    sizes: as long as that sum's own decay counts fewer than n of them.  An output multiplies that by a query and adds the roundings of the
+    state (again 2^-17), of the decayed products of queries and keys (2^-17, and 2^-17
+    for their decay), and of its own sum."""
+    n, heads, D = q.shape
+    H = k.shape[1]
+    group = heads // H
+    lam = torch.exp(log_decay.double())[:, None, None]
+    S, size = state.double().clone(), state.double().abs().clone()
+    out = torch.zeros(n, heads, D, dtype=torch.float64)
+    most = torch.zeros_like(out)
+    for t in range(n):
+        kv = k[t].double()[:, :, None] * v[t].double()[:, None, :]
+        S, size = lam * S + kv, lam * size + kv.abs()
+        x = q[t].double().view(H, group, D)
+        out[t] = scale * torch.bmm(x, S).reshape(heads, D)
+        most[t] = abs(scale) * torch.bmm(x.abs(), size).reshape(heads, D)
+    held = 1.0 / max(1e-9, 1.0 - float(lam.max()))  # tokens that count: the sum of a term's decays
+    steps = 2 * 2.0 ** -17 + 2.0 ** -24 * (min(n, held) + D)
+    return out, S, most * (steps + 3 * 2.0 ** -17), size * steps
