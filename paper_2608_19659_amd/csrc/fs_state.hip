@@ -19,7 +19,7 @@
 namespace fs {
 namespace {
 
-constexpr int kChunk = 64, kThreads = 256;
+constexpr int kChunk = 64, kThreads = 256;  // kThreads: of a block that goes token by token, or joins
 
 // Powers of l by exp2 of multiples of its logarithm, which is at least -10^4 here
 // so that 0 times it is 0 where l is 0 (log_decay -infinity).  Positive ones count
@@ -29,6 +29,12 @@ __device__ __forceinline__ float log2_decay(const StateArgs &A, int h) {
   return x > 0.0f ? 0.0f : x < -1e4f ? -1e4f : x;
 }
 __device__ __forceinline__ float power(float l2, int n) { return __builtin_amdgcn_exp2f(l2 * (float)n); }
+
+// The same to the last bit: what a state is multiplied by once for many tokens.
+__device__ __forceinline__ float exact_power(const StateArgs &A, int h, int n) {
+  const float x = A.log_decay[h];
+  return (float)exp((x > 0.0f ? 0.0 : (double)x) * n);
+}
 
 struct Sequence {
   int first, count, state;  // state -1: none is read or kept
@@ -48,10 +54,97 @@ __device__ __forceinline__ Sequence sequence(const StateArgs &A, int s) {
   return q;
 }
 
+// ------------------------------------------------------------------- segments --
+// Segments of `segment` tokens (a multiple of 64), numbered over the sequences;
+// sequences of at most step_most tokens have none.
+__device__ __forceinline__ int segments(const StateArgs &A, int s) {
+  int first;
+  const int n = s < A.n_seqs ? count_of(A, s, &first) : 0;
+  return n > A.step_most ? (n - 1) / A.segment + 1 : 0;
+}
+// A sequence of two segments or more has a place in the workspace for each.
+__device__ __forceinline__ int places(const StateArgs &A, int s) {
+  const int n = segments(A, s);
+  return n > 1 ? n : 0;
+}
+// Places of the sequences before `s` (all of a wavefront's lanes call it).
+__device__ __forceinline__ int places_before(const StateArgs &A, int s) {
+  int sum = 0;
+  for (int i = threadIdx.x & 63; i < s; i += 64) sum += places(A, i);
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  return sum;
+}
+// (Sequences that overlap, which the call does not allow, may have more segments
+// than there are places: those are left out.)
+__device__ __forceinline__ bool room_for(const StateArgs &A, int before, int n) { return (int64_t)before + n <= A.n_places; }
+
+__device__ __forceinline__ int sum_upto(int v, int lane) {
+  for (int o = 1; o < 64; o <<= 1) {
+    const int below = __shfl_up(v, o);
+    if (lane >= o) v += below;
+  }
+  return v;
+}
+struct Segment {
+  int sequence, number, before;  // -1: there is none; its number in the sequence; places before the sequence's
+};
+__device__ __forceinline__ Segment find_segment(const StateArgs &A, int x) {
+  if (A.segment >= A.max_q) return {x, 0, 0};  // a segment a sequence
+  const int lane = threadIdx.x & 63;
+  int before = 0, taken = 0;
+  for (int s0 = 0; s0 < A.n_seqs; s0 += 64) {
+    const int n = segments(A, s0 + lane), m = n > 1 ? n : 0, upto = sum_upto(n, lane), took = sum_upto(m, lane);
+    const uint64_t in = __ballot(x < before + upto);
+    if (in) {
+      const int at = __builtin_ctzll(in), first = taken + __shfl(took - m, at);
+      if (!room_for(A, first, __shfl(m, at))) break;
+      return {s0 + at, x - before - __shfl(upto - n, at), first};
+    }
+    before += __shfl(upto, 63);
+    taken += __shfl(took, 63);
+  }
+  return {-1, 0, 0};
+}
+
 // ------------------------------------------------------------- token by token --
 // A block has COLS columns of a head's state, a thread HELD pieces of four in
-// rows ROWS apart.
+// rows ROWS apart.  Sequences in segments, whose own sums are there by then, are
+// joined in the same launch.
 constexpr int kStepHeads = 8;  // query heads at a time
+
+// A sequence's segments in order: local[j] becomes the state after segment j, and
+// the place of the last, which made no sum, takes the state that the sequence
+// starts from (its own may be written by the last segment while the first reads).
+template <int D>
+__device__ __forceinline__ void join_segments(const StateArgs &A, int sequence_at, int h, int part, int parts) {
+  constexpr int PIECES = D * D / 4 / kThreads, AHEAD = 4;
+  const int n = segments(A, sequence_at);
+  if (n < 2) return;
+  const int before = places_before(A, sequence_at);
+  if (!room_for(A, before, n)) return;
+  const Sequence q = sequence(A, sequence_at);
+  const int64_t D2 = (int64_t)D * D, step = A.n_heads * D2;
+  const float kept = exact_power(A, h, A.segment);
+  for (int piece = part; piece < PIECES; piece += parts) {
+    const int64_t at = (piece * kThreads + threadIdx.x) * 4;
+    float *const p = A.local + ((int64_t)before * A.n_heads + h) * D2 + at;
+    float4v s = {0, 0, 0, 0};
+    if (!q.fresh) s = *(const float4v *)(A.states + ((int64_t)q.state * A.n_heads + h) * D2 + at);
+    *(float4v *)(p + (n - 1) * step) = s;
+    for (int j = 0; j + 1 < n; j += AHEAD) {
+      float4v own[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) own[i] = *(const float4v *)(p + min(j + i, n - 2) * step);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (j + i > n - 2) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(kept, s[e], own[i][e]);
+        *(float4v *)(p + (j + i) * step) = s;
+      }
+    }
+  }
+}
 
 template <int TYPE, int D, int COLS>
 __global__ __launch_bounds__(kThreads) void k_state_step(StateArgs A) {
@@ -61,7 +154,11 @@ __global__ __launch_bounds__(kThreads) void k_state_step(StateArgs A) {
   const int part = blockIdx.x % PARTS, h = blockIdx.x / PARTS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int group = A.n_q_heads / A.n_heads, row = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
   const Sequence q = sequence(A, blockIdx.y);
-  if (q.count < 1 || q.count > A.step_most) return;
+  if (q.count > A.step_most) {
+    if (A.segment < A.max_q) join_segments<D>(A, blockIdx.y, h, part, PARTS);
+    return;
+  }
+  if (q.count < 1) return;
   const float l = power(log2_decay(A, h), 1);
   float *const at = q.state < 0 ? nullptr : A.states + ((int64_t)q.state * A.n_heads + h) * D * D + part * COLS + col;
   float4v s[HELD];
@@ -117,184 +214,173 @@ __global__ __launch_bounds__(kThreads) void k_state_step(StateArgs A) {
 }
 
 // ------------------------------------------------------------------ in chunks --
-// Segments of `segment` tokens (a multiple of 64), numbered over the sequences;
-// sequences of at most step_most tokens have none.
-__device__ __forceinline__ int segments(const StateArgs &A, int s) {
-  int first;
-  const int n = s < A.n_seqs ? count_of(A, s, &first) : 0;
-  return n > A.step_most ? (n - 1) / A.segment + 1 : 0;
-}
-// A sequence of two segments or more has a place in the workspace for each.
-__device__ __forceinline__ int places(const StateArgs &A, int s) {
-  const int n = segments(A, s);
-  return n > 1 ? n : 0;
-}
-// Places of the sequences before `s` (all of a wavefront's lanes call it).
-__device__ __forceinline__ int places_before(const StateArgs &A, int s) {
-  int sum = 0;
-  for (int i = threadIdx.x & 63; i < s; i += 64) sum += places(A, i);
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  return sum;
-}
-// (Sequences that overlap, which the call does not allow, may have more segments
-// than there are places: those are left out.)
-__device__ __forceinline__ bool room_for(const StateArgs &A, int before, int n) { return (int64_t)before + n <= A.n_places; }
-
-__device__ __forceinline__ int sum_upto(int v, int lane) {
-  for (int o = 1; o < 64; o <<= 1) {
-    const int below = __shfl_up(v, o);
-    if (lane >= o) v += below;
-  }
-  return v;
-}
-struct Segment {
-  int sequence, number, before;  // -1: there is none; its number in the sequence; places before the sequence's
-};
-__device__ __forceinline__ Segment find_segment(const StateArgs &A, int x) {
-  if (A.segment >= A.max_q) return {x, 0, 0};  // a segment a sequence
-  const int lane = threadIdx.x & 63;
-  int before = 0, taken = 0;
-  for (int s0 = 0; s0 < A.n_seqs; s0 += 64) {
-    const int n = segments(A, s0 + lane), m = n > 1 ? n : 0, upto = sum_upto(n, lane), took = sum_upto(m, lane);
-    const uint64_t in = __ballot(x < before + upto);
-    if (in) {
-      const int at = __builtin_ctzll(in), first = taken + __shfl(took - m, at);
-      if (!room_for(A, first, __shfl(m, at))) break;
-      return {s0 + at, x - before - __shfl(upto - n, at), first};
-    }
-    before += __shfl(upto, 63);
-    taken += __shfl(took, 63);
-  }
-  return {-1, 0, 0};
-}
-
+using half8v = _Float16 __attribute__((ext_vector_type(8)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using short4v = short __attribute__((ext_vector_type(4)));
 using short8v = short __attribute__((ext_vector_type(8)));
-using int2v = int __attribute__((ext_vector_type(2)));
 
+template <int TYPE>
 __device__ __forceinline__ float4v multiply(short8v a, short8v b, float4v c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  if constexpr (TYPE == kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// A binary32 value as the sum of two bfloat16 values: 16 bits of it.  With one
-// alone the states, which are binary32, would be off by 2^-9 of a token's share, and
-// an output by as much again as its own rounding.
-struct Pair {
-  short8v hi, lo;
-};
-__device__ __forceinline__ void split(float x, short &hi, short &lo) {
-  const uint16_t h = bf16_bits(x);
-  hi = (short)h;
-  lo = (short)bf16_bits(x - bf16_value(h));
-}
+// Binary32 values enter a product as sums of PARTS values of its 16-bit type: what
+// one alone loses (2^-9 of a value in bfloat16) an output would be off by as much
+// again as by its own rounding, and a state, which is binary32, by far more.
+// binary16 has no room for any binary32 value, so the values of a row or column of
+// the operand are multiplied by a power of two that brings their largest to 2^14,
+// and the result by its inverse (exactly); what is below 2^-39 of the largest is lost.
+template <int TYPE, int COUNT, int PARTS>
+struct Parts {
+  short8v part[COUNT][PARTS];
 
-// Tiles of 64 rows in LDS as bfloat16, rows 32 bytes longer than they are, so that
-// eight rows' same columns lie on all banks.  binary16 elements are the sums of two
-// bfloat16 values (exactly): SPLITS tiles then.
-template <int TYPE, int D>
-struct Tile {
-  static constexpr int SPLITS = TYPE == kF16 ? 2 : 1, PITCH = D + 16, SIZE = kChunk * PITCH;
-  static constexpr int PIECES = kChunk * D / 8 / kThreads, PER_ROW = D / 8, STEP = kThreads / PER_ROW;
-
-  // 16 bytes a piece of rows [0, count) from `from` on, zeros behind them.
-  __device__ static __forceinline__ void load(const void *from, int64_t stride, int count, bool whole, int4v (&raw)[PIECES]) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int r = threadIdx.x / PER_ROW + i * STEP;
-      const uint16_t *const p = (const uint16_t *)from + r * stride + threadIdx.x % PER_ROW * 8;
-      raw[i] = r >= count ? int4v{0, 0, 0, 0} : whole ? *(const int4v *)p : load16(p);
+  // `most`: bits of the largest magnitude of all that is multiplied by one factor.
+  __device__ __forceinline__ float set(const float (&x)[COUNT][8], uint32_t most) {
+    float factor = 1.0f, inverse = 1.0f;
+    if constexpr (TYPE == kF16) {
+      const uint32_t exponent = max(most >> 23, 15u);  // at most 255
+      factor = __uint_as_float((268 - exponent) << 23);
+      inverse = __uint_as_float((exponent - 14) << 23);
     }
+#pragma unroll
+    for (int t = 0; t < COUNT; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float rest = TYPE == kF16 ? x[t][e] * factor : x[t][e];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          const uint16_t bits = bits16<TYPE>(rest);
+          part[t][p][e] = (short)bits;
+          if (p + 1 < PARTS) rest -= value16<TYPE>(bits);
+        }
+      }
+    return inverse;
   }
-  __device__ static __forceinline__ void store(short *tile, const int4v (&raw)[PIECES]) {
+};
+
+// The largest of lanes that differ in their upper two bits.
+__device__ __forceinline__ uint32_t most_of_four(uint32_t x) {
+  x = max(x, (uint32_t)__shfl_xor((int)x, 16));
+  return max(x, (uint32_t)__shfl_xor((int)x, 32));
+}
+template <int TYPE, int COUNT>
+__device__ __forceinline__ uint32_t largest(const float (&x)[COUNT][8]) {
+  if constexpr (TYPE != kF16) return 0;
+  uint32_t most = 0;
+#pragma unroll
+  for (int t = 0; t < COUNT; ++t)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[t][e]) & 0x7fffffffu);
+  return most_of_four(most);
+}
+
+// 16 bytes a lane from base + offset to LDS: the wavefront's 1024 bytes from `to`
+// on, in lane order.  The compiler does not know of the load: arrive() waits.
+__device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory", "m0");
+}
+// Waits until at most LEFT of this wavefront's loads and stores are under way and
+// its LDS accesses are done, then for the block's other wavefronts.
+template <int LEFT>
+__device__ __forceinline__ void arrive() {
+  static_assert(LEFT < 16 || LEFT == 63, "a count, or all");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// A wavefront for 16 of the values' columns.  Tiles of 64 tokens' rows lie in LDS as
+// they are in memory but for the order of a row's pieces of 16 bytes: piece c of
+// row r at place c ^ turn(r), so that 16 rows' same pieces lie on all banks.
+// SUMS: a segment's own sum to `local`, no outputs.  DIRECT: rows that start on
+// multiples of 16 bytes go to LDS without registers, a step ahead.
+template <int TYPE_, int D_, bool SUMS_, bool DIRECT_>
+struct ChunkShape {
+  static constexpr int TYPE = TYPE_, D = D_, WAVES = D / 16, THREADS = 64 * WAVES, PIECES = kChunk * D / 8 / THREADS;
+  static constexpr bool SUMS = SUMS_, DIRECT = DIRECT_;
+  static constexpr int TILE = kChunk * D;                       // 16-bit words
+  static constexpr int PRODUCTS = SUMS ? 0 : 2 * 4 * 2 * 512;   // of queries and keys, as operands in two parts
+  static constexpr int BYTES = ((SUMS ? 4 : 6) * TILE + PRODUCTS) * 2 + (SUMS ? 0 : 512);
+
+  __device__ static __forceinline__ int turn(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+
+  // Rows [0, count) of 64 to a tile, the last one in the place of those behind it.
+  __device__ static __forceinline__ void fetch(const void *from, int64_t stride, int count, short *tile) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      short *const to = tile + (threadIdx.x / PER_ROW + i * STEP) * PITCH + threadIdx.x % PER_ROW * 8;
-      if constexpr (TYPE == kBF16) {
-        *(int4v *)to = raw[i];
+      const int piece = i * THREADS + threadIdx.x, r = piece / (D / 8), c = piece % (D / 8) ^ turn(r);
+      if constexpr (DIRECT) {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        load_to_lds((const uint8_t *)from, (uint32_t)min(r, count - 1) * (uint32_t)(stride * 2) + c * 16,
+                    (uint32_t)(size_t)(__attribute__((address_space(3))) short *)tile + i * THREADS * 16 + wave * 1024);
       } else {
-        Pair p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          short hi, lo;
-          split(f16_value((uint16_t)(raw[i][e >> 1] >> 16 * (e & 1))), hi, lo);
-          p.hi[e] = hi;
-          p.lo[e] = lo;
-        }
-        *(short8v *)to = p.hi;
-        *(short8v *)(to + SIZE) = p.lo;
+        *(int4v *)(tile + piece * 8) = load16((const uint16_t *)from + min(r, count - 1) * stride + c * 8);
       }
     }
-  }
-  __device__ static __forceinline__ bool finite(const int4v (&raw)[PIECES]) {
-    using short2 = uint16_t __attribute__((ext_vector_type(2)));
-    short2 most = {0, 0};
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(short2, raw[i][e] & 0x7fff7fff));
-    return max(most.x, most.y) < (TYPE == kF16 ? 0x7c00 : 0x7f80);
   }
   // An operand: a lane has row r0 + lane % 16 and columns c + 4 g .. and
   // c + 16 + 4 g .., g = lane / 16: the order in which a product's results lie.
   __device__ static __forceinline__ short8v rows(const short *tile, int r0, int c) {
-    const int lane = threadIdx.x & 63;
-    const short *const p = tile + (r0 + (lane & 15)) * PITCH + c + (lane >> 4) * 4;
-    const short4v a = *(const short4v *)p, b = *(const short4v *)(p + 16);
+    const int r = r0 + (threadIdx.x & 15), at = c + (threadIdx.x >> 4 & 3) * 4;
+    const short4v a = *(const short4v *)(tile + r * D + ((at >> 3) ^ turn(r)) * 8 + (at & 7));
+    const short4v b = *(const short4v *)(tile + r * D + (((at + 16) >> 3) ^ turn(r)) * 8 + (at & 7));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
   // The transpose: a lane has column c + lane % 16 and rows r0 + 4 g .., r0 + 16 + 4 g ..
   __device__ static __forceinline__ short8v columns(const short *tile, int r0, int c) {
     using Place = __attribute__((address_space(3))) short4v;
-    const int lane = threadIdx.x & 63, r = lane & 15;
-    Place *const p = (Place *)(tile + (r0 + (lane >> 4) * 4 + (r >> 2)) * PITCH + c + (r & 3) * 4);
-    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
-    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place *)((__attribute__((address_space(3))) short *)p + 16 * PITCH));
+    const int l = threadIdx.x & 15, r = r0 + (threadIdx.x >> 4 & 3) * 4 + (l >> 2), at = c + (l & 3) * 4;
+    const auto place = [&](int row) { return (Place *)(tile + row * D + ((at >> 3) ^ turn(row)) * 8 + (at & 7)); };
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(place(r)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(place(r + 16));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
-
-// The token of an operand's element e in step t, in the results' order (see rows).
+// The token of an operand's element e in step t, in that order.
 __device__ __forceinline__ constexpr int token(int t, int e, int g) { return t * 32 + (e >> 2) * 16 + 4 * g + (e & 3); }
 
-// Four wavefronts, each with D / 4 of the values' columns.
-// SUMS: a segment's own sum to `local`, no outputs.
-template <int TYPE, int D, bool SUMS>
-struct ChunkShape {
-  using T = Tile<TYPE, D>;
-  static constexpr int PART = T::SPLITS * T::SIZE;         // a tensor's tiles, in 16-bit words
-  static constexpr int PROBS = SUMS ? 0 : 2 * 4 * 2 * 512;  // probabilities, as operands
-  static constexpr int BYTES = ((SUMS ? 2 : 3) * PART + PROBS) * 2 + 16;
-};
-
-template <int TYPE, int D, bool SUMS>
-__global__ __launch_bounds__(kThreads) void k_state_chunk(StateArgs A) {
-  using Shape = ChunkShape<TYPE, D, SUMS>;
-  using T = Tile<TYPE, D>;
-  constexpr int VT = D / 64, KT = D / 16, KS = D / 32, SPLITS = T::SPLITS;  // a wavefront's column tiles; row tiles, steps
-  extern __shared__ __attribute__((aligned(16))) short state_lds[];
-  short *const lk = state_lds, *const lv = lk + Shape::PART, *const lq = lv + Shape::PART, *const lp = lq + Shape::PART;
-  int *const bad = (int *)((char *)state_lds + Shape::BYTES - 16);  // values that are no numbers, of this chunk and the next
-  const Segment seg = find_segment(A, blockIdx.x);
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
+  constexpr int TYPE = S::TYPE, D = S::D, KT = D / 16, KS = D / 32;  // tiles and steps of a key's elements
+  constexpr int HALVES = S::WAVES / 4, TASKS = 2 / HALVES;           // wavefronts to 16 query rows, pairs of key tiles to one
+  constexpr int PARTS = TYPE == kF16 ? 2 : 3;                        // of a decayed value: 22 or 24 bits, as the states have
+  constexpr uint16_t INFINITE = TYPE == kF16 ? 0x7c00 : 0x7f80;
+  extern __shared__ __attribute__((aligned(1024))) short state_lds[];
+  short *const lk = state_lds, *const lv = lk + 2 * S::TILE, *const lq = lv + 2 * S::TILE, *const lp = lq + 2 * S::TILE;
+  float *const undo = (float *)(lp + S::PRODUCTS);  // of a row of products, what undoes its factor
+  Segment seg = find_segment(A, blockIdx.x);
+  seg.sequence = __builtin_amdgcn_readfirstlane(seg.sequence);  // so that the compiler knows them for the block's
+  seg.number = __builtin_amdgcn_readfirstlane(seg.number);
+  seg.before = __builtin_amdgcn_readfirstlane(seg.before);
   if (seg.sequence < 0) return;
   const Sequence q = sequence(A, seg.sequence);
   if (q.count <= A.step_most) return;
   const int start = seg.number * A.segment, tokens = min(A.segment, q.count - start), h = blockIdx.y;
-  const int group = A.n_q_heads / A.n_heads, lane = threadIdx.x & 63, g = lane >> 4;
+  const int group = A.n_q_heads / A.n_heads, lane = threadIdx.x & 63, g = lane >> 4, own = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool last = start + tokens == q.count;
-  if (SUMS && last) return;
-  const int64_t D2 = (int64_t)D * D;
+  if (S::SUMS && last) return;
+  const int64_t D2 = (int64_t)D * D, row0 = q.first + start;
   float *const local = A.local + ((int64_t)(seg.before + seg.number) * A.n_heads + h) * D2;
-  const float l2 = log2_decay(A, h);
-  const int dv0 = wave * (D / 4);
+  const int dv0 = wave * 16, mine_i = wave / HALVES, mine_t = wave % HALVES * TASKS;
 
-  // s[a][b]: rows 16 a + 4 g .. of column dv0 + 16 b + lane % 16
-  float4v s[KT][VT] = {};
-  const auto place = [&](int a, int b, int e) { return (16 * a + 4 * g + e) * D + dv0 + 16 * b + (lane & 15); };
-  if constexpr (!SUMS) {
+  const auto fetch_kv = [&](int c, int buf) {
+    S::fetch((const uint16_t *)A.k + (row0 + c) * A.k_stride + h * D, A.k_stride, tokens - c, lk + buf * S::TILE);
+    S::fetch((const uint16_t *)A.v + (row0 + c) * A.v_stride + h * D, A.v_stride, tokens - c, lv + buf * S::TILE);
+  };
+  const auto fetch_q = [&](int c, int head, int buf) {
+    S::fetch((const uint16_t *)A.q + (row0 + c) * A.q_stride + ((int64_t)h * group + head) * D, A.q_stride, tokens - c, lq + buf * S::TILE);
+  };
+  fetch_kv(0, 0);
+  if constexpr (!S::SUMS) fetch_q(0, 0, 0);
+
+  // s[a]: rows 16 a + 4 g .. of column dv0 + lane % 16
+  float4v s[KT] = {};
+  const auto place = [&](int a, int e) { return (16 * a + 4 * g + e) * D + dv0 + own; };
+  if constexpr (!S::SUMS) {
     const float *from = nullptr;
-    // the segments' starts as k_state_join leaves them
+    // the segments' starts as k_state_step leaves them
     if (seg.number) from = local - (int64_t)A.n_heads * D2;
     else if (!q.fresh) from = last ? A.states + ((int64_t)q.state * A.n_heads + h) * D2
                                    : A.local + ((int64_t)(seg.before + (q.count - 1) / A.segment) * A.n_heads + h) * D2;
@@ -302,267 +388,204 @@ __global__ __launch_bounds__(kThreads) void k_state_chunk(StateArgs A) {
 #pragma unroll
       for (int a = 0; a < KT; ++a)
 #pragma unroll
-        for (int b = 0; b < VT; ++b)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[a][b][e] = from[place(a, b, e)];
+        for (int e = 0; e < 4; ++e) s[a][e] = from[place(a, e)];
   }
-
-  const int64_t row0 = q.first + start;
-  const auto aligned = [](const void *p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)(stride * 2)) & 15) == 0; };
-  const bool whole_k = aligned(A.k, A.k_stride), whole_v = aligned(A.v, A.v_stride), whole_q = aligned(A.q, A.q_stride);
-  int4v rk[T::PIECES], rv[T::PIECES], rq[T::PIECES];
-  const auto ask_kv = [&](int c) {
-    const int64_t row = row0 + c;
-    T::load((const uint16_t *)A.k + row * A.k_stride + h * D, A.k_stride, tokens - c, whole_k, rk);
-    T::load((const uint16_t *)A.v + row * A.v_stride + h * D, A.v_stride, tokens - c, whole_v, rv);
-  };
-  const auto ask_q = [&](int c, int head) {
-    T::load((const uint16_t *)A.q + (row0 + c) * A.q_stride + ((int64_t)h * group + head) * D, A.q_stride, tokens - c, whole_q, rq);
-  };
-  ask_kv(0);
-  if constexpr (!SUMS) ask_q(0, 0);
-  if (threadIdx.x < 2) bad[threadIdx.x] = 0;
-
+  const float l2 = log2_decay(A, h), chunk_kept = exact_power(A, h, kChunk);
   // the decay between a token of this wavefront's rows and one before it
-  float fade[4][4], seen[4];
-  if constexpr (!SUMS) {
+  float fade[2 * TASKS][4], row_decay = 0.0f;
+  if constexpr (!S::SUMS) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2 * TASKS; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) fade[j][e] = A.scale * power(l2, max(0, (wave - j) * 16 + (lane & 15) - 4 * g - e));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) seen[i] = A.scale * power(l2, i * 16 + (lane & 15) + 1);
+      for (int e = 0; e < 4; ++e) fade[j][e] = A.scale * power(l2, max(0, (mine_i - 2 * mine_t - j) * 16 + own - 4 * g - e));
+    row_decay = A.scale * power(l2, own + 1);
   }
 
-  for (int c = 0, turn = 0; c < tokens; c += kChunk, turn ^= 1) {
+  arrive<0>();
+  for (int c = 0, buf = 0, step = 0; c < tokens; c += kChunk, buf ^= 1) {
     const int n = min(kChunk, tokens - c);
-    __syncthreads();  // the last chunk's tiles are read
-    T::store(lk, rk);
-    T::store(lv, rv);
-    if (!SUMS && !T::finite(rv)) bad[turn] = 1;
-    if constexpr (!SUMS) T::store(lq, rq);
-    if (c + kChunk < tokens) ask_kv(c + kChunk);
-    __syncthreads();
-    short8v v[VT][2][SPLITS];
+    const short *const k = lk + buf * S::TILE;
+    const bool more = c + kChunk < tokens;
+    if (c) arrive<S::SUMS ? 0 : 4>();  // behind the loads of this chunk the four stores of the last full one
+    if (more) fetch_kv(c + kChunk, buf ^ 1);
+    short8v v[2];
 #pragma unroll
-    for (int b = 0; b < VT; ++b)
+    for (int t = 0; t < 2; ++t) v[t] = S::columns(lv + buf * S::TILE, t * 32, dv0);
+    // the first token whose value in this lane's column is no number
+    int none = kChunk;
+    {
+      using short2 = uint16_t __attribute__((ext_vector_type(2)));
+      short2 most = {0, 0};
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const int4v raw = __builtin_bit_cast(int4v, v[t]);
 #pragma unroll
-        for (int x = 0; x < SPLITS; ++x) v[b][t][x] = T::columns(lv + x * T::SIZE, t * 32, dv0 + b * 16);
-    const bool numbers = SUMS || bad[turn] == 0;
-    int none[VT];  // of each column the first token whose value is no number
-    if (!numbers) {
-      // Tokens before it have a weight of 0 for it, which times it is no number: the
-      // products take 0 in its place, and what sees it is made no number behind them.
-#pragma unroll
-      for (int b = 0; b < VT; ++b) {
-        none[b] = kChunk;
+        for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(short2, raw[e] & 0x7fff7fff));
+      }
+      if (__any(max(most.x, most.y) >= INFINITE)) {
+        // Tokens before it have a weight of 0 for it, which times it is no number: the
+        // products take 0 in its place, and what sees it is made no number behind them.
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if ((v[b][t][0][e] & 0x7f80) == 0x7f80) {
-              none[b] = min(none[b], token(t, e, g));
-#pragma unroll
-              for (int x = 0; x < SPLITS; ++x) v[b][t][x][e] = 0;
+            if (((uint16_t)v[t][e] & INFINITE) == INFINITE) {
+              none = min(none, token(t, e, g));
+              v[t][e] = 0;
             }
-        for (int o = 16; o < 64; o <<= 1) none[b] = min(none[b], __shfl_xor(none[b], o));
+        for (int o = 16; o < 64; o <<= 1) none = min(none, __shfl_xor(none, o));
       }
     }
-    if constexpr (!SUMS) {
-      Pair past[VT][KS];  // the state as an operand: its results' order is the operands'
-#pragma unroll
-      for (int b = 0; b < VT; ++b)
+    const bool numbers = !__any(none < kChunk);
+
+    if constexpr (!S::SUMS) {
+      // the state as an operand: its results' order is the operands'
+      Parts<TYPE, KS, 2> past;
+      float past_undo[4];
+      {
+        float x[KS][8];
 #pragma unroll
         for (int t = 0; t < KS; ++t)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            short hi, lo;
-            split(s[2 * t + (e >> 2)][b][e & 3], hi, lo);
-            past[b][t].hi[e] = hi;
-            past[b][t].lo[e] = lo;
-          }
-      for (int head = 0; head < group; ++head) {
+          for (int e = 0; e < 8; ++e) x[t][e] = s[2 * t + (e >> 2)][e & 3];
+        const float inverse = past.set(x, largest<TYPE, KS>(x));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) past_undo[e] = TYPE == kF16 ? __shfl(inverse, 4 * g + e) : 1.0f;
+      }
+      for (int head = 0; head < group; ++head, ++step) {
         if (head) {
-          __syncthreads();
-          T::store(lq, rq);
-          __syncthreads();
+          if (n == kChunk) arrive<4>();
+          else arrive<0>();
         }
-        if (head + 1 < group) ask_q(c, head + 1);
-        else if (c + kChunk < tokens) ask_q(c + kChunk, 0);
-        // this wavefront's 16 rows of <q, k>, decayed, to LDS as operands
-        {
-          short8v mine[KS][SPLITS];
+        const short *const lq_now = lq + (step & 1) * S::TILE;
+        if (head + 1 < group) fetch_q(c, head + 1, (step + 1) & 1);
+        else if (more) fetch_q(c + kChunk, 0, (step + 1) & 1);
+        // 16 rows of <q, k>, decayed, by pairs of 16 keys, to LDS as operands
+        if (2 * mine_t <= mine_i) {
+          short8v mine[KS];
 #pragma unroll
-          for (int t = 0; t < KS; ++t)
+          for (int t = 0; t < KS; ++t) mine[t] = S::rows(lq_now, mine_i * 16, t * 32);
 #pragma unroll
-            for (int x = 0; x < SPLITS; ++x) mine[t][x] = T::rows(lq + x * T::SIZE, wave * 16, t * 32);
+          for (int task = 0; task < TASKS; ++task) {
+            const int t = mine_t + task;
+            if (2 * t > mine_i) break;
+            float x[1][8] = {};
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            Pair p = {};
-            if (2 * t <= wave) {
+            for (int half = 0; half < 2; ++half) {
+              const int j = 2 * t + half;
+              if (j > mine_i) break;
+              float4v sum = {0, 0, 0, 0};
 #pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const int j = 2 * t + half;
-                if (j > wave) continue;
-                float4v sum = {0, 0, 0, 0};
+              for (int d = 0; d < KS; ++d) sum = multiply<TYPE>(S::rows(k, j * 16, d * 32), mine[d], sum);
 #pragma unroll
-                for (int d = 0; d < KS; ++d) {
-                  const short8v k = T::rows(lk, j * 16, d * 32);
-                  sum = multiply(k, mine[d][0], sum);
-                  if constexpr (SPLITS == 2) {
-                    sum = multiply(k, mine[d][1], sum);
-                    sum = multiply(T::rows(lk + T::SIZE, j * 16, d * 32), mine[d][0], sum);
-                  }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  // later tokens are left out, whatever they are
-                  const float x = j == wave && 4 * g + e > (lane & 15) ? 0.0f : sum[e] * fade[j][e];
-                  short hi, lo;
-                  split(x, hi, lo);
-                  p.hi[half * 4 + e] = hi;
-                  p.lo[half * 4 + e] = lo;
-                }
-              }
-              *(short8v *)(lp + ((wave * 2 + t) * 64 + lane) * 8) = p.hi;
-              *(short8v *)(lp + 4096 + ((wave * 2 + t) * 64 + lane) * 8) = p.lo;
+              for (int e = 0; e < 4; ++e)  // later tokens are left out, whatever they are
+                x[0][half * 4 + e] = j == mine_i && 4 * g + e > own ? 0.0f : sum[e] * fade[task * 2 + half][e];
             }
+            Parts<TYPE, 1, 2> p;
+            const float inverse = p.set(x, largest<TYPE, 1>(x));
+            *(short8v *)(lp + ((mine_i * 2 + t) * 64 + lane) * 8) = p.part[0][0];
+            *(short8v *)(lp + 4096 + ((mine_i * 2 + t) * 64 + lane) * 8) = p.part[0][1];
+            if (TYPE == kF16 && g == 0) undo[(mine_i * 2 + t) * 16 + own] = inverse;
           }
         }
-        __syncthreads();
+        arrive<63>();
+        // two times 16 rows of outputs at once
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i * 16 >= n) break;
-          float4v o[VT] = {};
+        for (int u = 0; u < 2; ++u) {
+          if (u * 32 >= n) break;
+          float4v o[2] = {};
 #pragma unroll
           for (int t = 0; t < KS; ++t) {
-            const short8v x = T::rows(lq, i * 16, t * 32);
+            short8v x[2];
 #pragma unroll
-            for (int b = 0; b < VT; ++b) {
-              o[b] = multiply(past[b][t].hi, x, o[b]);
-              o[b] = multiply(past[b][t].lo, x, o[b]);
-            }
-            if constexpr (SPLITS == 2) {
-              const short8v y = T::rows(lq + T::SIZE, i * 16, t * 32);
+            for (int w = 0; w < 2; ++w) x[w] = S::rows(lq_now, u * 32 + w * 16, t * 32);
 #pragma unroll
-              for (int b = 0; b < VT; ++b) o[b] = multiply(past[b][t].hi, y, o[b]);
-            }
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+              for (int w = 0; w < 2; ++w) o[w] = multiply<TYPE>(past.part[t][p], x[w], o[w]);
           }
 #pragma unroll
-          for (int b = 0; b < VT; ++b)
+          for (int w = 0; w < 2; ++w) {
+            const float seen = row_decay * power(l2, u * 32 + w * 16);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[b][e] *= seen[i];
-#pragma unroll
-          for (int t = 0; t <= i / 2; ++t) {
-            const short8v hi = *(const short8v *)(lp + ((i * 2 + t) * 64 + lane) * 8);
-            const short8v lo = *(const short8v *)(lp + 4096 + ((i * 2 + t) * 64 + lane) * 8);
-#pragma unroll
-            for (int b = 0; b < VT; ++b) {
-              o[b] = multiply(v[b][t][0], hi, o[b]);
-              o[b] = multiply(v[b][t][0], lo, o[b]);
-              if constexpr (SPLITS == 2) o[b] = multiply(v[b][t][1], hi, o[b]);
-            }
+            for (int e = 0; e < 4; ++e) o[w][e] = (TYPE == kF16 ? o[w][e] * past_undo[e] : o[w][e]) * seen;
           }
-          if (!numbers) {
 #pragma unroll
-            for (int b = 0; b < VT; ++b)
+          for (int t = 0; t <= u; ++t)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              const int at = (u * 2 + w) * 2 + t;
+              float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : o[w];
+#pragma unroll
+              for (int p = 0; p < 2; ++p) sum = multiply<TYPE>(v[t], *(const short8v *)(lp + p * 4096 + (at * 64 + lane) * 8), sum);
+              if constexpr (TYPE == kF16) {
+                const float inverse = undo[at * 16 + own];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[w][e] = __builtin_fmaf(sum[e], inverse, o[w][e]);
+              } else {
+                o[w] = sum;
+              }
+            }
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const int row = u * 32 + w * 16 + own;
+            if (!numbers) {
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (i * 16 + (lane & 15) >= __shfl(none[b], 4 * g + e)) o[b][e] = __builtin_nanf("");
-          }
-          const int row = c + i * 16 + (lane & 15);
-          if (row < tokens) {
-#pragma unroll
-            for (int b = 0; b < VT; ++b) {
+                if (row >= __shfl(none, 4 * g + e)) o[w][e] = __builtin_nanf("");
+            }
+            if (row < n) {
               uint16_t bits[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) bits[e] = bits16<TYPE>(o[b][e]);
-              __builtin_memcpy((uint16_t *)A.out + ((row0 + row) * A.n_q_heads + h * group + head) * D + dv0 + b * 16 + 4 * g, bits, 8);
+              for (int e = 0; e < 4; ++e) bits[e] = bits16<TYPE>(o[w][e]);
+              __builtin_memcpy((uint16_t *)A.out + ((row0 + c + row) * A.n_q_heads + h * group + head) * D + dv0 + 4 * g, bits, 8);
             }
           }
         }
       }
-      if (threadIdx.x == 0) bad[turn ^ 1] = 0;
-      if (last && q.state < 0 && c + kChunk >= tokens) return;
+      if (last && q.state < 0 && !more) return;
     }
     // the state after the chunk
-    const float kept = power(l2, n);
-    Pair fading[VT][2];
+    const float kept = n == kChunk ? chunk_kept : exact_power(A, h, n);
+    Parts<TYPE, 2, PARTS> fading;
+    float inverse;
+    {
+      float x[2][8];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float w = power(l2, max(0, n - 1 - token(t, e, g)));
-#pragma unroll
-        for (int b = 0; b < VT; ++b) {
-          float x = bf16_value((uint16_t)v[b][t][0][e]);
-          if constexpr (SPLITS == 2) x += bf16_value((uint16_t)v[b][t][1][e]);
-          if (!numbers && token(t, e, g) == none[b]) x = __builtin_nanf("");
-          short hi, lo;
-          split(x * w, hi, lo);
-          fading[b][t].hi[e] = hi;
-          fading[b][t].lo[e] = lo;
+        for (int e = 0; e < 8; ++e) {
+          const int at = token(t, e, g);
+          x[t][e] = at < n ? value16<TYPE>((uint16_t)v[t][e]) * power(l2, n - 1 - at) : 0.0f;
+          if (at == none) x[t][e] = __builtin_nanf("");
         }
-      }
+      inverse = fading.set(x, largest<TYPE, 2>(x));
+    }
 #pragma unroll
     for (int a = 0; a < KT; ++a) {
-#pragma unroll
-      for (int b = 0; b < VT; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[a][b][e] *= kept;
+      float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : s[a] * kept;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const short8v k = T::columns(lk, t * 32, a * 16);
+        const short8v x = S::columns(k, t * 32, a * 16);
 #pragma unroll
-        for (int b = 0; b < VT; ++b) {
-          s[a][b] = multiply(k, fading[b][t].hi, s[a][b]);
-          s[a][b] = multiply(k, fading[b][t].lo, s[a][b]);
-        }
-        if constexpr (SPLITS == 2) {
-          const short8v y = T::columns(lk + T::SIZE, t * 32, a * 16);
+        for (int p = PARTS - 1; p >= 0; --p) sum = multiply<TYPE>(x, fading.part[t][p], sum);
+      }
+      if constexpr (TYPE == kF16) {
 #pragma unroll
-          for (int b = 0; b < VT; ++b) s[a][b] = multiply(y, fading[b][t].hi, s[a][b]);
-        }
+        for (int e = 0; e < 4; ++e) s[a][e] = __builtin_fmaf(sum[e], inverse, s[a][e] * kept);
+      } else {
+        s[a] = sum;
       }
     }
   }
   float *to = nullptr;
-  if constexpr (SUMS) to = local;
+  if constexpr (S::SUMS) to = local;
   else if (last && q.state >= 0) to = A.states + ((int64_t)q.state * A.n_heads + h) * D2;
   if (to)
 #pragma unroll
     for (int a = 0; a < KT; ++a)
 #pragma unroll
-      for (int b = 0; b < VT; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) to[place(a, b, e)] = s[a][b][e];
-}
-
-// A sequence's segments in order: local[j] becomes the state after segment j, and
-// the place of the last, which made no sum, takes the state that the sequence
-// starts from (its own may be written by the last segment while the first reads).
-template <int D>
-__global__ __launch_bounds__(kThreads) void k_state_join(StateArgs A) {
-  constexpr int PIECES = D * D / 4 / kThreads;
-  const int piece = blockIdx.x % PIECES, h = blockIdx.x / PIECES, n = segments(A, blockIdx.y);
-  if (n < 2) return;
-  const Sequence q = sequence(A, blockIdx.y);
-  const int64_t D2 = (int64_t)D * D, step = A.n_heads * D2, at = (piece * kThreads + threadIdx.x) * 4;
-  const int before = places_before(A, blockIdx.y);
-  if (!room_for(A, before, n)) return;
-  float *p = A.local + ((int64_t)before * A.n_heads + h) * D2 + at;
-  const float kept = power(log2_decay(A, h), A.segment);
-  float4v s = {0, 0, 0, 0};
-  if (!q.fresh) s = *(const float4v *)(A.states + ((int64_t)q.state * A.n_heads + h) * D2 + at);
-  *(float4v *)(p + (n - 1) * step) = s;
-  for (int j = 0; j + 1 < n; ++j, p += step) {
-    const float4v own = *(const float4v *)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(kept, s[e], own[e]);
-    *(float4v *)p = s;
-  }
+      for (int e = 0; e < 4; ++e) to[place(a, e)] = s[a][e];
 }
 
 __global__ void k_check_state(StateArgs A, int32_t *flag) {
@@ -579,11 +602,11 @@ __global__ void k_check_state(StateArgs A, int32_t *flag) {
 // Sequences of up to this many new tokens go token by token.
 constexpr int kStepMost = 8;
 
-// Tokens of a segment: one for each sequence where the heads fill the CUs, else so
-// many that about 512 segments and heads come out.
+// Tokens of a segment, so many that all sequences' tokens make about 256 segments of
+// a head, one for each CU.
 int segment_tokens(int64_t n_tokens, int64_t n_heads) {
-  const int64_t L = (n_tokens * n_heads / 512 + 63) / 64 * 64;
-  return (int)std::max<int64_t>(256, std::min<int64_t>(L, 1 << 30));
+  const int64_t L = (n_tokens * n_heads / 256 + kChunk - 1) / kChunk * kChunk;
+  return (int)std::max<int64_t>(kChunk, std::min<int64_t>(L, 1 << 30));
 }
 int64_t segments_at_most(int64_t n_tokens, int64_t n_seqs, int64_t n_heads) {
   return n_tokens / segment_tokens(n_tokens, n_heads) + n_seqs;
@@ -595,12 +618,21 @@ int64_t places_at_most(int64_t n_tokens, int64_t n_heads) {
   return n_tokens > L ? 2 * n_tokens / L : 0;
 }
 
-template <class K>
-hipError_t launch_chunks(K kernel, int bytes, dim3 grid, const StateArgs &A, hipStream_t s) {
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+template <class S>
+hipError_t chunks_as(dim3 grid, const StateArgs &A, hipStream_t s) {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_state_chunk<S>), hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
   if (e != hipSuccess) return e;
-  kernel<<<grid, kThreads, bytes, s>>>(A);
+  k_state_chunk<S><<<grid, S::THREADS, S::BYTES, s>>>(A);
   return hipGetLastError();
+}
+
+template <int TYPE, int D, bool SUMS>
+hipError_t chunks_of(dim3 grid, const StateArgs &A, hipStream_t s) {
+  // rows that start on multiples of 16 bytes, 64 of them within 32 bits
+  const auto whole = [](const void *p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)(stride * 2)) & 15) == 0 && stride <= 1 << 24; };
+  if (whole(A.k, A.k_stride) && whole(A.v, A.v_stride) && (SUMS || whole(A.q, A.q_stride)))
+    return chunks_as<ChunkShape<TYPE, D, SUMS, true>>(grid, A, s);
+  return chunks_as<ChunkShape<TYPE, D, SUMS, false>>(grid, A, s);
 }
 
 template <int TYPE, int D, int COLS>
@@ -608,29 +640,27 @@ hipError_t steps_as(const StateArgs &A, hipStream_t s) {
   k_state_step<TYPE, D, COLS><<<dim3(A.n_heads * (D / COLS), A.n_seqs), kThreads, 0, s>>>(A);
   return hipGetLastError();
 }
+template <int TYPE, int D>
+hipError_t steps_of(const StateArgs &A, hipStream_t s) {
+  const int64_t heads = (int64_t)A.n_seqs * A.n_heads;
+  if (heads >= 512) return steps_as<TYPE, D, D>(A, s);
+  if (heads >= 128) return steps_as<TYPE, D, 32>(A, s);
+  return steps_as<TYPE, D, 16>(A, s);
+}
 
 template <int TYPE, int D>
 hipError_t state_of(StateArgs A, hipStream_t s) {
-  hipError_t e = hipSuccess;
-  A.step_most = A.max_q > kStepMost && A.n_seqs == 1 ? 0 : kStepMost;
-  if (A.step_most) {
-    const int64_t heads = (int64_t)A.n_seqs * A.n_heads;
-    if (heads >= 512) e = steps_as<TYPE, D, D>(A, s);
-    else if (heads >= 128) e = steps_as<TYPE, D, 32>(A, s);
-    else e = steps_as<TYPE, D, 16>(A, s);
-    if (e != hipSuccess || A.max_q <= kStepMost) return e;
-  }
   A.segment = segment_tokens(A.n_tokens, A.n_heads);
-  if (A.segment >= A.max_q)
-    return launch_chunks(k_state_chunk<TYPE, D, false>, ChunkShape<TYPE, D, false>::BYTES, dim3(A.n_seqs, A.n_heads), A, s);
   A.n_places = (int32_t)places_at_most(A.n_tokens, A.n_heads);
-  const dim3 grid((unsigned)segments_at_most(A.n_tokens, A.n_seqs, A.n_heads), A.n_heads);
-  e = launch_chunks(k_state_chunk<TYPE, D, true>, ChunkShape<TYPE, D, true>::BYTES, grid, A, s);
-  if (e != hipSuccess) return e;
-  k_state_join<D><<<dim3(A.n_heads * (D * D / 4 / kThreads), A.n_seqs), kThreads, 0, s>>>(A);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  return launch_chunks(k_state_chunk<TYPE, D, false>, ChunkShape<TYPE, D, false>::BYTES, grid, A, s);
+  A.step_most = kStepMost;
+  if (A.max_q <= kStepMost) return steps_of<TYPE, D>(A, s);
+  if (A.n_seqs == 1) A.step_most = 0;  // no launch for what may be a single token
+  const bool one = A.segment >= A.max_q;  // a segment a sequence
+  const dim3 grid(one ? (unsigned)A.n_seqs : (unsigned)segments_at_most(A.n_tokens, A.n_seqs, A.n_heads), A.n_heads);
+  hipError_t e = hipSuccess;
+  if (!one) e = chunks_of<TYPE, D, true>(grid, A, s);
+  if (e == hipSuccess && (!one || A.step_most)) e = steps_of<TYPE, D>(A, s);
+  return e == hipSuccess ? chunks_of<TYPE, D, false>(grid, A, s) : e;
 }
 
 }  // namespace
