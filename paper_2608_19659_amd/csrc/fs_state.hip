@@ -117,7 +117,7 @@ constexpr int kStepHeads = 8;  // query heads at a time
 // starts from (its own may be written by the last segment while the first reads).
 template <int D>
 __device__ __forceinline__ void join_segments(const StateArgs &A, int sequence_at, int h, int part, int parts) {
-  constexpr int PIECES = D * D / 4 / kThreads, AHEAD = 4;
+  constexpr int PIECES = D * D / 4 / kThreads, AHEAD = 16;
   const int n = segments(A, sequence_at);
   if (n < 2) return;
   const int before = places_before(A, sequence_at);
@@ -293,7 +293,7 @@ __device__ __forceinline__ void arrive() {
 
 // A wavefront for 16 of the values' columns.  Tiles of 64 tokens' rows lie in LDS as
 // they are in memory but for the order of a row's pieces of 16 bytes: piece c of
-// row r at place c ^ turn(r), so that 16 rows' same pieces lie on all banks.
+// row r at place c ^ turn(r).
 // SUMS: a segment's own sum to `local`, no outputs.  DIRECT: rows that start on
 // multiples of 16 bytes go to LDS without registers, a step ahead.
 template <int TYPE_, int D_, bool SUMS_, bool DIRECT_>
@@ -301,10 +301,15 @@ struct ChunkShape {
   static constexpr int TYPE = TYPE_, D = D_, WAVES = D / 16, THREADS = 64 * WAVES, PIECES = kChunk * D / 8 / THREADS;
   static constexpr bool SUMS = SUMS_, DIRECT = DIRECT_;
   static constexpr int TILE = kChunk * D;                       // 16-bit words
-  static constexpr int PRODUCTS = SUMS ? 0 : 2 * 4 * 2 * 512;   // of queries and keys, as operands in two parts
-  static constexpr int BYTES = ((SUMS ? 4 : 6) * TILE + PRODUCTS) * 2 + (SUMS ? 0 : 512);
+  // products of queries and keys, as operands in two parts: of 16 query rows with 32
+  // keys, six of which are not all of later keys
+  static constexpr int PART = 6 * 512, PRODUCTS = 2 * PART, UNDO = 6 * 16;
+  static constexpr int VALUES = SUMS ? 2 : 1, QUERIES = D == 128 ? 4 : 3;  // tiles of values and queries; beside two of keys, products of two heads
+  static constexpr int BYTES = SUMS ? 4 * TILE * 2 : ((3 + QUERIES) * TILE + 2 * PRODUCTS) * 2 + 2 * UNDO * 4;
+  __device__ static __forceinline__ constexpr int product(int i, int t) { return i < 2 ? i : 2 * i - 2 + t; }
 
-  __device__ static __forceinline__ int turn(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+  // Sixteen rows' same pieces lie on all banks, and two neighbouring pieces of eight.
+  __device__ static __forceinline__ int turn(int r) { return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1); }
 
   // Rows [0, count) of 64 to a tile, the last one in the place of those behind it.
   __device__ static __forceinline__ void fetch(const void *from, int64_t stride, int count, short *tile) {
@@ -320,35 +325,45 @@ struct ChunkShape {
       }
     }
   }
-  // An operand: a lane has row r0 + lane % 16 and columns c + 4 g .. and
-  // c + 16 + 4 g .., g = lane / 16: the order in which a product's results lie.
-  __device__ static __forceinline__ short8v rows(const short *tile, int r0, int c) {
-    const int r = r0 + (threadIdx.x & 15), at = c + (threadIdx.x >> 4 & 3) * 4;
-    const short4v a = *(const short4v *)(tile + r * D + ((at >> 3) ^ turn(r)) * 8 + (at & 7));
-    const short4v b = *(const short4v *)(tile + r * D + (((at + 16) >> 3) ^ turn(r)) * 8 + (at & 7));
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  // An operand: a lane has row r0 + lane % 16 (r0 a multiple of 16) and columns
+  // 32 t + 8 g .., g = lane / 16.  at[t]: where, in words, for r0 = 0.
+  using Rows = int[D / 32];
+  __device__ static __forceinline__ void places_of_rows(Rows &at) {
+    const int r = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) at[t] = r * D + ((4 * t + g) ^ turn(r)) * 8;
   }
-  // The transpose: a lane has column c + lane % 16 and rows r0 + 4 g .., r0 + 16 + 4 g ..
-  __device__ static __forceinline__ short8v columns(const short *tile, int r0, int c) {
+  __device__ static __forceinline__ short8v rows(const short *tile, const Rows &at, int r0, int t) {
+    return *(const short8v *)(tile + at[t] + r0 * D);
+  }
+  // Transposes.  A lane has rows r0 + 4 g .., r0 + 16 + 4 g .. of a column: of
+  // c + lane % 16 or, for the states' rows, of key_of(a, lane % 16), so that the
+  // results of tiles 2 t and 2 t + 1 are in a lane what rows() gives of step t.
+  __device__ static __forceinline__ constexpr int key_of(int a, int m) { return a / 2 * 32 + (m >> 2) * 8 + (a & 1) * 4 + (m & 3); }
+  __device__ static __forceinline__ short8v columns_at(const short *tile, int r0, int at) {
     using Place = __attribute__((address_space(3))) short4v;
-    const int l = threadIdx.x & 15, r = r0 + (threadIdx.x >> 4 & 3) * 4 + (l >> 2), at = c + (l & 3) * 4;
-    const auto place = [&](int row) { return (Place *)(tile + row * D + ((at >> 3) ^ turn(row)) * 8 + (at & 7)); };
-    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(place(r)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(place(r + 16));
+    const int r = (threadIdx.x >> 4 & 3) * 4 + (threadIdx.x >> 2 & 3);
+    const short *const p = tile + r * D + ((at >> 3) ^ turn(r)) * 8 + (at & 7);
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place *)(p + r0 * D));
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place *)(p + (r0 + 16) * D));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
+  __device__ static __forceinline__ short8v columns(const short *tile, int r0, int c) { return columns_at(tile, r0, c + (threadIdx.x & 3) * 4); }
+  __device__ static __forceinline__ short8v keys(const short *tile, int r0, int a) { return columns_at(tile, r0, key_of(a, (threadIdx.x & 3) * 4)); }
 };
-// The token of an operand's element e in step t, in that order.
+// The token of a transpose's element e in step t; results lie like that, so that they
+// are operands without a move.
 __device__ __forceinline__ constexpr int token(int t, int e, int g) { return t * 32 + (e >> 2) * 16 + 4 * g + (e & 3); }
 
 template <class S>
 __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   constexpr int TYPE = S::TYPE, D = S::D, KT = D / 16, KS = D / 32;  // tiles and steps of a key's elements
-  constexpr int HALVES = S::WAVES / 4, TASKS = 2 / HALVES;           // wavefronts to 16 query rows, pairs of key tiles to one
+  constexpr int TASKS = S::WAVES == 8 ? 1 : 2;                       // pairs of key tiles to a wavefront
   constexpr int PARTS = TYPE == kF16 ? 2 : 3;                        // of a decayed value: 22 or 24 bits, as the states have
   constexpr uint16_t INFINITE = TYPE == kF16 ? 0x7c00 : 0x7f80;
   extern __shared__ __attribute__((aligned(1024))) short state_lds[];
-  short *const lk = state_lds, *const lv = lk + 2 * S::TILE, *const lq = lv + 2 * S::TILE, *const lp = lq + 2 * S::TILE;
-  float *const undo = (float *)(lp + S::PRODUCTS);  // of a row of products, what undoes its factor
+  short *const lk = state_lds, *const lv = lk + 2 * S::TILE, *const lq = lv + S::VALUES * S::TILE, *const lp = lq + S::QUERIES * S::TILE;
+  float *const undo = (float *)(lp + 2 * S::PRODUCTS);  // of a row of products, what undoes its factor
   Segment seg = find_segment(A, blockIdx.x);
   seg.sequence = __builtin_amdgcn_readfirstlane(seg.sequence);  // so that the compiler knows them for the block's
   seg.number = __builtin_amdgcn_readfirstlane(seg.number);
@@ -363,21 +378,43 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   if (S::SUMS && last) return;
   const int64_t D2 = (int64_t)D * D, row0 = q.first + start;
   float *const local = A.local + ((int64_t)(seg.before + seg.number) * A.n_heads + h) * D2;
-  const int dv0 = wave * 16, mine_i = wave / HALVES, mine_t = wave % HALVES * TASKS;
+  const int dv0 = wave * 16;
+  // Products are made by 16 query rows and pairs of 16 keys: each SIMD (of eight
+  // wavefronts w and w + 4) has two or three tiles of them.
+  const int mine_i = S::WAVES == 4 ? wave : wave < 4 ? min(wave + 1, 3) : wave == 5 ? 2 : 0;
+  const int mine_t = S::WAVES == 4 ? 0 : wave == 3 || wave == 5 ? 1 : wave > 5 ? 2 : 0;
 
-  const auto fetch_kv = [&](int c, int buf) {
+  const auto fetch_k = [&](int c, int buf) {
     S::fetch((const uint16_t *)A.k + (row0 + c) * A.k_stride + h * D, A.k_stride, tokens - c, lk + buf * S::TILE);
+  };
+  const auto fetch_v = [&](int c, int buf) {
     S::fetch((const uint16_t *)A.v + (row0 + c) * A.v_stride + h * D, A.v_stride, tokens - c, lv + buf * S::TILE);
   };
   const auto fetch_q = [&](int c, int head, int buf) {
     S::fetch((const uint16_t *)A.q + (row0 + c) * A.q_stride + ((int64_t)h * group + head) * D, A.q_stride, tokens - c, lq + buf * S::TILE);
   };
-  fetch_kv(0, 0);
-  if constexpr (!S::SUMS) fetch_q(0, 0, 0);
+  // The block's (chunk, head) pairs, one after another: the queries of a later one
+  // are fetched while one is multiplied.
+  int next_c = 0, next_head = 0, next_buf = 0;
+  const auto fetch_next_q = [&] {
+    if (next_c >= tokens) return false;
+    fetch_q(next_c, next_head, next_buf);
+    next_buf = next_buf == S::QUERIES - 1 ? 0 : next_buf + 1;
+    if (++next_head == group) {
+      next_head = 0;
+      next_c += kChunk;
+    }
+    return true;
+  };
+  fetch_k(0, 0);
+  fetch_v(0, 0);
+  if constexpr (!S::SUMS) {
+    for (int i = 0; i < S::QUERIES - 1; ++i) fetch_next_q();
+  }
 
-  // s[a]: rows 16 a + 4 g .. of column dv0 + lane % 16
+  // s[a]: rows key_of(a, 4 g) .. of column dv0 + lane % 16
   float4v s[KT] = {};
-  const auto place = [&](int a, int e) { return (16 * a + 4 * g + e) * D + dv0 + own; };
+  const auto place = [&](int a, int e) { return S::key_of(a, 4 * g + e) * D + dv0 + own; };
   if constexpr (!S::SUMS) {
     const float *from = nullptr;
     // the segments' starts as k_state_step leaves them
@@ -402,15 +439,25 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   }
 
   arrive<0>();
-  for (int c = 0, buf = 0, step = 0; c < tokens; c += kChunk, buf ^= 1) {
+  const int out_at = own * A.n_q_heads * (D * 2) + g * 8;  // bytes; 64 rows fit 32 bits
+  typename S::Rows at_rows;
+  S::places_of_rows(at_rows);
+  bool fetched = false;
+  for (int c = 0, buf = 0, q_buf = 0; c < tokens; c += kChunk, buf ^= 1) {
     const int n = min(kChunk, tokens - c);
     const short *const k = lk + buf * S::TILE;
     const bool more = c + kChunk < tokens;
-    if (c) arrive<S::SUMS ? 0 : 4>();  // behind the loads of this chunk the four stores of the last full one
-    if (more) fetch_kv(c + kChunk, buf ^ 1);
+    // behind the loads of this chunk: four stores of the last one, which was whole, and later queries
+    if (c) {
+      if (S::SUMS) arrive<0>();
+      else if (S::QUERIES > 3 && fetched) arrive<4 + S::PIECES>();
+      else arrive<4>();
+    }
+    if (more) fetch_k(c + kChunk, buf ^ 1);
+    if (S::SUMS && more) fetch_v(c + kChunk, buf ^ 1);
     short8v v[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) v[t] = S::columns(lv + buf * S::TILE, t * 32, dv0);
+    for (int t = 0; t < 2; ++t) v[t] = S::columns(lv + (S::SUMS ? buf : 0) * S::TILE, t * 32, dv0);
     // the first token whose value in this lane's column is no number
     int none = kChunk;
     {
@@ -439,7 +486,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
     const bool numbers = !__any(none < kChunk);
 
     if constexpr (!S::SUMS) {
-      // the state as an operand: its results' order is the operands'
+      // the state as an operand
       Parts<TYPE, KS, 2> past;
       float past_undo[4];
       {
@@ -452,95 +499,123 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) past_undo[e] = TYPE == kF16 ? __shfl(inverse, 4 * g + e) : 1.0f;
       }
-      for (int head = 0; head < group; ++head, ++step) {
-        if (head) {
-          if (n == kChunk) arrive<4>();
-          else arrive<0>();
+      // 16 rows of <q, k>, decayed, by pairs of 16 keys, to LDS as operands
+      const auto products = [&](const short *lq_of, int to) {
+        if (2 * mine_t > mine_i) return;
+        short8v mine[KS];
+#pragma unroll
+        for (int t = 0; t < KS; ++t) mine[t] = S::rows(lq_of + mine_i * 16 * D, at_rows, 0, t);
+#pragma unroll
+        for (int task = 0; task < TASKS; ++task) {
+          const int t = mine_t + task;
+          if (2 * t > mine_i) break;
+          float x[1][8] = {};
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int j = 2 * t + half;
+            if (j > mine_i) break;
+            short8v keys[KS];
+#pragma unroll
+            for (int d = 0; d < KS; ++d) keys[d] = S::rows(k + j * 16 * D, at_rows, 0, d);
+            float4v sum = {0, 0, 0, 0};
+#pragma unroll
+            for (int d = 0; d < KS; ++d) sum = multiply<TYPE>(keys[d], mine[d], sum);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)  // later tokens are left out, whatever they are
+              x[0][half * 4 + e] = j == mine_i && 4 * g + e > own ? 0.0f : sum[e] * fade[task * 2 + half][e];
+          }
+          Parts<TYPE, 1, 2> p;
+          const float inverse = p.set(x, largest<TYPE, 1>(x));
+          short *const out = lp + to * S::PRODUCTS + (S::product(mine_i, t) * 64 + lane) * 8;
+          *(short8v *)out = p.part[0][0];
+          *(short8v *)(out + S::PART) = p.part[0][1];
+          if (TYPE == kF16 && g == 0) undo[to * S::UNDO + S::product(mine_i, t) * 16 + own] = inverse;
         }
-        const short *const lq_now = lq + (step & 1) * S::TILE;
-        if (head + 1 < group) fetch_q(c, head + 1, (step + 1) & 1);
-        else if (more) fetch_q(c + kChunk, 0, (step + 1) & 1);
-        // 16 rows of <q, k>, decayed, by pairs of 16 keys, to LDS as operands
-        if (2 * mine_t <= mine_i) {
-          short8v mine[KS];
+      };
+      // The first head's products, then each head's outputs beside the next one's products.
+      products(lq + q_buf * S::TILE, 0);
+      arrive<63>();
+      if (more) fetch_v(c + kChunk, 0);  // all have this chunk's values
+      for (int head = 0; head < group; ++head) {
+        const short *const lq_now = lq + q_buf * S::TILE, *const lp_now = lp + (head & 1) * S::PRODUCTS;
+        q_buf = q_buf == S::QUERIES - 1 ? 0 : q_buf + 1;
+        fetched = fetch_next_q();
+        // (One wavefront of a SIMD before its outputs, the other behind them.)
+        const bool ahead = head + 1 < group;
+        if (ahead && wave < 4) products(lq + q_buf * S::TILE, (head + 1) & 1);
+        // Two times two tiles of 16 rows of outputs, all of their operands on the way from
+        // LDS before the first product: a wavefront that waits for each has one other to
+        // wait behind.
+        {
+          uint8_t *const out = (uint8_t *)A.out + (((row0 + c) * A.n_q_heads + h * group + head) * D + dv0) * 2;
 #pragma unroll
-          for (int t = 0; t < KS; ++t) mine[t] = S::rows(lq_now, mine_i * 16, t * 32);
+          for (int u = 0; u < 2; ++u) {
+            if (u * 32 >= n) break;
+            short8v x[2][KS], w[2][2][2];
 #pragma unroll
-          for (int task = 0; task < TASKS; ++task) {
-            const int t = mine_t + task;
-            if (2 * t > mine_i) break;
-            float x[1][8] = {};
+            for (int t = 0; t < KS; ++t)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const int j = 2 * t + half;
-              if (j > mine_i) break;
-              float4v sum = {0, 0, 0, 0};
+              for (int i = 0; i < 2; ++i) x[i][t] = S::rows(lq_now, at_rows, u * 32 + i * 16, t);
 #pragma unroll
-              for (int d = 0; d < KS; ++d) sum = multiply<TYPE>(S::rows(k, j * 16, d * 32), mine[d], sum);
+            for (int t = 0; t <= u; ++t)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)  // later tokens are left out, whatever they are
-                x[0][half * 4 + e] = j == mine_i && 4 * g + e > own ? 0.0f : sum[e] * fade[task * 2 + half][e];
+              for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) w[i][t][p] = *(const short8v *)(lp_now + p * S::PART + (S::product(u * 2 + i, t) * 64 + lane) * 8);
+            __builtin_amdgcn_sched_barrier(0);
+            float4v o[2] = {};
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+#pragma unroll
+              for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) o[i] = multiply<TYPE>(past.part[t][p], x[i][t], o[i]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float seen = row_decay * power(l2, u * 32 + i * 16);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][e] = (TYPE == kF16 ? o[i][e] * past_undo[e] : o[i][e]) * seen;
             }
-            Parts<TYPE, 1, 2> p;
-            const float inverse = p.set(x, largest<TYPE, 1>(x));
-            *(short8v *)(lp + ((mine_i * 2 + t) * 64 + lane) * 8) = p.part[0][0];
-            *(short8v *)(lp + 4096 + ((mine_i * 2 + t) * 64 + lane) * 8) = p.part[0][1];
-            if (TYPE == kF16 && g == 0) undo[(mine_i * 2 + t) * 16 + own] = inverse;
-          }
-        }
-        arrive<63>();
-        // two times 16 rows of outputs at once
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (u * 32 >= n) break;
-          float4v o[2] = {};
+            for (int t = 0; t <= u; ++t)
 #pragma unroll
-          for (int t = 0; t < KS; ++t) {
-            short8v x[2];
+              for (int i = 0; i < 2; ++i) {
+                float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : o[i];
 #pragma unroll
-            for (int w = 0; w < 2; ++w) x[w] = S::rows(lq_now, u * 32 + w * 16, t * 32);
+                for (int p = 0; p < 2; ++p) sum = multiply<TYPE>(v[t], w[i][t][p], sum);
+                if constexpr (TYPE == kF16) {
+                  const float inverse = undo[(head & 1) * S::UNDO + S::product(u * 2 + i, t) * 16 + own];
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+                  for (int e = 0; e < 4; ++e) o[i][e] = __builtin_fmaf(sum[e], inverse, o[i][e]);
+                } else {
+                  o[i] = sum;
+                }
+              }
 #pragma unroll
-              for (int w = 0; w < 2; ++w) o[w] = multiply<TYPE>(past.part[t][p], x[w], o[w]);
-          }
+            for (int i = 0; i < 2; ++i) {
+              const int row = u * 32 + i * 16 + own;
+              if (!numbers) {
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const float seen = row_decay * power(l2, u * 32 + w * 16);
+                for (int e = 0; e < 4; ++e)
+                  if (row >= __shfl(none, 4 * g + e)) o[i][e] = __builtin_nanf("");
+              }
+              if (row < n) {
+                uint16_t bits[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[w][e] = (TYPE == kF16 ? o[w][e] * past_undo[e] : o[w][e]) * seen;
-          }
-#pragma unroll
-          for (int t = 0; t <= u; ++t)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const int at = (u * 2 + w) * 2 + t;
-              float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : o[w];
-#pragma unroll
-              for (int p = 0; p < 2; ++p) sum = multiply<TYPE>(v[t], *(const short8v *)(lp + p * 4096 + (at * 64 + lane) * 8), sum);
-              if constexpr (TYPE == kF16) {
-                const float inverse = undo[at * 16 + own];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[w][e] = __builtin_fmaf(sum[e], inverse, o[w][e]);
-              } else {
-                o[w] = sum;
+                for (int e = 0; e < 4; ++e) bits[e] = bits16<TYPE>(o[i][e]);
+                __builtin_memcpy(out + (uint32_t)(out_at + (u * 32 + i * 16) * A.n_q_heads * (D * 2)), bits, 8);
               }
             }
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const int row = u * 32 + w * 16 + own;
-            if (!numbers) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (row >= __shfl(none, 4 * g + e)) o[w][e] = __builtin_nanf("");
-            }
-            if (row < n) {
-              uint16_t bits[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) bits[e] = bits16<TYPE>(o[w][e]);
-              __builtin_memcpy((uint16_t *)A.out + ((row0 + c + row) * A.n_q_heads + h * group + head) * D + dv0 + 4 * g, bits, 8);
-            }
           }
+        }
+        if (ahead && wave >= 4) products(lq + q_buf * S::TILE, (head + 1) & 1);
+        // The next one's products need the queries after it: behind them what this
+        // one has asked for, and its stores.
+        if (head + 1 < group) {
+          if (n < kChunk) arrive<0>();
+          else if (S::QUERIES == 3) arrive<4>();
+          else if (head == 0 && more) fetched ? arrive<4 + 3 * S::PIECES>() : arrive<4 + 2 * S::PIECES>();
+          else fetched ? arrive<4 + S::PIECES>() : arrive<4>();
         }
       }
       if (last && q.state < 0 && !more) return;
@@ -561,20 +636,28 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
         }
       inverse = fading.set(x, largest<TYPE, 2>(x));
     }
+    constexpr int AT_ONCE = KT < 8 ? KT : 8;
 #pragma unroll
-    for (int a = 0; a < KT; ++a) {
-      float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : s[a] * kept;
+    for (int a0 = 0; a0 < KT; a0 += AT_ONCE) {
+      short8v x[AT_ONCE][2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const short8v x = S::columns(k, t * 32, a * 16);
+      for (int a = 0; a < AT_ONCE; ++a)
 #pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) sum = multiply<TYPE>(x, fading.part[t][p], sum);
-      }
-      if constexpr (TYPE == kF16) {
+        for (int t = 0; t < 2; ++t) x[a][t] = S::keys(k, t * 32, a0 + a);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[a][e] = __builtin_fmaf(sum[e], inverse, s[a][e] * kept);
-      } else {
-        s[a] = sum;
+      for (int a = 0; a < AT_ONCE; ++a) {
+        float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : s[a0 + a] * kept;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) sum = multiply<TYPE>(x[a][t], fading.part[t][p], sum);
+        if constexpr (TYPE == kF16) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[a0 + a][e] = __builtin_fmaf(sum[e], inverse, s[a0 + a][e] * kept);
+        } else {
+          s[a0 + a] = sum;
+        }
       }
     }
   }
