@@ -67,13 +67,6 @@ __device__ __forceinline__ int places(const StateArgs &A, int s) {
   const int n = segments(A, s);
   return n > 1 ? n : 0;
 }
-// Places of the sequences before `s` (all of a wavefront's lanes call it).
-__device__ __forceinline__ int places_before(const StateArgs &A, int s) {
-  int sum = 0;
-  for (int i = threadIdx.x & 63; i < s; i += 64) sum += places(A, i);
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  return sum;
-}
 // (Sequences that overlap, which the call does not allow, may have more segments
 // than there are places: those are left out.)
 __device__ __forceinline__ bool room_for(const StateArgs &A, int before, int n) { return (int64_t)before + n <= A.n_places; }
@@ -106,59 +99,72 @@ __device__ __forceinline__ Segment find_segment(const StateArgs &A, int x) {
   return {-1, 0, 0};
 }
 
-// ------------------------------------------------------------- token by token --
-// A block has COLS columns of a head's state, a thread HELD pieces of four in
-// rows ROWS apart.  Sequences in segments, whose own sums are there by then, are
-// joined in the same launch.
-constexpr int kStepHeads = 8;  // query heads at a time
-
-// A sequence's segments in order: local[j] becomes the state after segment j, and
-// the place of the last, which made no sum, takes the state that the sequence
-// starts from (its own may be written by the last segment while the first reads).
-template <int D>
-__device__ __forceinline__ void join_segments(const StateArgs &A, int sequence_at, int h, int part, int parts) {
-  constexpr int PIECES = D * D / 4 / kThreads, AHEAD = 16;
-  const int n = segments(A, sequence_at);
-  if (n < 2) return;
-  const int before = places_before(A, sequence_at);
+// Sequence by sequence of those in segments: the segments in order.  local[j] becomes
+// the state after segment j, and the place of the last, which made no sum, takes the
+// state that the sequence starts from (its own may be written by the last segment
+// while the first reads).  A thread has WIDE elements, so that many blocks have some;
+// `block`: of all joining ones.
+template <int D, int WIDE>
+__device__ __forceinline__ void join_segments(const StateArgs &A, int block) {
+  constexpr int PIECES = D * D / kThreads / WIDE, AHEAD = 32 / WIDE;
+  using Wide = float __attribute__((ext_vector_type(WIDE)));
+  const int h = block / PIECES % A.n_heads, lane = threadIdx.x & 63;
+  int left = block / (PIECES * A.n_heads), before = 0, at_sequence = -1;  // the sequence's number among them
+  for (int s0 = 0; s0 < A.n_seqs && at_sequence < 0; s0 += 64) {
+    const int m = places(A, s0 + lane), took = sum_upto(m, lane);
+    uint64_t some = __ballot(m > 0);
+    const int count = __popcll(some);
+    if (left < count) {
+      for (; left; --left) some &= some - 1;
+      const int at = __builtin_ctzll(some);
+      at_sequence = s0 + at;
+      before += __shfl(took - m, at);
+    } else {
+      left -= count;
+      before += __shfl(took, 63);
+    }
+  }
+  if (at_sequence < 0) return;
+  const int n = places(A, at_sequence);
   if (!room_for(A, before, n)) return;
-  const Sequence q = sequence(A, sequence_at);
-  const int64_t D2 = (int64_t)D * D, step = A.n_heads * D2;
+  const Sequence q = sequence(A, at_sequence);
+  const int64_t D2 = (int64_t)D * D, step = A.n_heads * D2, at = (block % PIECES * kThreads + threadIdx.x) * WIDE;
   const float kept = exact_power(A, h, A.segment);
-  for (int piece = part; piece < PIECES; piece += parts) {
-    const int64_t at = (piece * kThreads + threadIdx.x) * 4;
-    float *const p = A.local + ((int64_t)before * A.n_heads + h) * D2 + at;
-    float4v s = {0, 0, 0, 0};
-    if (!q.fresh) s = *(const float4v *)(A.states + ((int64_t)q.state * A.n_heads + h) * D2 + at);
-    *(float4v *)(p + (n - 1) * step) = s;
-    for (int j = 0; j + 1 < n; j += AHEAD) {
-      float4v own[AHEAD];
+  float *const p = A.local + ((int64_t)before * A.n_heads + h) * D2 + at;
+  Wide s = {};
+  if (!q.fresh) s = *(const Wide *)(A.states + ((int64_t)q.state * A.n_heads + h) * D2 + at);
+  *(Wide *)(p + (n - 1) * step) = s;
+  for (int j = 0; j + 1 < n; j += AHEAD) {
+    Wide own[AHEAD];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) own[i] = *(const float4v *)(p + min(j + i, n - 2) * step);
+    for (int i = 0; i < AHEAD; ++i) own[i] = *(const Wide *)(p + min(j + i, n - 2) * step);
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        if (j + i > n - 2) break;
+    for (int i = 0; i < AHEAD; ++i) {
+      if (j + i > n - 2) break;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(kept, s[e], own[i][e]);
-        *(float4v *)(p + (j + i) * step) = s;
-      }
+      for (int e = 0; e < WIDE; ++e) s[e] = __builtin_fmaf(kept, s[e], own[i][e]);
+      *(Wide *)(p + (j + i) * step) = s;
     }
   }
 }
 
-template <int TYPE, int D, int COLS>
+// ------------------------------------------------------------- token by token --
+// A block has COLS columns of a head's state, a thread HELD pieces of four in
+// rows ROWS apart.  Blocks behind those of the last sequence join segments, whose own
+// sums are there by then (of WIDE elements a thread; 0: none).
+constexpr int kStepHeads = 8;  // query heads at a time
+
+template <int TYPE, int D, int COLS, int WIDE>
 __global__ __launch_bounds__(kThreads) void k_state_step(StateArgs A) {
+  if constexpr (WIDE > 0)
+    if ((int)blockIdx.y >= A.n_seqs) return join_segments<D, WIDE>(A, (blockIdx.y - A.n_seqs) * gridDim.x + blockIdx.x);
   constexpr int LANES = COLS / 4, ROWS = kThreads / LANES, HELD = D / ROWS, PARTS = D / COLS, WAVES = kThreads / 64;
   static_assert(HELD >= 1 && LANES <= 64, "a piece a thread at least, a row in a wavefront");
   __shared__ float ks[D], qs[kStepHeads][D], sums[WAVES][kStepHeads][COLS];
   const int part = blockIdx.x % PARTS, h = blockIdx.x / PARTS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int group = A.n_q_heads / A.n_heads, row = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
   const Sequence q = sequence(A, blockIdx.y);
-  if (q.count > A.step_most) {
-    if (A.segment < A.max_q) join_segments<D>(A, blockIdx.y, h, part, PARTS);
-    return;
-  }
-  if (q.count < 1) return;
+  if (q.count < 1 || q.count > A.step_most) return;
   const float l = power(log2_decay(A, h), 1);
   float *const at = q.state < 0 ? nullptr : A.states + ((int64_t)q.state * A.n_heads + h) * D * D + part * COLS + col;
   float4v s[HELD];
@@ -304,8 +310,8 @@ struct ChunkShape {
   // products of queries and keys, as operands in two parts: of 16 query rows with 32
   // keys, six of which are not all of later keys
   static constexpr int PART = 6 * 512, PRODUCTS = 2 * PART, UNDO = 6 * 16;
-  static constexpr int VALUES = SUMS ? 2 : 1, QUERIES = D == 128 ? 4 : 3;  // tiles of values and queries; beside two of keys, products of two heads
-  static constexpr int BYTES = SUMS ? 4 * TILE * 2 : ((3 + QUERIES) * TILE + 2 * PRODUCTS) * 2 + 2 * UNDO * 4;
+  static constexpr int KEYS = SUMS ? 4 : 2, VALUES = SUMS ? 4 : 1, QUERIES = D == 128 ? 4 : 3;  // tiles; beside them products of two heads
+  static constexpr int BYTES = SUMS ? 8 * TILE * 2 : ((3 + QUERIES) * TILE + 2 * PRODUCTS) * 2 + 2 * UNDO * 4;
   __device__ static __forceinline__ constexpr int product(int i, int t) { return i < 2 ? i : 2 * i - 2 + t; }
 
   // Sixteen rows' same pieces lie on all banks, and two neighbouring pieces of eight.
@@ -362,7 +368,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   constexpr int PARTS = TYPE == kF16 ? 2 : 3;                        // of a decayed value: 22 or 24 bits, as the states have
   constexpr uint16_t INFINITE = TYPE == kF16 ? 0x7c00 : 0x7f80;
   extern __shared__ __attribute__((aligned(1024))) short state_lds[];
-  short *const lk = state_lds, *const lv = lk + 2 * S::TILE, *const lq = lv + S::VALUES * S::TILE, *const lp = lq + S::QUERIES * S::TILE;
+  short *const lk = state_lds, *const lv = lk + S::KEYS * S::TILE, *const lq = lv + S::VALUES * S::TILE, *const lp = lq + S::QUERIES * S::TILE;
   float *const undo = (float *)(lp + 2 * S::PRODUCTS);  // of a row of products, what undoes its factor
   Segment seg = find_segment(A, blockIdx.x);
   seg.sequence = __builtin_amdgcn_readfirstlane(seg.sequence);  // so that the compiler knows them for the block's
@@ -408,6 +414,11 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   };
   fetch_k(0, 0);
   fetch_v(0, 0);
+  if constexpr (S::SUMS)  // whole chunks, as all but a sequence's last segment has
+    for (int i = 1; i < 3 && i * kChunk < tokens; ++i) {
+      fetch_k(i * kChunk, i);
+      fetch_v(i * kChunk, i);
+    }
   if constexpr (!S::SUMS) {
     for (int i = 0; i < S::QUERIES - 1; ++i) fetch_next_q();
   }
@@ -417,7 +428,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   const auto place = [&](int a, int e) { return S::key_of(a, 4 * g + e) * D + dv0 + own; };
   if constexpr (!S::SUMS) {
     const float *from = nullptr;
-    // the segments' starts as k_state_step leaves them
+    // the segments' starts as join_segments leaves them
     if (seg.number) from = local - (int64_t)A.n_heads * D2;
     else if (!q.fresh) from = last ? A.states + ((int64_t)q.state * A.n_heads + h) * D2
                                    : A.local + ((int64_t)(seg.before + (q.count - 1) / A.segment) * A.n_heads + h) * D2;
@@ -438,23 +449,29 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
     row_decay = A.scale * power(l2, own + 1);
   }
 
-  arrive<0>();
+  if constexpr (!S::SUMS) arrive<0>();
   const int out_at = own * A.n_q_heads * (D * 2) + g * 8;  // bytes; 64 rows fit 32 bits
   typename S::Rows at_rows;
   S::places_of_rows(at_rows);
   bool fetched = false;
-  for (int c = 0, buf = 0, q_buf = 0; c < tokens; c += kChunk, buf ^= 1) {
+  for (int c = 0, buf = 0, q_buf = 0; c < tokens; c += kChunk, buf = (buf + 1) & (S::KEYS - 1)) {
     const int n = min(kChunk, tokens - c);
     const short *const k = lk + buf * S::TILE;
     const bool more = c + kChunk < tokens;
     // behind the loads of this chunk: four stores of the last one, which was whole, and later queries
-    if (c) {
-      if (S::SUMS) arrive<0>();
-      else if (S::QUERIES > 3 && fetched) arrive<4 + S::PIECES>();
+    if (S::SUMS) {  // behind them the loads of up to two chunks
+      if (tokens - c > 2 * kChunk) arrive<4 * S::PIECES>();
+      else if (more) arrive<2 * S::PIECES>();
+      else arrive<0>();
+    } else if (c) {
+      if (S::QUERIES > 3 && fetched) arrive<4 + S::PIECES>();
       else arrive<4>();
     }
-    if (more) fetch_k(c + kChunk, buf ^ 1);
-    if (S::SUMS && more) fetch_v(c + kChunk, buf ^ 1);
+    if (S::SUMS && c + 3 * kChunk < tokens) {
+      fetch_k(c + 3 * kChunk, (buf + 3) & 3);
+      fetch_v(c + 3 * kChunk, (buf + 3) & 3);
+    }
+    if (!S::SUMS && more) fetch_k(c + kChunk, buf ^ 1);
     short8v v[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) v[t] = S::columns(lv + (S::SUMS ? buf : 0) * S::TILE, t * 32, dv0);
@@ -509,21 +526,23 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
         for (int task = 0; task < TASKS; ++task) {
           const int t = mine_t + task;
           if (2 * t > mine_i) break;
-          float x[1][8] = {};
+          short8v keys[2][KS];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int j = 2 * t + half;
-            if (j > mine_i) break;
-            short8v keys[KS];
+          for (int d = 0; d < KS; ++d)
 #pragma unroll
-            for (int d = 0; d < KS; ++d) keys[d] = S::rows(k + j * 16 * D, at_rows, 0, d);
-            float4v sum = {0, 0, 0, 0};
+            for (int half = 0; half < 2; ++half) keys[half][d] = S::rows(k + (2 * t + half) * 16 * D, at_rows, 0, d);
+          __builtin_amdgcn_sched_barrier(0);
+          float4v sum[2] = {};
 #pragma unroll
-            for (int d = 0; d < KS; ++d) sum = multiply<TYPE>(keys[d], mine[d], sum);
+          for (int d = 0; d < KS; ++d)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) sum[half] = multiply<TYPE>(keys[half][d], mine[d], sum[half]);
+          float x[1][8];
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int e = 0; e < 4; ++e)  // later tokens are left out, whatever they are
-              x[0][half * 4 + e] = j == mine_i && 4 * g + e > own ? 0.0f : sum[e] * fade[task * 2 + half][e];
-          }
+              x[0][half * 4 + e] = (2 * t + half) * 16 + 4 * g + e > mine_i * 16 + own ? 0.0f : sum[half][e] * fade[task * 2 + half][e];
           Parts<TYPE, 1, 2> p;
           const float inverse = p.set(x, largest<TYPE, 1>(x));
           short *const out = lp + to * S::PRODUCTS + (S::product(mine_i, t) * 64 + lane) * 8;
@@ -626,14 +645,26 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
     float inverse;
     {
       float x[2][8];
+      const float behind = (float)(n - 1 - 4 * g);  // tokens, of the chunk's behind this lane's first
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int at = token(t, e, g);
-          x[t][e] = at < n ? value16<TYPE>((uint16_t)v[t][e]) * power(l2, n - 1 - at) : 0.0f;
-          if (at == none) x[t][e] = __builtin_nanf("");
-        }
+        for (int e = 0; e < 8; ++e)
+          x[t][e] = value16<TYPE>((uint16_t)v[t][e]) * __builtin_amdgcn_exp2f(l2 * (behind - (float)token(t, e, 0)));
+      if (n < kChunk) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (token(t, e, g) >= n) x[t][e] = 0.0f;
+      }
+      if (!numbers) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (token(t, e, g) == none) x[t][e] = __builtin_nanf("");
+      }
       inverse = fading.set(x, largest<TYPE, 2>(x));
     }
     constexpr int AT_ONCE = KT < 8 ? KT : 8;
@@ -718,17 +749,23 @@ hipError_t chunks_of(dim3 grid, const StateArgs &A, hipStream_t s) {
   return chunks_as<ChunkShape<TYPE, D, SUMS, false>>(grid, A, s);
 }
 
-template <int TYPE, int D, int COLS>
-hipError_t steps_as(const StateArgs &A, hipStream_t s) {
-  k_state_step<TYPE, D, COLS><<<dim3(A.n_heads * (D / COLS), A.n_seqs), kThreads, 0, s>>>(A);
+template <int TYPE, int D, int COLS, int WIDE>
+hipError_t steps_as(const StateArgs &A, int64_t joined, hipStream_t s) {
+  const int64_t width = (int64_t)A.n_heads * (D / COLS);
+  const int64_t joins = WIDE ? joined * A.n_heads * (D * D / kThreads / std::max(WIDE, 1)) : 0;
+  k_state_step<TYPE, D, COLS, WIDE><<<dim3((unsigned)width, (unsigned)(A.n_seqs + (joins + width - 1) / width)), kThreads, 0, s>>>(A);
   return hipGetLastError();
 }
+// Single tokens, and behind them `joined` sequences' segments to be joined.
+// (Joining 128 segments of 2 heads takes 24 us with four elements a thread, 11 with
+// one; 8 of 32 heads 7.5 and 12, where blocks are many.)
 template <int TYPE, int D>
-hipError_t steps_of(const StateArgs &A, hipStream_t s) {
+hipError_t steps_of(const StateArgs &A, int64_t joined, hipStream_t s) {
   const int64_t heads = (int64_t)A.n_seqs * A.n_heads;
-  if (heads >= 512) return steps_as<TYPE, D, D>(A, s);
-  if (heads >= 128) return steps_as<TYPE, D, 32>(A, s);
-  return steps_as<TYPE, D, 16>(A, s);
+  if (joined) return joined * A.n_heads >= 16 ? steps_as<TYPE, D, 32, 4>(A, joined, s) : steps_as<TYPE, D, 16, 1>(A, joined, s);
+  if (heads >= 512) return steps_as<TYPE, D, D, 0>(A, 0, s);
+  if (heads >= 128) return steps_as<TYPE, D, 32, 0>(A, 0, s);
+  return steps_as<TYPE, D, 16, 0>(A, 0, s);
 }
 
 template <int TYPE, int D>
@@ -736,13 +773,14 @@ hipError_t state_of(StateArgs A, hipStream_t s) {
   A.segment = segment_tokens(A.n_tokens, A.n_heads);
   A.n_places = (int32_t)places_at_most(A.n_tokens, A.n_heads);
   A.step_most = kStepMost;
-  if (A.max_q <= kStepMost) return steps_of<TYPE, D>(A, s);
+  if (A.max_q <= kStepMost) return steps_of<TYPE, D>(A, 0, s);
   if (A.n_seqs == 1) A.step_most = 0;  // no launch for what may be a single token
   const bool one = A.segment >= A.max_q;  // a segment a sequence
   const dim3 grid(one ? (unsigned)A.n_seqs : (unsigned)segments_at_most(A.n_tokens, A.n_seqs, A.n_heads), A.n_heads);
-  hipError_t e = hipSuccess;
-  if (!one) e = chunks_of<TYPE, D, true>(grid, A, s);
-  if (e == hipSuccess && (!one || A.step_most)) e = steps_of<TYPE, D>(A, s);
+  hipError_t e = one ? hipSuccess : chunks_of<TYPE, D, true>(grid, A, s);
+  // at most so many sequences have more tokens than a segment
+  const int64_t joined = one ? 0 : std::min<int64_t>(A.n_seqs, A.n_tokens / A.segment);
+  if (e == hipSuccess && (joined || A.step_most)) e = steps_of<TYPE, D>(A, joined, s);
   return e == hipSuccess ? chunks_of<TYPE, D, false>(grid, A, s) : e;
 }
 
