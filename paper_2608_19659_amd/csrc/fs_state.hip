@@ -45,22 +45,27 @@ __device__ __forceinline__ int count_of(const StateArgs &A, int s, int *first) {
   *first = a;
   return min(b - a, A.max_q);
 }
-__device__ __forceinline__ Sequence sequence(const StateArgs &A, int s) {
+__device__ __forceinline__ Sequence sequence_of(const StateArgs &A, int first, int count, int index, int held) {
   Sequence q;
-  q.count = count_of(A, s, &q.first);
-  const int index = A.index[s], held = A.ctx_lens[s];
+  q.first = first;
+  q.count = count;
   q.state = index >= 0 && index < A.n_states ? index : -1;
   q.fresh = q.state < 0 || held <= q.count;
   return q;
+}
+__device__ __forceinline__ Sequence sequence(const StateArgs &A, int s) {
+  int first;
+  const int count = count_of(A, s, &first);
+  return sequence_of(A, first, count, A.index[s], A.ctx_lens[s]);
 }
 
 // ------------------------------------------------------------------- segments --
 // Segments of `segment` tokens (a multiple of 64), numbered over the sequences;
 // sequences of at most step_most tokens have none.
+__device__ __forceinline__ int segments_in(const StateArgs &A, int count) { return count > A.step_most ? (count - 1) / A.segment + 1 : 0; }
 __device__ __forceinline__ int segments(const StateArgs &A, int s) {
   int first;
-  const int n = s < A.n_seqs ? count_of(A, s, &first) : 0;
-  return n > A.step_most ? (n - 1) / A.segment + 1 : 0;
+  return s < A.n_seqs ? segments_in(A, count_of(A, s, &first)) : 0;
 }
 // A sequence of two segments or more has a place in the workspace for each.
 __device__ __forceinline__ int places(const StateArgs &A, int s) {
@@ -79,24 +84,30 @@ __device__ __forceinline__ int sum_upto(int v, int lane) {
   return v;
 }
 struct Segment {
-  int sequence, number, before;  // -1: there is none; its number in the sequence; places before the sequence's
+  int number, before;  // its number in the sequence; -1: there is none; places before the sequence's
+  Sequence sequence;
 };
 __device__ __forceinline__ Segment find_segment(const StateArgs &A, int x) {
-  if (A.segment >= A.max_q) return {x, 0, 0};  // a segment a sequence
+  if (A.segment >= A.max_q) return {0, 0, sequence(A, x)};  // a segment a sequence
   const int lane = threadIdx.x & 63;
   int before = 0, taken = 0;
   for (int s0 = 0; s0 < A.n_seqs; s0 += 64) {
-    const int n = segments(A, s0 + lane), m = n > 1 ? n : 0, upto = sum_upto(n, lane), took = sum_upto(m, lane);
+    const int s = min(s0 + lane, A.n_seqs - 1);
+    int first;  // all loads at once: the block can do nothing without them
+    const int count = count_of(A, s, &first), index = A.index[s], held = A.ctx_lens[s];
+    const int n = s0 + lane < A.n_seqs ? segments_in(A, count) : 0, m = n > 1 ? n : 0;
+    const int upto = sum_upto(n, lane), took = sum_upto(m, lane);
     const uint64_t in = __ballot(x < before + upto);
     if (in) {
-      const int at = __builtin_ctzll(in), first = taken + __shfl(took - m, at);
-      if (!room_for(A, first, __shfl(m, at))) break;
-      return {s0 + at, x - before - __shfl(upto - n, at), first};
+      const int at = __builtin_ctzll(in), place = taken + __shfl(took - m, at);
+      if (!room_for(A, place, __shfl(m, at))) break;
+      return {x - before - __shfl(upto - n, at), place,
+              sequence_of(A, __shfl(first, at), __shfl(count, at), __shfl(index, at), __shfl(held, at))};
     }
     before += __shfl(upto, 63);
     taken += __shfl(took, 63);
   }
-  return {-1, 0, 0};
+  return {-1, 0, {}};
 }
 
 // Sequence by sequence of those in segments: the segments in order.  local[j] becomes
@@ -370,20 +381,22 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   extern __shared__ __attribute__((aligned(1024))) short state_lds[];
   short *const lk = state_lds, *const lv = lk + S::KEYS * S::TILE, *const lq = lv + S::VALUES * S::TILE, *const lp = lq + S::QUERIES * S::TILE;
   float *const undo = (float *)(lp + 2 * S::PRODUCTS);  // of a row of products, what undoes its factor
-  Segment seg = find_segment(A, blockIdx.x);
-  seg.sequence = __builtin_amdgcn_readfirstlane(seg.sequence);  // so that the compiler knows them for the block's
-  seg.number = __builtin_amdgcn_readfirstlane(seg.number);
-  seg.before = __builtin_amdgcn_readfirstlane(seg.before);
-  if (seg.sequence < 0) return;
-  const Sequence q = sequence(A, seg.sequence);
+  const Segment seg = find_segment(A, blockIdx.x);
+  const int number = __builtin_amdgcn_readfirstlane(seg.number), before = __builtin_amdgcn_readfirstlane(seg.before);
+  if (number < 0) return;
+  Sequence q = seg.sequence;  // the block's: known to be so to the compiler as well
+  q.first = __builtin_amdgcn_readfirstlane(q.first);
+  q.count = __builtin_amdgcn_readfirstlane(q.count);
+  q.state = __builtin_amdgcn_readfirstlane(q.state);
+  q.fresh = __builtin_amdgcn_readfirstlane(q.fresh);
   if (q.count <= A.step_most) return;
-  const int start = seg.number * A.segment, tokens = min(A.segment, q.count - start), h = blockIdx.y;
+  const int start = number * A.segment, tokens = min(A.segment, q.count - start), h = blockIdx.y;
   const int group = A.n_q_heads / A.n_heads, lane = threadIdx.x & 63, g = lane >> 4, own = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool last = start + tokens == q.count;
   if (S::SUMS && last) return;
   const int64_t D2 = (int64_t)D * D, row0 = q.first + start;
-  float *const local = A.local + ((int64_t)(seg.before + seg.number) * A.n_heads + h) * D2;
+  float *const local = A.local + ((int64_t)(before + number) * A.n_heads + h) * D2;
   const int dv0 = wave * 16;
   // Products are made by 16 query rows and pairs of 16 keys: each SIMD (of eight
   // wavefronts w and w + 4) has two or three tiles of them.
@@ -429,9 +442,9 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   if constexpr (!S::SUMS) {
     const float *from = nullptr;
     // the segments' starts as join_segments leaves them
-    if (seg.number) from = local - (int64_t)A.n_heads * D2;
+    if (number) from = local - (int64_t)A.n_heads * D2;
     else if (!q.fresh) from = last ? A.states + ((int64_t)q.state * A.n_heads + h) * D2
-                                   : A.local + ((int64_t)(seg.before + (q.count - 1) / A.segment) * A.n_heads + h) * D2;
+                                   : A.local + ((int64_t)(before + (q.count - 1) / A.segment) * A.n_heads + h) * D2;
     if (from)
 #pragma unroll
       for (int a = 0; a < KT; ++a)
@@ -677,17 +690,24 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
         for (int t = 0; t < 2; ++t) x[a][t] = S::keys(k, t * 32, a0 + a);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int a = 0; a < AT_ONCE; ++a) {
-        float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : s[a0 + a] * kept;
+      for (int a = 0; a < AT_ONCE; a += 4) {  // four sums side by side, none waits for itself
+        float4v sum[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = TYPE == kF16 ? float4v{0, 0, 0, 0} : s[a0 + a + i] * kept;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p) sum = multiply<TYPE>(x[a][t], fading.part[t][p], sum);
-        if constexpr (TYPE == kF16) {
+          for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[a0 + a][e] = __builtin_fmaf(sum[e], inverse, s[a0 + a][e] * kept);
-        } else {
-          s[a0 + a] = sum;
+            for (int i = 0; i < 4; ++i) sum[i] = multiply<TYPE>(x[a + i][t], fading.part[t][p], sum[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (TYPE == kF16) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[a0 + a + i][e] = __builtin_fmaf(sum[i][e], inverse, s[a0 + a + i][e] * kept);
+          } else {
+            s[a0 + a + i] = sum[i];
+          }
         }
       }
     }
