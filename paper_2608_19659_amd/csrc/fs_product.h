@@ -123,6 +123,8 @@ template <int TYPE, int THREADS, int HELD, bool NORMED>
 __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
   __shared__ uint32_t lds[THREADS / 64];
   __shared__ Squares squares[NORMED ? THREADS / 64 : 1];
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < A.n_zero; i += THREADS) A.zero[i] = 0;
   Squares mine = {0.0f, 0.0f};
   const auto norm = [&](int c, float(&x)[8]) {
     float g[8];
@@ -364,6 +366,44 @@ __device__ __forceinline__ bool join_parts(int8_t *lds, int wk, int wave, int la
   return true;
 }
 
+// The sums of the blocks that share a tile meet in memory: each writes its own, and
+// the last to arrive adds the others' (whole numbers: the order is of no account).
+// They go from block to block, whose L2 may be another XCD's, at the device's scope,
+// past the L2.  True: of the last one.
+template <class S>
+__device__ __forceinline__ bool join_blocks(const MatmulArgs &A, int slot, int part, int parts, bool mine, int wt, int lane,
+                                            int4v (&acc)[S::MT][S::NT]) {
+  __shared__ int last;
+  constexpr int COUNT = S::MT * S::NT, LANES = S::TILES * 64;
+  using Two = unsigned long long;
+  Two *const sums = (Two *)A.partials + ((int64_t)slot * parts * COUNT * LANES + wt * 64 + lane) * 2;
+  const auto at = [&](int p, int c) { return sums + ((int64_t)p * COUNT + c) * LANES * 2; };
+  if (mine) {
+#pragma unroll
+    for (int c = 0; c < COUNT; ++c) {
+      const int4v v = acc[c / S::NT][c % S::NT];
+      __hip_atomic_store(at(part, c), (Two)(uint32_t)v[0] | (Two)(uint32_t)v[1] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(at(part, c) + 1, (Two)(uint32_t)v[2] | (Two)(uint32_t)v[3] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each wavefront's stores are done before the block counts as there
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(A.arrived + slot, 1) == parts - 1;
+  __syncthreads();
+  if (!last) return false;
+  if (mine)
+    for (int p = 0; p < parts; ++p) {
+      if (p == part) continue;
+#pragma unroll
+      for (int c = 0; c < COUNT; ++c) {
+        const Two a = __hip_atomic_load(at(p, c), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const Two b = __hip_atomic_load(at(p, c) + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        acc[c / S::NT][c % S::NT] += int4v{(int)(uint32_t)a, (int)(a >> 32), (int)(uint32_t)b, (int)(b >> 32)};
+      }
+    }
+  return true;
+}
+
 // A wavefront's part of a tile, from token m and channel n on.
 template <class S>
 __device__ __forceinline__ void store_tile(const MatmulArgs &A, int m, int n, int lane, int4v (&acc)[S::MT][S::NT],
@@ -578,15 +618,24 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
   __shared__ __attribute__((aligned(1024))) int8_t lds[S::BYTES];
   // Workgroups go round the eight XCDs in turn: each XCD gets a run of tiles,
   // in groups of eight rows of tiles, so that its L2 serves both operands.
-  const int total = tiles_m * tiles_n, per = (total + 7) / 8;
-  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  // (Finished products: an XCD's tiles behind the first A.whole are cut into A.parts
+  // along the inner dimension, a block a part.)
+  const int total = tiles_m * tiles_n, per = (total + 7) / 8, xcd = blockIdx.x & 7;
+  int in_xcd = blockIdx.x >> 3, part = 0, parts = 1;
+  if (FINISH != kScaled && in_xcd >= A.whole) {
+    parts = A.parts;
+    part = (in_xcd - A.whole) % parts;
+    in_xcd = A.whole + (in_xcd - A.whole) / parts;
+  }
+  const int id = xcd * per + in_xcd;
+  if (in_xcd >= per || id >= total) return;
   const int group = id / (8 * tiles_n), gm = min(8, tiles_m - group * 8), in = id - group * 8 * tiles_n;
   const int m0 = (group * 8 + in % gm) * S::BM, n0 = in / gm * kChannels<S, FINISH>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wk = wave / S::TILES, wt = wave % S::TILES;
   const int wm = wt / (S::BN / S::WN) * S::WM, wn = wt % (S::BN / S::WN) * S::WN;
-  const int8_t *const ta = A.a + (int64_t)m0 * A.a_stride, *const tw = A.w + (int64_t)n0 * A.w_stride;
+  const int each = A.K / S::BK / parts * S::BK, k0 = part * each, K = part == parts - 1 ? A.K - k0 : each;
+  const int8_t *const ta = A.a + (int64_t)m0 * A.a_stride + k0, *const tw = A.w + (int64_t)n0 * A.w_stride + k0;
   const int last_a = A.M - 1 - m0, last_w = A.N - 1 - n0;
   // a weight row of the tile, in rows from its first one on
   const auto from_w = [&](int r) {
@@ -604,7 +653,7 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
     // both operands through registers: 333 x 1001 x 1999 11.8 and 14.5, 64 x 5001 x
     // 5119 18.2 and 23.3, 3000 x 5001 x 2999 76 and 89.)
     constexpr int AHEAD = S::NS >= 3 && S::MT * S::NT <= 8 ? 2 : 1;
-    const int stages = (A.K + S::BK - 1) / S::BK;
+    const int stages = (K + S::BK - 1) / S::BK;
     const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)lds + wave * 1024;
     Piece rw[AHEAD][S::LW];
     uint32_t row_a[S::LA];
@@ -613,14 +662,14 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
     for (int i = 0; i < S::LA; ++i) row_a[i] = (uint32_t)min(place<S>(i).x, last_a) * (uint32_t)A.a_stride;
 #pragma unroll
     for (int i = 0; i < S::LW; ++i) pw[i] = tw + (int64_t)from_w(place<S>(i).x) * A.w_stride;
-    const int last_piece = (A.K - 1) & ~15;
+    const int last_piece = (K - 1) & ~15;
     const auto fetch = [&](int p, int t, int slot) {
 #pragma unroll
       for (int i = 0; i < S::LA; ++i)
         load_to_lds(ta, row_a[i] + min(t * S::BK + place<S>(i).y, last_piece), base + slot * S::STAGE + i * S::THREADS * 16);
-      const bool over = (t + 1) * S::BK > A.K;
+      const bool over = (t + 1) * S::BK > K;
 #pragma unroll
-      for (int i = 0; i < S::LW; ++i) rw[p][i].load(pw[i], t * S::BK + place<S>(i).y, A.K, over);
+      for (int i = 0; i < S::LW; ++i) rw[p][i].load(pw[i], t * S::BK + place<S>(i).y, K, over);
     };
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p)
@@ -630,11 +679,11 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
       for (int p = 0; p < AHEAD; ++p) {
         const int t = t0 + p;
         if (t >= stages) break;
-        const bool over = (t + 1) * S::BK > A.K;
+        const bool over = (t + 1) * S::BK > K;
         int8_t *const la = lds + slot * S::STAGE, *const lw = la + S::PART_A;
 #pragma unroll
         for (int i = 0; i < S::LW; ++i)
-          *(int4v *)(lw + (i * S::THREADS + threadIdx.x) * 16) = rw[p][i].codes(t * S::BK + place<S>(i).y, A.K, over);
+          *(int4v *)(lw + (i * S::THREADS + threadIdx.x) * 16) = rw[p][i].codes(t * S::BK + place<S>(i).y, K, over);
         // the codes of stage t: behind them its weights' loads and a stage's where two are under way
         if (t + 1 < stages) wait_loads<(AHEAD == 2 ? S::LA + 2 * S::LW : S::LW)>();
         else wait_loads<0>();
@@ -645,10 +694,10 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
         slot = slot == S::NS - 1 ? 0 : slot + 1;
       }
     }
-    done = A.K;
+    done = K;
   }
   if constexpr (DIRECT == kBoth) {
-    const int full = A.K / S::BK;
+    const int full = K / S::BK;
     const uint32_t base = (uint32_t)(size_t)(__attribute__((address_space(3))) int8_t *)lds + wave * 1024;
     // a lane's places in a stage, from the tile's first row on (strides fit 32 bits: see matmul_as)
     uint32_t oa[S::LA], ow[S::LW];
@@ -678,7 +727,7 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
   }
   // Rows at any alignment, or their last part: through registers, AHEAD stages'
   // loads under way (as many as there are registers for).
-  if (DIRECT != kCodes && done < A.K) {
+  if (DIRECT != kCodes && done < K) {
     constexpr int AHEAD = DIRECT == kBoth || S::MT * S::NT > 8 ? 1 : 2;
     Piece ra[AHEAD][S::LA], rw[AHEAD][S::LW];
     const int8_t *pa[S::LA], *pw[S::LW];
@@ -687,35 +736,38 @@ __global__ __launch_bounds__(S::THREADS) void k_matmul(MatmulArgs A, int tiles_m
 #pragma unroll
     for (int i = 0; i < S::LW; ++i) pw[i] = tw + (int64_t)from_w(place<S>(i).x) * A.w_stride;
     const auto fetch = [&](int p, int k) {
-      const bool over = k + S::BK > A.K;
+      const bool over = k + S::BK > K;
 #pragma unroll
-      for (int i = 0; i < S::LA; ++i) ra[p][i].load(pa[i], k + place<S>(i).y, A.K, over);
+      for (int i = 0; i < S::LA; ++i) ra[p][i].load(pa[i], k + place<S>(i).y, K, over);
 #pragma unroll
-      for (int i = 0; i < S::LW; ++i) rw[p][i].load(pw[i], k + place<S>(i).y, A.K, over);
+      for (int i = 0; i < S::LW; ++i) rw[p][i].load(pw[i], k + place<S>(i).y, K, over);
     };
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p)
-      if (done + p * S::BK < A.K) fetch(p, done + p * S::BK);
-    for (int k0 = done; k0 < A.K; k0 += AHEAD * S::BK) {
+      if (done + p * S::BK < K) fetch(p, done + p * S::BK);
+    for (int k0 = done; k0 < K; k0 += AHEAD * S::BK) {
 #pragma unroll
       for (int p = 0; p < AHEAD; ++p) {
         const int k = k0 + p * S::BK;
-        if (k >= A.K) break;
-        const bool over = k + S::BK > A.K;
+        if (k >= K) break;
+        const bool over = k + S::BK > K;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < S::LA; ++i)
-          *(int4v *)(lds + (i * S::THREADS + threadIdx.x) * 16) = ra[p][i].codes(k + place<S>(i).y, A.K, over);
+          *(int4v *)(lds + (i * S::THREADS + threadIdx.x) * 16) = ra[p][i].codes(k + place<S>(i).y, K, over);
 #pragma unroll
         for (int i = 0; i < S::LW; ++i)
-          *(int4v *)(lds + S::PART_A + (i * S::THREADS + threadIdx.x) * 16) = rw[p][i].codes(k + place<S>(i).y, A.K, over);
+          *(int4v *)(lds + S::PART_A + (i * S::THREADS + threadIdx.x) * 16) = rw[p][i].codes(k + place<S>(i).y, K, over);
         __syncthreads();
-        if (k + AHEAD * S::BK < A.K) fetch(p, k + AHEAD * S::BK);
+        if (k + AHEAD * S::BK < K) fetch(p, k + AHEAD * S::BK);
         multiply_stage<S>(lds, lds + S::PART_A, wm, wn, wk, lane, acc);
       }
     }
   }
-  if (!join_parts<S>(lds, wk, wave, lane, acc)) return;
+  const bool mine = join_parts<S>(lds, wk, wave, lane, acc);
+  if constexpr (FINISH != kScaled)
+    if (parts > 1 && !join_blocks<S>(A, xcd * (per - A.whole) + in_xcd - A.whole, part, parts, mine, wt, lane, acc)) return;
+  if (!mine) return;
   float sa[S::MT];
 #pragma unroll
   for (int i = 0; i < S::MT; ++i) sa[i] = A.a_scale[min(m0 + wm + i * 16 + (lane & 15), A.M - 1)];
@@ -923,7 +975,8 @@ template <int TYPE, Finish FINISH, int BM, int BN, int WM, int WN, int BK, int W
 hipError_t matmul_as(const MatmulArgs &A, hipStream_t s) {
   using S = Shape<TYPE, BM, BN, WM, WN, BK, WK, NS>;
   const int tm = (A.M - 1) / BM + 1, tn = (A.N - 1) / kChannels<S, FINISH> + 1;
-  const int grid = (tm * tn + 7) / 8 * 8;  // see matmul_fits
+  // see matmul_fits and choose
+  const int grid = FINISH == kScaled ? (tm * tn + 7) / 8 * 8 : 8 * (A.whole + ((tm * tn + 7) / 8 - A.whole) * A.parts);
   const auto whole = [](const int8_t *p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)stride) & 15) == 0 && stride <= 1 << 23; };
   // (both rows of a gated channel: in 32 bits from the tile's first on)
   const bool a = whole(A.a, A.a_stride), w = whole(A.w, A.w_stride) && (FINISH != kGated || A.N * A.w_stride <= (int64_t)1 << 31);
@@ -962,9 +1015,47 @@ int best_tile(int32_t M, int32_t N, int32_t K) {
   return best;
 }
 
+// The same for products that may be cut along the inner dimension: tiles of all 256
+// CUs whole, and those of the last round, if they are no more than half of them,
+// in as many parts as there are CUs for.  A part costs its writing and, but the
+// last's, its reading, at 4 TB/s, and what waits for them 3 us.  (N: rows of w.
+// us a call: 64 x 5120 x 20480 34 -> 24, 64 x (2 x 20480) x 5120 59 -> 53, 8192 x 5120
+// x 20480 890 -> 800.)
+struct Choice {
+  int tile, parts;
+  int64_t whole, rest;  // tiles of an XCD that are whole, and cut into parts
+
+  int64_t slots() const { return parts > 1 ? 8 * rest : 0; }
+  int64_t bytes() const { return slots() * parts * kTiles[tile].bm * kTiles[tile].bn * 4; }
+};
+
+Choice choose(int32_t M, int32_t N, int32_t K) {
+  Choice best{};
+  double least = 0.0;
+  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+    const Tile &t = kTiles[i];
+    const int64_t tiles = ((int64_t)(M + (int64_t)t.bm - 1) / t.bm) * ((N + (int64_t)t.bn - 1) / t.bn);
+    const int64_t per = (tiles + 7) / 8, rest = per % 32;
+    const double one = t.us * K / 5120.0, time = (double)((per + 31) / 32) * (1.5 + one);
+    if (i == 0 || time < least) {
+      best = {i, 1, per, 0};
+      least = time;
+    }
+    const int parts = rest ? (int)std::min<int64_t>(32 / rest, K / 1024) : 1;
+    if (parts < 2) continue;
+    const double moved = 8.0 * rest * (2 * parts - 1) * t.bm * t.bn * 4 / 4e6;
+    const double cut = (double)(per / 32) * (1.5 + one) + 1.5 + one / parts + 3.0 + moved;
+    if (cut < least) {
+      best = {i, parts, per - rest, rest};
+      least = cut;
+    }
+  }
+  return best;
+}
+
 template <int TYPE, Finish FINISH>
 hipError_t matmul_of(const MatmulArgs &A, hipStream_t s) {
-  switch (best_tile(A.M, FINISH == kGated ? 2 * A.N : A.N, A.K)) {
+  switch (FINISH == kScaled ? best_tile(A.M, A.N, A.K) : A.tile) {
     case 0: return matmul_as<TYPE, FINISH, 16, 16, 16, 16, 512, 8, 4>(A, s);
     case 1: return matmul_as<TYPE, FINISH, 16, 32, 16, 16, 512, 4, 3>(A, s);
     case 2: return matmul_as<TYPE, FINISH, 32, 32, 16, 16, 512, 2, 4>(A, s);

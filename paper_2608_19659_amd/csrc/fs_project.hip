@@ -27,6 +27,26 @@ bool launch_project_few(const QuantizeArgs &X, const MatmulArgs &A, bool gated, 
   return gated ? few_finished<kGated>(X, A, s, e) : few_finished<kFinished>(X, A, s, e);
 }
 
+ProjectParts plan_project(int64_t M, int64_t w_rows, int64_t K, void *counts, void *sums, QuantizeArgs *rows, MatmulArgs *product) {
+  if (M == 0 || w_rows == 0) return {};
+  const Choice c = choose((int32_t)M, (int32_t)w_rows, (int32_t)K);
+  if (product) {
+    product->tile = c.tile;
+    product->whole = (int32_t)c.whole;  // see project_fits
+    product->parts = c.parts;
+    product->arrived = (int32_t *)counts;
+    product->partials = (int32_t *)sums;
+    rows->zero = (int32_t *)counts;
+    rows->n_zero = (int32_t)c.slots();
+  }
+  return {(size_t)c.slots() * 4, (size_t)c.bytes()};
+}
+
+bool project_fits(int64_t M, int64_t w_rows, int64_t K) {
+  const Choice c = choose((int32_t)M, (int32_t)w_rows, (int32_t)K);
+  return 8 * (c.whole + c.rest * c.parts) <= kMostBlocks;
+}
+
 hipError_t launch_quantize_normed(const QuantizeArgs &A, hipStream_t s) {
   return A.type == kF32   ? quantize_of<kF32, true>(A, s)
          : A.type == kF16 ? quantize_of<kF16, true>(A, s)

@@ -24,6 +24,8 @@ struct QuantizeArgs {
   int32_t normed;     // the rows' RMS norm first:
   const float *gain;  // factor of each column, NULL for ones
   float eps;
+  int32_t *zero;  // cleared on the way
+  int32_t n_zero;
 };
 hipError_t launch_quantize_rows(const QuantizeArgs &A, hipStream_t s);
 
@@ -44,6 +46,8 @@ struct MatmulArgs {
   int32_t activation;
   const void *residual;  // of out's type, or NULL; may be out
   int64_t residual_stride;
+  int32_t tile, whole, parts;  // set by plan_project
+  int32_t *arrived, *partials;
 };
 // Whether the product's tiles are few enough for one launch.
 bool matmul_fits(int32_t M, int32_t N, int32_t K);
@@ -56,6 +60,13 @@ bool launch_linear_few(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s
 // The same with an RMS norm before and an activation and a residual behind, or
 // gated: w has 2 N rows, the gates' and then the values'.
 hipError_t launch_quantize_normed(const QuantizeArgs &A, hipStream_t s);
+// Bytes of the counts and of the parts' sums of a product of w_rows weight rows; where
+// `rows` and `product` are given they get these places and how the product is cut.
+struct ProjectParts {
+  size_t counts, sums;
+};
+ProjectParts plan_project(int64_t M, int64_t w_rows, int64_t K, void *counts, void *sums, QuantizeArgs *rows, MatmulArgs *product);
+bool project_fits(int64_t M, int64_t w_rows, int64_t K);
 hipError_t launch_project(const MatmulArgs &A, bool gated, hipStream_t s);
 bool launch_project_few(const QuantizeArgs &X, const MatmulArgs &A, bool gated, hipStream_t s, hipError_t *e);
 

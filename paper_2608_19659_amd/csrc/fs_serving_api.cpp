@@ -118,13 +118,22 @@ fs_status matmul(const fs::MatmulArgs &A, hipStream_t stream) {
   return e == hipSuccess ? FS_OK : hip_fail(e, "matrix product launch");
 }
 
+// Codes and scales of the rows, counts and sums of the product's parts.
+fs_status project_workspace_size(int64_t M, int64_t w_rows, int64_t K, size_t *bytes) {
+  const fs_status st = fs_linear_workspace_size(M, w_rows, K, bytes);
+  if (st != FS_OK) return st;
+  const fs::ProjectParts parts = fs::plan_project(M, w_rows, K, nullptr, nullptr, nullptr, nullptr);
+  *bytes += align256(parts.counts) + align256(parts.sums);
+  return FS_OK;
+}
+
 // fs_project and fs_gated_project.
 fs_status project(fs_context *ctx, const fs_norm *norm, int64_t w_rows, bool gated, fs::QuantizeArgs rows,
                   fs::MatmulArgs product, int64_t M, int64_t N, int64_t K, void *d_workspace, size_t workspace_bytes,
                   hipStream_t stream) {
   if (!ctx) return fail(FS_ERR_INVALID_ARGUMENT, "context is NULL");
   size_t need = 0;
-  const fs_status st = fs_linear_workspace_size(M, w_rows, K, &need);
+  const fs_status st = project_workspace_size(M, w_rows, K, &need);
   if (st != FS_OK) return st;
   if (!element_type((fs_dtype)rows.type) || !element_type((fs_dtype)product.out_type))
     return fail(FS_ERR_INVALID_ARGUMENT, "unknown element type");
@@ -144,7 +153,7 @@ fs_status project(fs_context *ctx, const fs_norm *norm, int64_t w_rows, bool gat
   if (workspace_bytes < need)
     return fail(FS_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(need) + " bytes");
   if ((uintptr_t)d_workspace & 15) return fail(FS_ERR_INVALID_ARGUMENT, "the workspace must start on a multiple of 16 bytes");
-  if (!fs::matmul_fits((int32_t)M, (int32_t)w_rows, (int32_t)K)) return too_many_tiles();
+  if (!fs::project_fits(M, w_rows, K)) return too_many_tiles();
   DeviceGuard dg(ctx->device);
   if (dg.err != hipSuccess) return hip_fail(dg.err, "hipSetDevice");
   rows.codes = (int8_t *)d_workspace;
@@ -156,6 +165,9 @@ fs_status project(fs_context *ctx, const fs_norm *norm, int64_t w_rows, bool gat
   product.a = rows.codes;
   product.a_scale = rows.scale;
   product.a_padded = 1;
+  uint8_t *const counts = (uint8_t *)rows.scale + align256(4 * (size_t)M);
+  const fs::ProjectParts parts = fs::plan_project(M, w_rows, K, nullptr, nullptr, nullptr, nullptr);
+  fs::plan_project(M, w_rows, K, counts, counts + align256(parts.counts), &rows, &product);
   if (norm) {
     rows.normed = 1;
     rows.gain = norm->gain;
@@ -260,7 +272,7 @@ fs_status fs_linear(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_s
 }
 
 fs_status fs_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes) {
-  return fs_linear_workspace_size(M, N, K, bytes);
+  return project_workspace_size(M, N, K, bytes);
 }
 
 fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
@@ -288,7 +300,7 @@ fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_
 
 fs_status fs_gated_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes) {
   if (N < 0 || N > kMost / 2) return fail(FS_ERR_INVALID_ARGUMENT, "2 N must be in [0, 2^31)");
-  return fs_linear_workspace_size(M, 2 * N, K, bytes);
+  return project_workspace_size(M, 2 * N, K, bytes);
 }
 
 fs_status fs_gated_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,

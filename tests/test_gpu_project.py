@@ -300,3 +300,50 @@ def test_results_are_the_same_on_every_run(env):
         plan = fs.GatedProjectPlan(ctx, d(x), d(w), d(sw), norm=fs.Norm(d(gain), EPS), bias=d(bias))
         first = bits(plan.run().clone())
         assert all(torch.equal(bits(plan.run()), first) for _ in range(3))
+
+
+# few enough tiles, or few enough in the last round, and a long inner dimension: the
+# blocks' tiles are cut along it
+CUT = [(5, 40, 2048), (16, 200, 8192), (9, 515, 5000), (20, 1000, 20480), (33, 2000, 3001), (64, 640, 4096), (64, 5120, 20480),
+       (64, 20480, 2560), (100, 2000, 9999), (130, 1300, 4096), (300, 4000, 4096), (700, 2560, 6144), (1500, 5120, 4096),
+       (2500, 5121, 3333), (5000, 5120, 4096)]
+
+
+@pytest.mark.parametrize("M,N,K", CUT)
+def test_products_cut_along_the_inner_dimension(env, M, N, K):
+    """The same whole numbers, so the bits of the projection that is not cut; twice on
+    a workspace of any contents."""
+    fs, ctx = env
+    note(f"cut {M}x{N}x{K}")
+    g = torch.Generator(device="cuda:0").manual_seed(M + N)
+    x = torch.randn(M, K, device="cuda:0", generator=g).to(torch.bfloat16)
+    w = torch.randint(-127, 128, (2 * N, K), device="cuda:0", generator=g, dtype=torch.int8)
+    sw = torch.rand(2 * N, device="cuda:0", generator=g) / (100.0 * math.sqrt(K))
+    res = torch.randn(M, N, device="cuda:0", generator=g).to(torch.bfloat16)
+    gate, value = (fs.linear(ctx, x, w[r], sw[r], out_dtype=torch.float32) for r in (slice(0, N), slice(N, 2 * N)))
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device="cuda:0")
+    for fill in (255, 1):
+        ws.fill_(fill)
+        got = fs.project(ctx, x, w[:N], sw[:N], residual=res, workspace=ws)
+        assert torch.equal(bits(got), bits((gate + res.float()).to(torch.bfloat16)))
+        for _ in range(2):
+            got = fs.gated_project(ctx, x, w, sw, activation="none", workspace=ws)
+            assert torch.equal(bits(got), bits((gate * value).to(torch.bfloat16)))
+
+
+def test_cut_products_in_a_graph(env):
+    fs, ctx = env
+    M, N, K = 64, 640, 8192
+    x, w, sw, _, gain = inputs(M, N, K, "bf16", rows=2 * N)
+    a = (ctx, d(x), d(w), d(sw))
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda:0")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        out = fs.gated_project(*a, norm=fs.Norm(a[3][:0].new_ones(K), EPS), stream=side, workspace=ws)
+    for i in range(4):
+        a[1].copy_(torch.randn(M, K, generator=gen(i)))
+        want = fs.gated_project(*a, norm=fs.Norm(None, EPS))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bits(out), bits(want)), i
