@@ -2,24 +2,26 @@
 
 A cell is (class, TP degree, load): what one tensor-parallel replica of a
 served model does at that load.  The command runs, on one GPU, the work of one
-rank of such a replica: decoder layers whose projections are 8-bit products
-(fs_linear), whose keys and values go rotated into a paged 8-bit cache
-(fs_cache_append) and whose attention reads it (fs_cache_attention), once as
-decode steps of several batch sizes and once as the prefill of a prompt.  From
+rank of such a replica: decoder layers whose projections are 8-bit products, with
+the norm before them and the activation or the residual stream behind
+(fs_project, fs_gated_project), whose keys and values go rotated into a paged 8-bit
+cache (fs_cache_append) and whose attention reads it (fs_cache_attention), or which
+keep a decaying state a head instead (fs_state_attention, --attention state), once
+as decode steps of several batch sizes and once as the prefill of a prompt.  From
 the times come an interval for every cell's capacity and tail; the planner's own calls
 (fs_certify, fs_score_candidates) then say what the fleet would be and which
 cell is worth a real measurement first.
 
     python -m paper_2608_19659_amd.probe
     python -m paper_2608_19659_amd.probe --tp 2 4 8 --batch 1 8 64 --budget 32
+    python -m paper_2608_19659_amd.probe --attention state
 
 What a rank's time leaves out is the sum over the replica's ranks after the
 output and the down projection.  The fast side of an interval has it hidden
 behind other work, the slow side has it exposed, at the rate and latency given
 (--link-gbs, --hop-us).  The vocabulary's projection, sampling and scheduling
 are in neither.  Weights and inputs are random; nothing here depends on
-their values.  torch supplies the norms and the activation between the
-operators, memory, streams and graphs.
+their values.  torch supplies memory, streams and graphs.
 """
 from __future__ import annotations
 
@@ -36,19 +38,25 @@ from .synth import Intervals, Problem
 QUANTUM = 1.0 / 64.0  # capacity grid, req/s
 UNSERVED = 1.0e6      # tail of a cell whose load no batch sustains: seconds past every SLO, yet a number
 PAGE = 64
+ATTENTIONS = ("cache", "state")
+EPS = 2.0 ** -7  # of the norms: bfloat16's step
 
 
 @dataclass(frozen=True)
 class Decoder:
-    """A decoder's sizes.  The defaults have 31 billion weights."""
+    """A decoder's sizes.  The defaults have 31 billion weights.  attention:
+    "cache" of every token's keys and values, or "state", one matrix a head."""
     hidden: int = 5120
     q_heads: int = 40
     kv_heads: int = 8
     head_dim: int = 128
     ffn: int = 20480
     layers: int = 80
+    attention: str = "cache"
 
     def check(self, tp: int):
+        if self.attention not in ATTENTIONS:
+            raise ValueError(f"attention must be one of {', '.join(ATTENTIONS)}, got {self.attention!r}")
         if tp < 1 or self.q_heads % tp or self.kv_heads % tp or self.ffn % tp:
             raise ValueError(f"{self.q_heads} and {self.kv_heads} heads and {self.ffn} columns do not divide over TP {tp}")
 
@@ -92,6 +100,20 @@ class Shard:
             w = torch.randint(-127, 128, (n, k), dtype=torch.int8, device=dev, generator=g)
             return w, torch.full((n,), 1.0 / (73.0 * math.sqrt(k)), device=dev)  # 73: deviation of the codes
 
+        self.cu, self.held, self.max_new = i32(np.concatenate([[0], np.cumsum(new)])), i32(held), max(new)
+        self.norm = fs.Norm(None, EPS)
+        self.x = torch.randn((sum(new), decoder.hidden), device=dev, generator=g).to(torch.bfloat16)
+        self.weights = []
+        for _ in range(self.layers):
+            self.weights.append((weight((self.hq + 2 * self.hkv) * D, decoder.hidden), weight(decoder.hidden, self.hq * D),
+                                 weight(2 * self.ffn, decoder.hidden), weight(decoder.hidden, self.ffn)))
+        if decoder.attention == "state":
+            # a head keeps half of what it holds for 0.7 to 177 tokens
+            self.log_decay = -torch.exp2(torch.linspace(0.0, -8.0, self.hkv, device=dev))
+            self.index = torch.arange(len(held), dtype=torch.int32, device=dev)
+            self.states = [torch.randn((len(held), self.hkv, D, D), device=dev, generator=g) for _ in range(self.layers)]
+            torch.cuda.current_stream(dev).synchronize()
+            return
         # each sequence's pages lie side by side in the pool
         pages = [-(-h // PAGE) for h in held]
         first = np.concatenate([[0], np.cumsum(pages)])
@@ -101,16 +123,12 @@ class Shard:
         at = np.concatenate([np.arange(h - n, h) for n, h in zip(new, held)])
         self.slots = i32(np.concatenate([first[s] * PAGE + np.arange(h - n, h)
                                          for s, (n, h) in enumerate(zip(new, held))]))
-        self.positions, self.table, self.held = i32(at), i32(table), i32(held)
-        self.cu, self.max_new = i32(np.concatenate([[0], np.cumsum(new)])), max(new)
+        self.positions, self.table = i32(at), i32(table)
         angle = torch.outer(torch.arange(max(held), device=dev, dtype=torch.float32),
                             10000.0 ** (-torch.arange(0, D, 2, device=dev, dtype=torch.float32) / D))
         self.cos, self.sin = angle.cos().contiguous(), angle.sin().contiguous()
-        self.x = torch.randn((len(at), decoder.hidden), device=dev, generator=g).to(torch.bfloat16)
-        self.weights, self.caches = [], []
+        self.caches = []
         for _ in range(self.layers):
-            self.weights.append((weight((self.hq + 2 * self.hkv) * D, decoder.hidden), weight(decoder.hidden, self.hq * D),
-                                 weight(2 * self.ffn, decoder.hidden), weight(decoder.hidden, self.ffn)))
             cache = fs.KVCache.empty(int(first[-1]), self.hkv, D, PAGE, dev)
             for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
                 codes.random_(-127, 128, generator=g)
@@ -120,20 +138,21 @@ class Shard:
 
     def layer(self, i: int, h, workspace=None):
         """A layer's share of the residual stream h, added to it in place."""
-        import torch
-        from torch.nn.functional import rms_norm, silu
         (qkv, qkv_s), (out, out_s), (up, up_s), (down, down_s) = self.weights[i]
         n, D, hq, hkv = h.shape[0], self.decoder.head_dim, self.hq, self.hkv
         on = dict(stream=self.stream, workspace=workspace)
-        rows = fs.linear(self.ctx, rms_norm(h, h.shape[1:]), qkv, qkv_s, **on).view(n, hq + 2 * hkv, D)
-        q = fs.cache_append(self.ctx, self.caches[i], rows[:, hq:hq + hkv], rows[:, hq + hkv:], self.slots,
-                            rows[:, :hq], self.positions, self.cos, self.sin, stream=self.stream)
-        seen = fs.cache_attention(self.ctx, self.caches[i], q, self.table, self.held, self.cu, self.max_new, **on)
-        h.add_(fs.linear(self.ctx, seen.view(n, hq * D), out, out_s, **on))
-        wide = fs.linear(self.ctx, rms_norm(h, h.shape[1:]), up, up_s, **on)
-        gated = torch.mul(silu(wide[:, :self.ffn]), wide[:, self.ffn:])
-        h.add_(fs.linear(self.ctx, gated, down, down_s, **on))
-        return h
+        rows = fs.project(self.ctx, h, qkv, qkv_s, norm=self.norm, **on).view(n, hq + 2 * hkv, D)
+        q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+        if self.decoder.attention == "state":
+            seen = fs.state_attention(self.ctx, self.states[i], q, k, v, self.index, self.held, self.cu, self.max_new,
+                                      self.log_decay, **on)
+        else:
+            q = fs.cache_append(self.ctx, self.caches[i], k, v, self.slots, q, self.positions, self.cos, self.sin,
+                                stream=self.stream)
+            seen = fs.cache_attention(self.ctx, self.caches[i], q, self.table, self.held, self.cu, self.max_new, **on)
+        fs.project(self.ctx, seen.view(n, hq * D), out, out_s, residual=h, out=h, **on)
+        gated = fs.gated_project(self.ctx, h, up, up_s, norm=self.norm, **on)
+        return fs.project(self.ctx, gated, down, down_s, residual=h, out=h, **on)
 
     def forward(self, workspace=None):
         import torch
@@ -309,6 +328,7 @@ def main(argv=None):
     p.add_argument("--batch", type=int, nargs="+", default=[1, 4, 16, 64], help="sequences of a decode step")
     p.add_argument("--budget", type=int, default=16, help="GPUs of the fleet")
     p.add_argument("--layers", type=int, default=8, help="layers that exist at once")
+    p.add_argument("--attention", choices=ATTENTIONS, default="cache", help="what the layers keep of earlier tokens")
     p.add_argument("--link-gbs", type=float, default=153.0, help="GB/s between two GPUs")
     p.add_argument("--hop-us", type=float, default=2.0, help="microseconds of a hop between GPUs")
     p.add_argument("--json", action="store_true", help="print one JSON object")
@@ -316,7 +336,7 @@ def main(argv=None):
     if min(o.batch) < 1 or max(o.batch) > fs.MAX_SEQUENCES or o.layers < 1 or o.link_gbs <= 0.0 or o.hop_us < 0.0:
         p.error("a batch, the layers and the link's rate must be positive, and a batch at most %d" % fs.MAX_SEQUENCES)
     import torch  # before the library, so that both use one HIP runtime
-    decoder, classes = Decoder(), CLASSES
+    decoder, classes = Decoder(attention=o.attention), CLASSES
     tps = sorted(set(o.tp))
     try:
         for tp in tps:
