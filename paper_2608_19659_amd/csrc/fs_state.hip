@@ -325,8 +325,16 @@ struct ChunkShape {
   static constexpr int BYTES = SUMS ? 8 * TILE * 2 : ((3 + QUERIES) * TILE + 2 * PRODUCTS) * 2 + 2 * UNDO * 4;
   __device__ static __forceinline__ constexpr int product(int i, int t) { return i < 2 ? i : 2 * i - 2 + t; }
 
-  // Sixteen rows' same pieces lie on all banks, and two neighbouring pieces of eight.
-  __device__ static __forceinline__ int turn(int r) { return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1); }
+  // So that reads meet in no bank.  A transpose takes two neighbouring pieces of
+  // eight rows at once: the pairs c / 2 of rows 0 to 7, and of 8 to 15, all differ.  A
+  // read of 16 bytes takes 16 lanes at once, rows 0-3 and 12-15 of a piece beside
+  // rows 4-11 of its neighbour (as counted of every order tried: 4 cycles a wavefront,
+  // 8 with any other): rows 8-11 have the pairs of rows 4-7, the other place of each.
+  // (Of 64 elements two rows lie side by side: the same of row pairs.)
+  __device__ static __forceinline__ int turn(int r) {
+    const int u = D == 128 ? r : r >> 1, half = D == 128 ? 8 : 4, upper = u / half & 1;
+    return ((u ^ (upper * half / 2)) & (half - 1)) << 1 | upper;
+  }
 
   // Rows [0, count) of 64 to a tile, the last one in the place of those behind it.
   __device__ static __forceinline__ void fetch(const void *from, int64_t stride, int count, short *tile) {
