@@ -22,9 +22,32 @@ namespace {
 // than an infinity, so neither is lost in the maximum.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// A wavefront's sum or largest, in every lane: rows of 16 by shifts within them, the
+// rows by two broadcasts (lanes that get nothing take 0), the last lane's to all.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, ROWS, 0xf, true);
+}
+template <class Join>
+__device__ __forceinline__ uint32_t join_wave(uint32_t v, Join join) {
+  v = join(v, from_lane<0x111, 0xf>(v));  // by 1, 2, 4, 8
+  v = join(v, from_lane<0x112, 0xf>(v));
+  v = join(v, from_lane<0x114, 0xf>(v));
+  v = join(v, from_lane<0x118, 0xf>(v));
+  v = join(v, from_lane<0x142, 0xa>(v));  // the last of rows 0 and 2 to rows 1 and 3
+  v = join(v, from_lane<0x143, 0xc>(v));  // of row 1 to rows 2 and 3
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return join_wave(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return __uint_as_float(join_wave(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+
 template <int THREADS>
 __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds) {
-  for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  v = wave_max(v);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   v = lds[0];
@@ -84,28 +107,16 @@ struct Squares {
     sum += o.sum;
     low += o.low;
   }
-  __device__ __forceinline__ void join_wave() {
-    for (int o = 32; o; o >>= 1) {
-      sum += __shfl_xor(sum, o);
-      low += __shfl_xor(low, o);
-    }
+  __device__ __forceinline__ void join_lanes() {
+    sum = wave_sum(sum);
+    low = wave_sum(low);
   }
-  // 1 / sqrt(mean + eps)
+  // 1 / sqrt(mean + eps), by v_rsq_f32: within a step
   __device__ __forceinline__ float factor(int count, float eps) const {
-    if (sum < 0x1p100f) return 1.0f / sqrtf(sum / (float)max(count, 1) + eps);
-    return 0x1p-72f / sqrtf(low / (float)count + eps * 0x1p-144f);
+    if (sum < 0x1p100f) return __builtin_amdgcn_rsqf(sum / (float)max(count, 1) + eps);
+    return 0x1p-72f * __builtin_amdgcn_rsqf(low / (float)count + eps * 0x1p-144f);
   }
 };
-
-template <int THREADS>
-__device__ __forceinline__ Squares block_sum(Squares v, Squares *lds) {
-  v.join_wave();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = lds[0];
-  for (int i = 1; i < THREADS / 64; ++i) v.add(lds[i]);
-  return v;
-}
 
 // Eight neighbouring gains from c on (`cols` of them, ones if there are none).
 __device__ __forceinline__ void gain8(const float *gain, int c, int cols, float (&g)[8]) {
@@ -126,9 +137,7 @@ __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < A.n_zero; i += THREADS) A.zero[i] = 0;
   Squares mine = {0.0f, 0.0f};
-  const auto norm = [&](int c, float(&x)[8]) {
-    float g[8];
-    gain8(A.gain, c, A.cols, g);
+  const auto norm = [&](const float(&g)[8], float(&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       mine.add(x[i]);
@@ -141,11 +150,16 @@ __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
   float v[HELD ? HELD : 1][8];
   uint32_t most = 0;
   if constexpr (HELD > 0) {
+    float gains[NORMED ? HELD : 1][8];  // on the way with the row
+    if constexpr (NORMED) {
+#pragma unroll
+      for (int j = 0; j < HELD; ++j) gain8(A.gain, min(own + j * step, A.cols), A.cols, gains[j]);
+    }
 #pragma unroll
     for (int j = 0; j < HELD; ++j) load8_of<TYPE>(A.x, at, min(own + j * step, A.cols), A.cols, whole, v[j]);
     if constexpr (NORMED) {
 #pragma unroll
-      for (int j = 0; j < HELD; ++j) norm(min(own + j * step, A.cols), v[j]);
+      for (int j = 0; j < HELD; ++j) norm(gains[j], v[j]);
     }
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
@@ -153,11 +167,26 @@ __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
   } else {
     for (int64_t c = own; c < A.cols; c += step) {
       load8_of<TYPE>(A.x, at, (int)c, A.cols, whole, v[0]);
-      if constexpr (NORMED) norm((int)c, v[0]);
+      if constexpr (NORMED) {
+        float g[8];
+        gain8(A.gain, (int)c, A.cols, g);
+        norm(g, v[0]);
+      }
       for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[0][i]));
     }
   }
+  if constexpr (NORMED) {
+    mine.join_lanes();
+    if ((threadIdx.x & 63) == 0) squares[threadIdx.x >> 6] = mine;
+  }
   const float a = __uint_as_float(block_max<THREADS>(most, lds));
+  float factor = 1.0f;
+  if constexpr (NORMED) {  // all wavefronts' squares are there
+    mine = squares[min((int)threadIdx.x & 63, THREADS / 64 - 1)];
+    if ((threadIdx.x & 63) >= THREADS / 64) mine = {0.0f, 0.0f};
+    mine.join_lanes();
+    factor = mine.factor(A.cols, A.eps);
+  }
   const bool zero = a < kTiny;
   const float inverse = zero ? 0.0f : 127.0f / a;
   int8_t *const out = A.codes + row * A.code_stride;
@@ -177,12 +206,7 @@ __global__ __launch_bounds__(THREADS) void k_quantize_rows(QuantizeArgs A) {
       store_codes8(out, (int)c, A.cols, v[0], inverse);
     }
   }
-  if constexpr (NORMED) {
-    const float factor = block_sum<THREADS>(mine, squares).factor(A.cols, A.eps);
-    if (threadIdx.x == 0) A.scale[row] = zero ? 0.0f : a * factor / 127.0f;
-  } else {
-    if (threadIdx.x == 0) A.scale[row] = zero ? 0.0f : a / 127.0f;
-  }
+  if (threadIdx.x == 0) A.scale[row] = zero ? 0.0f : (NORMED ? a * factor : a) / 127.0f;
 }
 
 // 16 codes of a row (of K > 0) from column k on.  load() only asks for the
@@ -794,19 +818,29 @@ __device__ __forceinline__ void codes_in_lds(const int8_t *raw, int raw_pitch, i
   const int8_t *const from = raw + row * raw_pitch;
   uint32_t most = 0;
   Squares sum = {0.0f, 0.0f};
+  constexpr int HELD = NORMED ? 2 : 1;
+  float normed[HELD][8] = {};  // of a row of two steps or less, between the passes
+  const auto norm = [&](int c, float(&v)[8]) {
+    float g[8];
+    load8<XTYPE>(from, c, true, v);
+    gain8(gain, c, K, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sum.add(v[i]);
+      v[i] *= g[i];
+      most = max(most, magnitude(v[i]));
+    }
+  };
   if (row < M) {
     if constexpr (NORMED) {
-      for (int c = first; c < K; c += step) {
-        float v[8], g[8];
-        load8<XTYPE>(from, c, true, v);
-        gain8(gain, c, K, g);
+      if (K <= HELD * step) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sum.add(v[i]);
-          most = max(most, magnitude(v[i] * g[i]));
-        }
+        for (int j = 0; j < HELD; ++j)
+          if (first + j * step < K) norm(first + j * step, normed[j]);
+      } else {
+        for (int c = first; c < K; c += step) norm(c, normed[0]);
       }
-      sum.join_wave();
+      sum.join_lanes();
     } else if constexpr (XTYPE == kF32) {
       for (int c = first; c < K; c += step) {
         float v[8];
@@ -825,7 +859,7 @@ __device__ __forceinline__ void codes_in_lds(const int8_t *raw, int raw_pitch, i
       most = magnitude(value16<XTYPE>(max(two.x, two.y)));
     }
   }
-  for (int o = 32; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  most = wave_max(most);
   if (lane == 0) most_of[wave] = most;
   if constexpr (NORMED) {
     if (lane == 0) squares[wave] = sum;
@@ -838,7 +872,13 @@ __device__ __forceinline__ void codes_in_lds(const int8_t *raw, int raw_pitch, i
   const float a = __uint_as_float(most);
   const bool zero = a < kTiny;
   const float inverse = zero ? 0.0f : 127.0f / a;
-  if (row < M) {
+  if (NORMED && row < M && K <= HELD * step) {
+#pragma unroll
+    for (int j = 0; j < HELD + 1; ++j) {  // a row's codes end in zeros, less than a step of them
+      const int c = first + j * step;
+      if (c < pitch) *(int2 *)(codes + row * pitch + c) = codes8(normed[j < HELD ? j : 0], j < HELD && c < K ? inverse : 0.0f);
+    }
+  } else if (row < M) {
     for (int c = first; c < pitch; c += step) {
       float v[8] = {};
       if (c < K) load8<XTYPE>(from, c, true, v);
@@ -852,6 +892,8 @@ __device__ __forceinline__ void codes_in_lds(const int8_t *raw, int raw_pitch, i
       }
       *(int2 *)(codes + row * pitch + c) = codes8(v, c < K ? inverse : 0.0f);
     }
+  }
+  if (row < M) {
     if (first == 0) {
       if constexpr (NORMED) {
         sum = squares[row * each];
@@ -965,6 +1007,7 @@ hipError_t quantize_as(const QuantizeArgs &A, hipStream_t s) {
 template <int TYPE, bool NORMED>
 hipError_t quantize_of(const QuantizeArgs &A, hipStream_t s) {
   // few rows: all of a CU's wavefronts on one; many: smaller blocks
+  if (A.rows <= 256 && A.cols <= 8192) return quantize_as<TYPE, 1024, 1, NORMED>(A, s);
   if (A.rows <= 256 && A.cols <= 3 * 8192) return quantize_as<TYPE, 1024, 3, NORMED>(A, s);
   if (A.cols <= 4 * 2048) return quantize_as<TYPE, 256, 4, NORMED>(A, s);
   if (A.cols <= 10 * 2048) return quantize_as<TYPE, 256, 10, NORMED>(A, s);
