@@ -61,8 +61,15 @@ template <int TYPE>
 __device__ __forceinline__ void load8_of(const void *x, int64_t row, int c, int cols, bool whole, float (&v)[8]) {
   if (cols - c >= 8) {
     load8<TYPE>(x, row + c, whole, v);
+  } else if (c < cols) {  // all loads under way together, the last element's in the place of those behind it
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_value<TYPE>(x, row + c + min(i, cols - c - 1));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= cols - c) v[i] = 0.0f;
   } else {
-    for (int i = 0; i < 8; ++i) v[i] = i < cols - c ? load_value<TYPE>(x, row + c + i) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
   }
 }
 
