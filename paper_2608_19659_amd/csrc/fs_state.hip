@@ -389,7 +389,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   extern __shared__ __attribute__((aligned(1024))) short state_lds[];
   short *const lk = state_lds, *const lv = lk + S::KEYS * S::TILE, *const lq = lv + S::VALUES * S::TILE, *const lp = lq + S::QUERIES * S::TILE;
   float *const undo = (float *)(lp + 2 * S::PRODUCTS);  // of a row of products, what undoes its factor
-  const Segment seg = find_segment(A, blockIdx.x);
+  const Segment seg = find_segment(A, blockIdx.y);
   const int number = __builtin_amdgcn_readfirstlane(seg.number), before = __builtin_amdgcn_readfirstlane(seg.before);
   if (number < 0) return;
   Sequence q = seg.sequence;  // the block's: known to be so to the compiler as well
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   q.state = __builtin_amdgcn_readfirstlane(q.state);
   q.fresh = __builtin_amdgcn_readfirstlane(q.fresh);
   if (q.count <= A.step_most) return;
-  const int start = number * A.segment, tokens = min(A.segment, q.count - start), h = blockIdx.y;
+  const int start = number * A.segment, tokens = min(A.segment, q.count - start), h = blockIdx.x;
   const int group = A.n_q_heads / A.n_heads, lane = threadIdx.x & 63, g = lane >> 4, own = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool last = start + tokens == q.count;
@@ -744,19 +744,37 @@ __global__ void k_check_state(StateArgs A, int32_t *flag) {
 // Sequences of up to this many new tokens go token by token.
 constexpr int kStepMost = 8;
 
-// Tokens of a segment, so many that all sequences' tokens make about 256 segments of
-// a head, one for each CU.
-int segment_tokens(int64_t n_tokens, int64_t n_heads) {
+// The least tokens of a segment: so many that all tokens make about 256 segments of a
+// head, one for each CU.
+int segment_least(int64_t n_tokens, int64_t n_heads) {
   const int64_t L = (n_tokens * n_heads / 256 + kChunk - 1) / kChunk * kChunk;
   return (int)std::max<int64_t>(kChunk, std::min<int64_t>(L, 1 << 30));
 }
-int64_t segments_at_most(int64_t n_tokens, int64_t n_seqs, int64_t n_heads) {
-  return n_tokens / segment_tokens(n_tokens, n_heads) + n_seqs;
+
+// Tokens of a segment, that many or more: those that take least if the tokens are as
+// many sequences of max_q as they make.  Times in us of what is measured at head_dim
+// 128 (a CU has one block of outputs then, two at 64): 2.2 for a chunk and query head, 1.5 for a chunk
+// beside, 2 for a chunk of a segment's sum, what launches and starts take; a segment a
+// sequence needs no sums.
+int segment_tokens(const StateArgs &A) {
+  const int least = segment_least(A.n_tokens, A.n_heads);
+  const int64_t sequences = std::max<int64_t>(1, (A.n_tokens + A.max_q / 2) / A.max_q), slots = A.head_dim == 128 ? 256 : 512;
+  const double chunk = 1.5 + 2.2 * (A.n_q_heads / A.n_heads);
+  const auto time = [&](int64_t L) {
+    const int64_t parts = (A.max_q + L - 1) / L, rounds = (sequences * parts * A.n_heads + slots - 1) / slots, chunks = std::min<int64_t>(L, A.max_q + kChunk - 1) / kChunk;
+    return (double)rounds * ((double)chunks * chunk + 6.0) + (parts > 1 ? (double)rounds * ((double)chunks * 2.0 + 5.0) + 6.0 : 0.0);
+  };
+  int64_t best = least;
+  for (int i = 1; i <= 8; ++i) {
+    const int64_t L = i < 8 ? least + (int64_t)least / kChunk * i / 2 * kChunk : (A.max_q + kChunk - 1) / kChunk * kChunk;
+    if (L >= least && time(L) < time(best)) best = L;
+  }
+  return (int)std::min<int64_t>(best, 1 << 30);
 }
-// Of sequences of more than a segment's L tokens: n of them have at most n / L + 1,
-// less than 2 n / L.
+// Places of sequences of more than a segment's L tokens: n of them have at most
+// n / L + 1 segments, less than 2 n / L.
 int64_t places_at_most(int64_t n_tokens, int64_t n_heads) {
-  const int64_t L = segment_tokens(n_tokens, n_heads);
+  const int64_t L = segment_least(n_tokens, n_heads);
   return n_tokens > L ? 2 * n_tokens / L : 0;
 }
 
@@ -798,13 +816,18 @@ hipError_t steps_of(const StateArgs &A, int64_t joined, hipStream_t s) {
 
 template <int TYPE, int D>
 hipError_t state_of(StateArgs A, hipStream_t s) {
-  A.segment = segment_tokens(A.n_tokens, A.n_heads);
+  A.max_q = std::min(A.max_q, A.n_tokens);
+  A.segment = segment_tokens(A);
   A.n_places = (int32_t)places_at_most(A.n_tokens, A.n_heads);
   A.step_most = kStepMost;
   if (A.max_q <= kStepMost) return steps_of<TYPE, D>(A, 0, s);
   if (A.n_seqs == 1) A.step_most = 0;  // no launch for what may be a single token
   const bool one = A.segment >= A.max_q;  // a segment a sequence
-  const dim3 grid(one ? (unsigned)A.n_seqs : (unsigned)segments_at_most(A.n_tokens, A.n_seqs, A.n_heads), A.n_heads);
+  // Heads first: blocks that find no segment come last.  (Between the others they left
+  // them to half of the CUs: one prompt of 12260 tokens beside 15 single ones, 12 heads,
+  // 148 us of the outputs instead of 92.)  No more than 256 segments and a sequence's
+  // last, see segment_least.
+  const dim3 grid(A.n_heads, one ? (unsigned)A.n_seqs : (unsigned)(A.n_tokens / A.segment + A.n_seqs));
   hipError_t e = one ? hipSuccess : chunks_of<TYPE, D, true>(grid, A, s);
   // at most so many sequences have more tokens than a segment
   const int64_t joined = one ? 0 : std::min<int64_t>(A.n_seqs, A.n_tokens / A.segment);
