@@ -555,10 +555,12 @@ typedef enum fs_activation {
 /* out[m][n] = act(y[m][n]) + residual[m][n], with y the projection of fs_linear
  * behind the norm (norm NULL: none), its bias (NULL: none) among it.  residual
  * [M][N] is of out_type (NULL: none); it may be out itself, with out's stride, and
- * may not overlap it otherwise.  All in binary32, rounded once; without norm,
- * activation and residual the bits of fs_linear.  Activations are off by less than
+ * may not overlap it otherwise (nor x in any way).  All in binary32, rounded once;
+ * without norm, activation and residual the bits of fs_linear.  Activations are off by less than
  * 2^-20 (1 + |y|) |act(y)| + 2^-22 |y|.  A row with a NaN or an infinity, in x or
- * x * gain, gives NaN. */
+ * x * gain, gives NaN; one whose x * gain are all below 2^-100 counts as zeros.
+ * Where few tiles would leave CUs idle a product is cut along K and its parts added in
+ * the workspace, by the last block of a tile to arrive: equal run to run. */
 fs_status fs_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
 fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
                      const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
@@ -694,10 +696,11 @@ typedef struct fs_state_pool {
  * may have one state.  out: [n_tokens][n_q_heads][head_dim] contiguous, of q's type.
  *
  * Sums and states are binary32.  Sequences of up to 8 new tokens go token by token.
- * Longer ones go in chunks of 64, where states, decayed values and decayed products
- * of queries and keys enter the products as pairs of bfloat16 values, 16 bits of
- * each: results are off by about 2^-17 of the sums' terms before they are rounded.
- * Equal run to run.  What a NaN or an infinity reaches by the formula (its own
+ * Longer ones go in chunks of 64, where states and the decayed products of queries and
+ * keys enter the products as two values of the element type (16 bits of each in
+ * bfloat16, 22 in binary16) and decayed values as three or two (24 or 22 bits): outputs
+ * are off by about 2^-17 of their sums' terms before they are rounded, states by about
+ * a rounding of binary32.  Equal run to run.  What a NaN or an infinity reaches by the formula (its own
  * token's outputs and later ones, the state) is not finite, and nothing else; a
  * state beyond 2^127 counts as infinite.
  *

@@ -1069,8 +1069,8 @@ int best_tile(int32_t M, int32_t N, int32_t K) {
 // CUs whole, and those of the last round, if they are no more than half of them,
 // in as many parts as there are CUs for.  A part costs its writing and, but the
 // last's, its reading, at 4 TB/s, and what waits for them 3 us.  (N: rows of w.
-// us a call: 64 x 5120 x 20480 34 -> 24, 64 x (2 x 20480) x 5120 59 -> 53, 8192 x 5120
-// x 20480 890 -> 800.)
+// us a call, with the quantisation, weights from memory, best uncut and cut: 64 x 5120 x
+// 20480 44 and 36, 64 x (2 x 20480) x 5120 58.9 and 58.0, 8192 x 5120 x 20480 872 and 852.)
 struct Choice {
   int tile, parts;
   int64_t whole, rest;  // tiles of an XCD that are whole, and cut into parts

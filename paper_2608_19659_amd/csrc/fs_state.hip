@@ -161,7 +161,10 @@ __device__ __forceinline__ void join_segments(const StateArgs &A, int block) {
 
 // ------------------------------------------------------------- token by token --
 // A block has COLS columns of a head's state, a thread HELD pieces of four in
-// rows ROWS apart.  Blocks behind those of the last sequence join segments, whose own
+// rows ROWS apart: the state is read and written once, all of it under way at once, and
+// columns need nothing of each other.  Few columns a block where heads are few, so that
+// more CUs load.  64 users of 8 heads 14.9 us (4.6 TB/s; a copy 5.2), one user of one
+// head 4.5, the time of three loads that wait for each other and of the launch.  Blocks behind those of the last sequence join segments, whose own
 // sums are there by then (of WIDE elements a thread; 0: none).
 constexpr int kStepHeads = 8;  // query heads at a time
 
@@ -380,6 +383,15 @@ struct ChunkShape {
 // are operands without a move.
 __device__ __forceinline__ constexpr int token(int t, int e, int g) { return t * 32 + (e >> 2) * 16 + 4 * g + (e & 3); }
 
+// One barrier a query head: while a head's outputs are made, the next one's products
+// of queries and keys are, a pair of query and key tiles a wavefront, and a later one's
+// queries are loaded.  The states' columns make the wavefronts independent but for
+// these products; every wavefront reads all of a head's queries from LDS, and that
+// beside the products' own chain is what bounds it.  Of 4 prompts of 2048 tokens (40
+// query heads over 8) 57 us, 17 of the segments' own sums, 7.8 of joining them; bytes'
+// time 40.  Counted there: matrix units 35 % busy, LDS 28 %, a fifteenth of that conflicts.
+// (Operands each awaited by itself 72 us, loads through registers 107, four wavefronts
+// of 32 columns 107.)
 template <class S>
 __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   constexpr int TYPE = S::TYPE, D = S::D, KT = D / 16, KS = D / 32;  // tiles and steps of a key's elements

@@ -93,9 +93,10 @@ def state_attend(q, k, v, state, log_decay, scale):
     by token in binary64.  q [n, heads, D], k, v [n, state heads, D], state
     [state heads, D, D], log_decay [state heads].
 
-    The bounds: every decayed product of a key and a value enters the state with
-    2^-17 of itself lost where it is held as two bfloat16 values (2^-9 of the first's
-    rounding, 2^-9 of that of the rest, half a step each); its decay is 2 to a power
+    The bounds: every decayed product of a key and a value may enter the state with
+    2^-17 of itself lost, as if it were held as two bfloat16 values (2^-9 of the first's
+    rounding, 2^-9 of that of the rest, half a step each; the states' precision has a
+    test of its own); its decay is 2 to a power
     below 128 where anything is left, which is off by 2^-24 of itself: 2^-17 again;
     and each of up to n additions and decays rounds by 2^-24 of the sum of the terms'
     sizes: as long as that sum's own decay counts fewer than n of them.  An output multiplies that by a query and adds the roundings of the

@@ -210,6 +210,26 @@ def test_a_prompt_in_parts_is_the_prompt(env):
     assert (b["states"].cpu()[whole.index[0]].double() - want).norm() < 1e-4 * want.norm()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [7, 64, 1000])
+def test_states_are_binary32(env, n, dtype):
+    """Every term of a state may lose 2^-23 of itself (22 bits) and is added with some
+    70 others and partial sums, each rounded by 2^-24 of what is there: if these fall
+    either way sqrt(70) of them, together less than 2^-20 of the terms' sizes in the
+    root mean square."""
+    fs, ctx = env
+    b = Batch([n], [5], [True], 3, 1, 64, dtype)
+    a = b.device()
+    fs.state_attention(ctx, **a)
+    got = a["states"].cpu()[b.index[0]].double()
+    _, want, _, room = ref.state_attend(b.q, b.k, b.v, b.pool[b.index[0]], b.decay, b.scale)
+    lam = torch.exp(b.decay.double())[:, None, None]
+    size = b.pool[b.index[0]].double().abs()
+    for t in range(n):
+        size = lam * size + (b.k[t].double()[:, :, None] * b.v[t].double()[:, None, :]).abs()
+    assert (got - want).norm() < 2.0 ** -20 * size.norm()
+
+
 def test_results_are_the_same_on_every_run(env):
     fs, ctx = env
     for news in ([1] * 9, [300, 1, 70], [1200]):
