@@ -488,7 +488,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   S::places_of_rows(at_rows);
   bool fetched = false;
   for (int c = 0, buf = 0, q_buf = 0; c < tokens; c += kChunk, buf = (buf + 1) & (S::KEYS - 1)) {
-    const int n = min(kChunk, tokens - c);
+    const int n = S::SUMS ? kChunk : min(kChunk, tokens - c);  // a segment's own sum is of whole chunks
     const short *const k = lk + buf * S::TILE;
     const bool more = c + kChunk < tokens;
     // behind the loads of this chunk: four stores of the last one, which was whole, and later queries
