@@ -695,8 +695,8 @@ typedef struct fs_state_pool {
  * without new tokens leaves its state as it is.  No two sequences with new tokens
  * may have one state.  out: [n_tokens][n_q_heads][head_dim] contiguous, of q's type.
  *
- * Sums and states are binary32.  Sequences of up to 8 new tokens go token by token.
- * Longer ones go in chunks of 64, where states and the decayed products of queries and
+ * Sums and states are binary32.  Sequences of up to 8 new tokens go token by token
+ * (in a call of one sequence: if max_q is at most 8).  Others go in chunks of 64, where states and the decayed products of queries and
  * keys enter the products as two values of the element type (16 bits of each in
  * bfloat16, 22 in binary16) and decayed values as three or two (24 or 22 bits): outputs
  * are off by about 2^-17 of their sums' terms before they are rounded, states by about

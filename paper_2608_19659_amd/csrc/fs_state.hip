@@ -160,12 +160,13 @@ __device__ __forceinline__ void join_segments(const StateArgs &A, int block) {
 }
 
 // ------------------------------------------------------------- token by token --
-// A block has COLS columns of a head's state, a thread HELD pieces of four in
-// rows ROWS apart: the state is read and written once, all of it under way at once, and
-// columns need nothing of each other.  Few columns a block where heads are few, so that
-// more CUs load.  64 users of 8 heads 14.9 us (4.6 TB/s; a copy 5.2), one user of one
-// head 4.5, the time of three loads that wait for each other and of the launch.  Blocks behind those of the last sequence join segments, whose own
-// sums are there by then (of WIDE elements a thread; 0: none).
+// A block has COLS columns of a head's state, a thread HELD pieces of four in rows
+// ROWS apart: the state is read and written once, all of it under way at once, and
+// columns need nothing of each other.  Few columns a block where heads are few, so
+// that more CUs load.  64 users of 8 heads 14.9 us (4.6 TB/s; a copy 5.2), one user of
+// one head 4.5, the time of a launch and of loads that wait for each other.  Blocks
+// behind those of the last sequence join segments, whose own sums are there by then (of
+// WIDE elements a thread; 0: none).
 constexpr int kStepHeads = 8;  // query heads at a time
 
 template <int TYPE, int D, int COLS, int WIDE>
@@ -179,11 +180,11 @@ __global__ __launch_bounds__(kThreads) void k_state_step(StateArgs A) {
   const int group = A.n_q_heads / A.n_heads, row = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
   const Sequence q = sequence(A, blockIdx.y);
   if (q.count < 1 || q.count > A.step_most) return;
-  const float l = power(log2_decay(A, h), 1);
   float *const at = q.state < 0 ? nullptr : A.states + ((int64_t)q.state * A.n_heads + h) * D * D + part * COLS + col;
   float4v s[HELD];
 #pragma unroll
   for (int i = 0; i < HELD; ++i) s[i] = q.fresh ? float4v{0, 0, 0, 0} : *(const float4v *)(at + (int64_t)(i * ROWS + row) * D);
+  const float l = exact_power(A, h, 1);  // while the state is on its way
   for (int t = q.first; t < q.first + q.count; ++t) {
     float4v v;
 #pragma unroll
