@@ -487,7 +487,8 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
   const int out_at = own * A.n_q_heads * (D * 2) + g * 8;  // bytes; 64 rows fit 32 bits
   typename S::Rows at_rows;
   S::places_of_rows(at_rows);
-  bool fetched = false;
+  bool fetched = false, made = false;  // the last phase's queries; this chunk's first products
+  int p_buf = 0;
   for (int c = 0, buf = 0, q_buf = 0; c < tokens; c += kChunk, buf = (buf + 1) & (S::KEYS - 1)) {
     const int n = S::SUMS ? kChunk : min(kChunk, tokens - c);  // a segment's own sum is of whole chunks
     const short *const k = lk + buf * S::TILE;
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
         for (int e = 0; e < 4; ++e) past_undo[e] = TYPE == kF16 ? __shfl(inverse, 4 * g + e) : 1.0f;
       }
       // 16 rows of <q, k>, decayed, by pairs of 16 keys, to LDS as operands
-      const auto products = [&](const short *lq_of, int to) {
+      const auto products = [&](const short *k, const short *lq_of, int to) {
         if (2 * mine_t > mine_i) return;
         short8v mine[KS];
 #pragma unroll
@@ -585,17 +586,26 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
           if (TYPE == kF16 && g == 0) undo[to * S::UNDO + S::product(mine_i, t) * 16 + own] = inverse;
         }
       };
-      // The first head's products, then each head's outputs beside the next one's products.
-      products(lq + q_buf * S::TILE, 0);
-      arrive<63>();
-      if (more) fetch_v(c + kChunk, 0);  // all have this chunk's values
+      // The first head's products, then each head's outputs beside the next one's
+      // products; beside the last one's the next chunk's first, whose keys are there two
+      // phases after they were asked for.  The next chunk's values are asked for behind
+      // a barrier, when all have this one's.
+      const bool early = more && group >= 3;
+      if (!made) {
+        products(k, lq + q_buf * S::TILE, p_buf);
+        arrive<63>();
+        if (more) fetch_v(c + kChunk, 0);
+      }
       for (int head = 0; head < group; ++head) {
-        const short *const lq_now = lq + q_buf * S::TILE, *const lp_now = lp + (head & 1) * S::PRODUCTS;
+        const short *const lq_now = lq + q_buf * S::TILE, *const lp_now = lp + p_buf * S::PRODUCTS;
         q_buf = q_buf == S::QUERIES - 1 ? 0 : q_buf + 1;
+        const bool values = made && head == 1 && more;
+        if (values) fetch_v(c + kChunk, 0);
         fetched = fetch_next_q();
         // (One wavefront of a SIMD before its outputs, the other behind them.)
-        const bool ahead = head + 1 < group;
-        if (ahead && wave < 4) products(lq + q_buf * S::TILE, (head + 1) & 1);
+        const bool ahead = head + 1 < group || early;
+        const short *const k_next = head + 1 < group ? k : lk + (buf ^ 1) * S::TILE;
+        if (ahead && wave < 4) products(k_next, lq + q_buf * S::TILE, p_buf ^ 1);
         // Two times two tiles of 16 rows of outputs, all of their operands on the way from
         // LDS before the first product: a wavefront that waits for each has one other to
         // wait behind.
@@ -637,7 +647,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) sum = multiply<TYPE>(v[t], w[i][t][p], sum);
                 if constexpr (TYPE == kF16) {
-                  const float inverse = undo[(head & 1) * S::UNDO + S::product(u * 2 + i, t) * 16 + own];
+                  const float inverse = undo[p_buf * S::UNDO + S::product(u * 2 + i, t) * 16 + own];
 #pragma unroll
                   for (int e = 0; e < 4; ++e) o[i][e] = __builtin_fmaf(sum[e], inverse, o[i][e]);
                 } else {
@@ -661,16 +671,19 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
             }
           }
         }
-        if (ahead && wave >= 4) products(lq + q_buf * S::TILE, (head + 1) & 1);
+        if (ahead && wave >= 4) products(k_next, lq + q_buf * S::TILE, p_buf ^ 1);
         // The next one's products need the queries after it: behind them what this
         // one has asked for, and its stores.
         if (head + 1 < group) {
           if (n < kChunk) arrive<0>();
           else if (S::QUERIES == 3) arrive<4>();
-          else if (head == 0 && more) fetched ? arrive<4 + 3 * S::PIECES>() : arrive<4 + 2 * S::PIECES>();
+          else if (head == 0 && more && !made) fetched ? arrive<4 + 3 * S::PIECES>() : arrive<4 + 2 * S::PIECES>();
+          else if ((head == 0 && more) || values) fetched ? arrive<4 + 2 * S::PIECES>() : arrive<4 + S::PIECES>();
           else fetched ? arrive<4 + S::PIECES>() : arrive<4>();
         }
+        p_buf ^= 1;
       }
+      made = early;
       if (last && q.state < 0 && !more) return;
     }
     // the state after the chunk

@@ -118,3 +118,26 @@ def state_attend(q, k, v, state, log_decay, scale):
     held = 1.0 / max(1e-9, 1.0 - float(lam.max()))  # tokens that count: the sum of a term's decays
     steps = 2 * 2.0 ** -17 + 2.0 ** -24 * (min(n, held) + D)
     return out, S, most * (steps + 3 * 2.0 ** -17), size * steps
+
+
+def state_attend_at_once(q, k, v, state, log_decay, scale):
+    """The same by its closed form, all tokens at once (n^2 products a head; on the
+    inputs' device): o_i = scale (l^(i+1) S^T q_i + sum_(j<=i) l^(i-j) <q_i, k_j> v_j)."""
+    n, heads, D = q.shape
+    H = k.shape[1]
+    t = torch.arange(n, device=q.device, dtype=torch.float64)
+    rate = log_decay.double()[:, None, None]
+    fade = torch.where(t[:, None] >= t[None], torch.exp(rate * (t[:, None] - t[None]).clamp(min=0)), 0.0)  # [H, n, n]
+    since, left = torch.exp(rate * (t[:, None] + 1)), torch.exp(rate * (n - 1 - t)[:, None])  # [H, n, 1]
+    end = torch.exp(rate * n)
+
+    def values(q, k, v, S):
+        q, k, v = (x.transpose(0, 1).contiguous() for x in (q, k, v))  # [heads, n, D]
+        q = q.view(H, heads // H, n, D)
+        out = (q @ k.transpose(1, 2)[:, None] * fade[:, None]) @ v[:, None] + since[:, None] * (q @ S[:, None])
+        return out.reshape(heads, n, D).transpose(0, 1), end * S + (k * left).transpose(1, 2) @ v
+    out, S = values(q.double(), k.double(), v.double(), state.double())
+    most, size = values(q.double().abs(), k.double().abs(), v.double().abs(), state.double().abs())
+    held = 1.0 / max(1e-9, 1.0 - float(torch.exp(rate).max()))
+    steps = 2 * 2.0 ** -17 + 2.0 ** -24 * (min(n, held) + D)
+    return out * scale, S, most * abs(scale) * (steps + 3 * 2.0 ** -17), size * steps

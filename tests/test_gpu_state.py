@@ -121,6 +121,66 @@ def test_long_segments(env):
     run(env, Batch([2500, 300], [3, 0], [True, True], 64, 1, 64, "bf16", decay=[-(2.0 ** -(s % 9)) for s in range(64)]))
 
 
+# (heads, sequences and tokens enough that a block has several chunks, one or two of a
+# segment's own sum among them)
+MANY = [(128, 64, 3, [330, 300], 0), (128, 96, 5, [257, 64, 400], 0), (64, 200, 4, [449, 130], 0), (128, 128, 1, [200, 450], 0),
+        (64, 128, 2, [700, 9], 0), (128, 64, 3, [330, 300], 3), (64, 128, 3, [250, 251], 1), (128, 20, 3, [3000], 0),
+        (64, 40, 3, [5000, 1000], 0), (128, 20, 4, [2000, 1999], 1)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,heads,group,news,pad", MANY, ids=str)
+def test_blocks_of_many_chunks(env, D, heads, group, news, pad, dtype):
+    fs, ctx = env
+    note(f"many chunks D{D} {heads}x{group} {news} pad{pad} {dtype}")
+    g = torch.Generator(device="cuda:0").manual_seed(sum(news) + heads)
+    T, S = sum(news), len(news)
+    wide = torch.randn(T, heads * (group + 2) * D + pad, device="cuda:0", generator=g).to(TYPES[dtype])
+    cut = lambda a, n: wide[:, a * D:(a + n) * D].unflatten(1, (n, D))  # noqa: E731
+    q, k, v = cut(0, heads * group), cut(heads * group, heads), cut(heads * (group + 1), heads)
+    pool = torch.randn(S, heads, D, D, device="cuda:0", generator=g) * 3
+    start = pool.clone()
+    decay = -torch.exp2(-torch.linspace(0, 9, heads, device="cuda:0"))
+    cu = [0]
+    for n in news:
+        cu.append(cu[-1] + n)
+    held = [0] + [7] * (S - 1)
+    out = fs.state_attention(ctx, pool, q, k, v, i32(list(range(S))), i32([n + h for n, h in zip(news, held)]), i32(cu), max(news), decay)
+    for s, n in enumerate(news):
+        rows = slice(cu[s], cu[s] + n)
+        for h in range(0, heads, 16):  # so many heads at a time
+            of = slice(h, min(h + 16, heads))
+            qs = slice(of.start * group, of.stop * group)
+            first = start[s, of] if held[s] else torch.zeros_like(start[s, of])
+            want, state, room, state_room = ref.state_attend_at_once(q[rows, qs], k[rows, of], v[rows, of], first, decay[of], D ** -0.5)
+            got = out[rows, qs].double()
+            room = room + (want.abs() + room) * STEP[dtype] + (2.0 ** -25 if dtype == "f16" else 0.0)
+            assert ((got - want).abs() <= room).all(), (s, h)
+            assert ((pool[s, of].double() - state).abs() <= state_room + 2.0 ** -149).all(), (s, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("at", [0, 63, 64, 130, 199])
+def test_no_numbers_in_blocks_of_many_chunks(env, at, dtype):
+    fs, ctx = env
+    heads, group, D, n = 200, 3, 64, 200
+    g = torch.Generator(device="cuda:0").manual_seed(at)
+    make = lambda h: torch.randn(2 * n, h, D, device="cuda:0", generator=g).to(TYPES[dtype])  # noqa: E731
+    q, k, v = make(heads * group), make(heads), make(heads)
+    decay = -torch.full((heads,), 0.02, device="cuda:0")
+    where = (i32([0, 1]), i32([n, n]), i32([0, n, 2 * n]), n, decay)
+    pools = [torch.zeros(2, heads, D, D, device="cuda:0") for _ in range(2)]
+    want = fs.state_attention(ctx, pools[0], q, k, v, *where)
+    v[n + at, 7, 9] = math.nan
+    got = fs.state_attention(ctx, pools[1], q, k, v, *where)
+    hit = torch.zeros_like(got, dtype=torch.bool)
+    hit[n + at:, 7 * group:8 * group, 9] = True
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], want[~hit])
+    hit = torch.zeros_like(pools[0], dtype=torch.bool)
+    hit[1, 7, :, 9] = True
+    assert torch.isnan(pools[1][hit]).all() and torch.equal(pools[1][~hit], pools[0][~hit])
+
+
 @pytest.mark.parametrize("n", [1, 8, 100, 600])
 @pytest.mark.parametrize("decay", [0.0, -1e-7, -30.0, -1e30, -math.inf])
 def test_decays_from_all_to_nothing(env, n, decay):
