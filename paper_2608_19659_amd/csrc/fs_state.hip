@@ -164,7 +164,7 @@ __device__ __forceinline__ void join_segments(const StateArgs &A, int block) {
 // ROWS apart: the state is read and written once, all of it under way at once, and
 // columns need nothing of each other.  Few columns a block where heads are few, so
 // that more CUs load.  64 users of 8 heads 14.9 us (4.6 TB/s; a copy 5.2), one user of
-// one head 4.5, the time of a launch and of loads that wait for each other.  Blocks
+// one head 4.6, the time of a launch and of loads that wait for each other.  Blocks
 // behind those of the last sequence join segments, whose own sums are there by then (of
 // WIDE elements a thread; 0: none).
 constexpr int kStepHeads = 8;  // query heads at a time
@@ -389,8 +389,8 @@ __device__ __forceinline__ constexpr int token(int t, int e, int g) { return t *
 // queries are loaded.  The states' columns make the wavefronts independent but for
 // these products; every wavefront reads all of a head's queries from LDS, and that
 // beside the products' own chain is what bounds it.  Of 4 prompts of 2048 tokens (40
-// query heads over 8) 57 us, 17 of the segments' own sums, 7.8 of joining them; bytes'
-// time 40.  Counted there: matrix units 35 % busy, LDS 28 %, a fifteenth of that conflicts.
+// query heads over 8) 58 us, 16 of the segments' own sums, 7.6 of joining them; bytes'
+// time 40.  Counted there: matrix units 34 % busy, LDS 27 %, a fifteenth of that conflicts.
 // (Operands each awaited by itself 72 us, loads through registers 107, four wavefronts
 // of 32 columns 107.)
 template <class S>
