@@ -493,7 +493,7 @@ fs_status fs_profile_loop(fs_context *ctx, const fs_problem *p, fs_intervals iv,
  * offsets are 64-bit.  Outputs and workspaces may not overlap inputs.  A call
  * with nothing to do (no rows, no tokens) returns FS_OK and enqueues nothing.
  * Checks under FS_VALIDATE=1 wait for the stream: while it is being captured
- * the cache's calls are refused with FS_ERR_DEVICE. */
+ * the calls of caches and states are refused with FS_ERR_DEVICE. */
 typedef enum fs_dtype { FS_F32 = 0, FS_F16 = 1, FS_BF16 = 2 } fs_dtype;
 
 /* Codes of each row of x [rows][cols] (row stride x_stride >= cols), with one

@@ -1,5 +1,6 @@
 """State attention on the GPU, token by token and in chunks, against its
 recurrence in 64 bits."""
+import ctypes
 import math
 
 import pytest
@@ -440,3 +441,43 @@ def test_arguments_that_are_refused(env):
         fs.state_attention(ctx, **long, workspace=torch.empty(1024, dtype=torch.uint8, device="cuda:0"))
     assert e.value.status == fs.FS_ERR_WORKSPACE_TOO_SMALL
     assert torch.equal(bits(a["states"]), bits(b.pool))
+
+
+@pytest.mark.parametrize("T,S", [(16384, 64), (16384, 4096), (70, 4096), (3, 4096)])
+def test_sequences_that_overlap_end_without_harm(env, T, S):
+    """All rows given to every other sequence: more segments than the workspace, which
+    ends with its last byte, has places for."""
+    fs, ctx = env
+    note(f"state of overlapping sequences, {T} rows, {S} sequences")
+    heads, group, D = 8, 2, 64
+    q = torch.zeros(T, heads * group, D, dtype=torch.bfloat16, device="cuda:0")
+    k = torch.zeros(T, heads, D, dtype=torch.bfloat16, device="cuda:0")
+    pool = torch.ones(2, heads, D, D, device="cuda:0")
+    decay = torch.full((heads,), -0.5, device="cuda:0")
+    index, lens, cu = i32([-1] * S), i32([T] * S), i32([0, T] * (S // 2) + [0])
+    like = fs._StatePool(None, 2, heads, D)
+    need = fs._size(fs.load_library().fs_state_attention_workspace_size, ctypes.byref(like), heads * group, T, S)
+    room = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda:0")
+    out = fs.state_attention(ctx, pool, q, k, k, index, lens, cu, T, decay, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert (room[need:] == 77).all() and (pool == 1).all() and out.shape == q.shape
+    run(env, Batch([70, 300], [3, 1], [True, True], 1, 2, 64, "bf16"))
+
+
+def test_keys_values_and_queries_of_one_tensor_and_steps_in_a_row(env):
+    """One tensor for all three, and 40 calls of a token each against one of 40."""
+    fs, ctx = env
+    note("40 steps and a prompt of 40")
+    H, D = 3, 128
+    x = torch.randn(40, H, D, generator=gen(5)).bfloat16()
+    decay = torch.tensor([0.0, -0.1, -math.inf])
+    want, state, room, state_room = ref.state_attend(x, x, x, torch.zeros(H, D, D), decay, D ** -0.5)
+    pools = [torch.full((1, H, D, D), math.nan, device="cuda:0") for _ in range(2)]
+    dx, dd = x.to("cuda:0"), decay.to("cuda:0")
+    whole = fs.state_attention(ctx, pools[0], dx, dx, dx, i32([0]), i32([40]), i32([0, 40]), 40, dd)
+    steps = [fs.state_attention(ctx, pools[1], dx[t:t + 1], dx[t:t + 1], dx[t:t + 1], i32([0]), i32([t + 1]), i32([0, 1]), 1, dd)
+             for t in range(40)]
+    for out, pool in ((whole, pools[0]), (torch.cat(steps), pools[1])):
+        off = (out.cpu().double() - want).abs()
+        assert (off <= room + (want.abs() + room) * STEP["bf16"]).all()
+        assert ((pool[0].cpu().double() - state).abs() <= state_room + 2.0 ** -149).all()
