@@ -123,7 +123,7 @@ struct StateArgs {
   float scale;
   int32_t step_most, segment, n_places;  // set by the launcher
 };
-size_t state_workspace(int32_t n_heads, int32_t head_dim, int64_t n_tokens);
+size_t state_workspace(int32_t n_heads, int32_t head_dim, int64_t n_tokens, int32_t n_seqs);
 hipError_t launch_state_attention(const StateArgs &A, hipStream_t s);
 hipError_t launch_check_state(const StateArgs &A, int32_t *flag, hipStream_t s);
 

@@ -485,7 +485,7 @@ fs_status fs_state_attention_workspace_size(const fs_state_pool *pool, int32_t n
   if (!bytes) return fail(FS_ERR_INVALID_ARGUMENT, "bytes is NULL");
   const fs_status st = check_pool(pool, n_q_heads, n_tokens, n_seqs);
   if (st != FS_OK) return st;
-  *bytes = align256(fs::state_workspace(pool->n_heads, pool->head_dim, n_tokens));
+  *bytes = align256(fs::state_workspace(pool->n_heads, pool->head_dim, n_tokens, n_seqs));
   return FS_OK;
 }
 

@@ -770,21 +770,24 @@ __global__ void k_check_state(StateArgs A, int32_t *flag) {
 // Sequences of up to this many new tokens go token by token.
 constexpr int kStepMost = 8;
 
-// The least tokens of a segment: so many that all tokens make about 256 segments of a
-// head, one for each CU.
-int segment_least(int64_t n_tokens, int64_t n_heads) {
-  const int64_t L = (n_tokens * n_heads / 256 + kChunk - 1) / kChunk * kChunk;
+// Blocks of outputs at once: a CU has one at head_dim 128, two at 64.
+int64_t blocks_at_once(int32_t head_dim) { return head_dim == 128 ? 256 : 512; }
+
+// The least tokens of a segment: so many that all tokens make about a segment of a
+// head for each of those.
+int segment_least(int64_t n_tokens, int64_t n_heads, int32_t head_dim) {
+  const int64_t L = (n_tokens * n_heads / blocks_at_once(head_dim) + kChunk - 1) / kChunk * kChunk;
   return (int)std::max<int64_t>(kChunk, std::min<int64_t>(L, 1 << 30));
 }
 
 // Tokens of a segment, that many or more: those that take least if the tokens are as
 // many sequences of max_q as they make.  Times in us of what is measured at head_dim
-// 128 (a CU has one block of outputs then, two at 64): 2.2 for a chunk and query head, 1.5 for a chunk
+// 128: 2.2 for a chunk and query head, 1.5 for a chunk
 // beside, 2 for a chunk of a segment's sum, what launches and starts take; a segment a
 // sequence needs no sums.
 int segment_tokens(const StateArgs &A) {
-  const int least = segment_least(A.n_tokens, A.n_heads);
-  const int64_t sequences = std::max<int64_t>(1, (A.n_tokens + A.max_q / 2) / A.max_q), slots = A.head_dim == 128 ? 256 : 512;
+  const int least = segment_least(A.n_tokens, A.n_heads, A.head_dim);
+  const int64_t sequences = std::max<int64_t>(1, (A.n_tokens + A.max_q / 2) / A.max_q), slots = blocks_at_once(A.head_dim);
   const double chunk = 1.5 + 2.2 * (A.n_q_heads / A.n_heads);
   const auto time = [&](int64_t L) {
     const int64_t parts = (A.max_q + L - 1) / L, rounds = (sequences * parts * A.n_heads + slots - 1) / slots, chunks = std::min<int64_t>(L, A.max_q + kChunk - 1) / kChunk;
@@ -797,11 +800,11 @@ int segment_tokens(const StateArgs &A) {
   }
   return (int)std::min<int64_t>(best, 1 << 30);
 }
-// Places of sequences of more than a segment's L tokens: n of them have at most
-// n / L + 1 segments, less than 2 n / L.
-int64_t places_at_most(int64_t n_tokens, int64_t n_heads) {
-  const int64_t L = segment_least(n_tokens, n_heads);
-  return n_tokens > L ? 2 * n_tokens / L : 0;
+// Places of sequences of more than a segment's L tokens: n of them have less than
+// n / L + 1 segments, and so many sequences n / L at most.
+int64_t places_at_most(int64_t n_tokens, int64_t n_heads, int32_t head_dim, int64_t n_seqs) {
+  const int64_t L = segment_least(n_tokens, n_heads, head_dim);
+  return n_tokens > L ? n_tokens / L + std::min(n_seqs, n_tokens / L) : 0;
 }
 
 template <class S>
@@ -844,14 +847,14 @@ template <int TYPE, int D>
 hipError_t state_of(StateArgs A, hipStream_t s) {
   A.max_q = std::min(A.max_q, A.n_tokens);
   A.segment = segment_tokens(A);
-  A.n_places = (int32_t)places_at_most(A.n_tokens, A.n_heads);
+  A.n_places = (int32_t)places_at_most(A.n_tokens, A.n_heads, A.head_dim, A.n_seqs);
   A.step_most = kStepMost;
   if (A.max_q <= kStepMost) return steps_of<TYPE, D>(A, 0, s);
   if (A.n_seqs == 1) A.step_most = 0;  // no launch for what may be a single token
   const bool one = A.segment >= A.max_q;  // a segment a sequence
   // Heads first: blocks that find no segment come last.  (Between the others they left
   // them to half of the CUs: one prompt of 12260 tokens beside 15 single ones, 12 heads,
-  // 148 us of the outputs instead of 92.)  No more than 256 segments and a sequence's
+  // 148 us of the outputs instead of 92.)  No more than blocks_at_once segments and a sequence's
   // last, see segment_least.
   const dim3 grid(A.n_heads, one ? (unsigned)A.n_seqs : (unsigned)(A.n_tokens / A.segment + A.n_seqs));
   hipError_t e = one ? hipSuccess : chunks_of<TYPE, D, true>(grid, A, s);
@@ -863,8 +866,8 @@ hipError_t state_of(StateArgs A, hipStream_t s) {
 
 }  // namespace
 
-size_t state_workspace(int32_t n_heads, int32_t head_dim, int64_t n_tokens) {
-  return (size_t)(places_at_most(n_tokens, n_heads) * n_heads * head_dim * head_dim) * 4;
+size_t state_workspace(int32_t n_heads, int32_t head_dim, int64_t n_tokens, int32_t n_seqs) {
+  return (size_t)(places_at_most(n_tokens, n_heads, head_dim, n_seqs) * n_heads * head_dim * head_dim) * 4;
 }
 
 hipError_t launch_check_state(const StateArgs &A, int32_t *flag, hipStream_t s) {
