@@ -13,6 +13,7 @@
 //   where there are few heads: a pass that makes each segment's own sum, one that
 //   adds them up in order, and the outputs from there.
 #include <algorithm>
+#include <cmath>
 
 #include "fs_serving.h"
 
@@ -780,22 +781,33 @@ int segment_least(int64_t n_tokens, int64_t n_heads, int32_t head_dim) {
   return (int)std::max<int64_t>(kChunk, std::min<int64_t>(L, 1 << 30));
 }
 
-// Tokens of a segment, that many or more: those that take least if the tokens are as
-// many sequences of max_q as they make.  Times in us of what is measured at head_dim
-// 128: 2.2 for a chunk and query head, 1.5 for a chunk
-// beside, 2 for a chunk of a segment's sum, what launches and starts take; a segment a
-// sequence needs no sums.
+// Tokens of a segment, that many or more: those that take least if one sequence has
+// max_q new tokens and the others share what is left (where that is no more than
+// kStepMost each, the long one is alone).  Times in us of what is measured at head_dim
+// 128: 2.2 for a chunk and query head, 1.5 for a chunk beside, 2 for a chunk of a
+// segment's sum, what launches and starts take; a segment a sequence needs no sums.
+// Sequences of one length are whole rounds of blocks; of others half a segment each is
+// left over, and blocks behind the first round fill up what is free.  (Lengths in
+// eighths of the least: 6 prompts of 17211 tokens, 8 heads of 128, 422 us, 553 where
+// only its halves are tried; 27 of up to 15696 tokens, 6 heads of 64 over 3, 169, and
+// 235 as equal ones.)
 int segment_tokens(const StateArgs &A) {
-  const int least = segment_least(A.n_tokens, A.n_heads, A.head_dim);
-  const int64_t sequences = std::max<int64_t>(1, (A.n_tokens + A.max_q / 2) / A.max_q), slots = blocks_at_once(A.head_dim);
-  const double chunk = 1.5 + 2.2 * (A.n_q_heads / A.n_heads);
+  const int64_t least = segment_least(A.n_tokens, A.n_heads, A.head_dim), longest = (A.max_q + kChunk - 1) / kChunk * kChunk;
+  const double slots = (double)blocks_at_once(A.head_dim), chunk = 1.5 + 2.2 * (A.n_q_heads / A.n_heads);
+  const double other = A.n_seqs > 1 ? std::min<double>(A.max_q, (double)(A.n_tokens - A.max_q) / (A.n_seqs - 1)) : 0.0;
+  const double others = other > kStepMost ? A.n_seqs - 1 : 0;
+  const bool equal = others == 0 || other == A.max_q;
   const auto time = [&](int64_t L) {
-    const int64_t parts = (A.max_q + L - 1) / L, rounds = (sequences * parts * A.n_heads + slots - 1) / slots, chunks = std::min<int64_t>(L, A.max_q + kChunk - 1) / kChunk;
-    return (double)rounds * ((double)chunks * chunk + 6.0) + (parts > 1 ? (double)rounds * ((double)chunks * 2.0 + 5.0) + 6.0 : 0.0);
+    const double parts = (double)((A.max_q + L - 1) / L), chunks = (double)(std::min(L, longest) / kChunk);
+    const double blocks = A.n_heads * (parts + others * (equal ? parts : std::max(1.0, other / (double)L + 0.5)));
+    const double whole = A.n_heads * ((double)A.max_q + others * other) / (double)(chunks * kChunk);
+    const double rounds = blocks <= slots ? 1.0 : equal ? std::ceil(blocks / slots) : whole / slots + 0.8;
+    return rounds * (chunks * chunk + 6.0) + (parts > 1 ? rounds * (chunks * 2.0 + 5.0) + 6.0 : 0.0);
   };
   int64_t best = least;
-  for (int i = 1; i <= 8; ++i) {
-    const int64_t L = i < 8 ? least + (int64_t)least / kChunk * i / 2 * kChunk : (A.max_q + kChunk - 1) / kChunk * kChunk;
+  const int64_t step = std::max<int64_t>(1, least / 8 / kChunk) * kChunk;
+  for (int i = 1; i <= 28; ++i) {
+    const int64_t L = i < 28 ? least + i * step : longest;
     if (L >= least && time(L) < time(best)) best = L;
   }
   return (int)std::min<int64_t>(best, 1 << 30);
