@@ -57,6 +57,22 @@ def test_states_of_segments(lib):
     assert status == fs.FS_OK and got <= 2 * 257 * 64 * 64 * 4
 
 
+@pytest.mark.parametrize("D,at_once", [(128, 256), (64, 512)])
+@pytest.mark.parametrize("heads,T,S", [(1, 65, 1), (1, 129, 2), (2, 32768, 1), (8, 8192, 4), (8, 8192, 300), (12, 389, 23), (3, 179966, 27)])
+def test_states_of_the_most_segments(lib, D, at_once, heads, T, S):
+    """As many sequences of a token more than whole segments as there may be: places for
+    all of their segments, and not for one more a sequence."""
+    L = max(64, -(-(T * heads // at_once) // 64) * 64)
+    long = min(S, T // (L + 1))
+    lengths = [L + 1] * long
+    if long:
+        lengths[0] += (T - sum(lengths)) // L * L
+    places = sum(-(-n // L) for n in lengths)
+    status, got = size(lib.fs_state_attention_workspace_size, ctypes.byref(pool(n_heads=heads, head_dim=D)), heads, T, S)
+    assert status == fs.FS_OK
+    assert places * heads * D * D * 4 <= got <= (places + min(S, T // L)) * heads * D * D * 4
+
+
 @pytest.mark.parametrize("change,args,status", [
     (dict(head_dim=80), (2, 5, 1), fs.FS_ERR_UNSUPPORTED), (dict(head_dim=256), (2, 5, 1), fs.FS_ERR_UNSUPPORTED),
     (dict(n_heads=0), (2, 5, 1), fs.FS_ERR_INVALID_ARGUMENT), (dict(n_states=-1), (2, 5, 1), fs.FS_ERR_INVALID_ARGUMENT),
