@@ -22,14 +22,24 @@ namespace {
 
 constexpr int kChunk = 64, kThreads = 256;  // kThreads: of a block that goes token by token, or joins
 
-// Powers of l by exp2 of multiples of its logarithm, which is at least -10^4 here
-// so that 0 times it is 0 where l is 0 (log_decay -infinity).  Positive ones count
-// as 0; a NaN stays one.
-__device__ __forceinline__ float log2_decay(const StateArgs &A, int h) {
-  const float x = A.log_decay[h] * 1.44269504f;
-  return x > 0.0f ? 0.0f : x < -1e4f ? -1e4f : x;
+// Powers of l up to 127 by exp2 of multiples of its logarithm, which is at least -10^4
+// here so that 0 times it is 0 where l is 0 (log_decay -infinity).  Positive ones count
+// as 0; a NaN stays one.  The logarithm in two parts, the first of 17 bits, whose
+// multiples are exact, the second as the factor 1 + its multiple: a far token's power
+// is off by two steps like a near one's (a logarithm of 24 bits, times 100, would be off
+// by 2^-17 of the power).
+struct Rate {
+  float upper, lower;
+};
+__device__ __forceinline__ Rate log2_decay(const StateArgs &A, int h) {
+  const double exact = (double)A.log_decay[h] * 1.4426950408889634, x = exact > 0.0 ? 0.0 : exact < -1e4 ? -1e4 : exact;
+  const float upper = __uint_as_float((__float_as_uint((float)x) + 0x40) & ~0x7fu);
+  return {upper, (float)((x - (double)upper) * 0.6931471805599453)};
 }
-__device__ __forceinline__ float power(float l2, int n) { return __builtin_amdgcn_exp2f(l2 * (float)n); }
+__device__ __forceinline__ float power(Rate l, float n) {
+  const float p = __builtin_amdgcn_exp2f(l.upper * n);
+  return __builtin_fmaf(p, l.lower * n, p);
+}
 
 // The same to the last bit: what a state is multiplied by once for many tokens.
 __device__ __forceinline__ float exact_power(const StateArgs &A, int h, int n) {
@@ -473,15 +483,16 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[a][e] = from[place(a, e)];
   }
-  const float l2 = log2_decay(A, h), chunk_kept = exact_power(A, h, kChunk);
+  const Rate l2 = log2_decay(A, h);
+  const float chunk_kept = exact_power(A, h, kChunk);
   // the decay between a token of this wavefront's rows and one before it
   float fade[2 * TASKS][4], row_decay = 0.0f;
   if constexpr (!S::SUMS) {
 #pragma unroll
     for (int j = 0; j < 2 * TASKS; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) fade[j][e] = A.scale * power(l2, max(0, (mine_i - 2 * mine_t - j) * 16 + own - 4 * g - e));
-    row_decay = A.scale * power(l2, own + 1);
+      for (int e = 0; e < 4; ++e) fade[j][e] = A.scale * power(l2, (float)max(0, (mine_i - 2 * mine_t - j) * 16 + own - 4 * g - e));
+    row_decay = A.scale * power(l2, (float)(own + 1));
   }
 
   if constexpr (!S::SUMS) arrive<0>();
@@ -636,7 +647,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
                 for (int i = 0; i < 2; ++i) o[i] = multiply<TYPE>(past.part[t][p], x[i][t], o[i]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const float seen = row_decay * power(l2, u * 32 + i * 16);
+              const float seen = row_decay * power(l2, (float)(u * 32 + i * 16));
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[i][e] = (TYPE == kF16 ? o[i][e] * past_undo[e] : o[i][e]) * seen;
             }
@@ -698,7 +709,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          x[t][e] = value16<TYPE>((uint16_t)v[t][e]) * __builtin_amdgcn_exp2f(l2 * (behind - (float)token(t, e, 0)));
+          x[t][e] = value16<TYPE>((uint16_t)v[t][e]) * power(l2, behind - (float)token(t, e, 0));
       if (n < kChunk) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
