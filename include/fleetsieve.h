@@ -696,13 +696,14 @@ typedef struct fs_state_pool {
  * may have one state.  out: [n_tokens][n_q_heads][head_dim] contiguous, of q's type.
  *
  * Sums and states are binary32.  Sequences of up to 8 new tokens go token by token
- * (in a call of one sequence: if max_q is at most 8).  Others go in chunks of 64, where states and the decayed products of queries and
- * keys enter the products as two values of the element type (16 bits of each in
- * bfloat16, 22 in binary16) and decayed values as three or two (24 or 22 bits): outputs
- * are off by about 2^-17 of their sums' terms before they are rounded, states by about
- * a rounding of binary32.  Equal run to run.  What a NaN or an infinity reaches by the formula (its own
- * token's outputs and later ones, the state) is not finite, and nothing else; a
- * state beyond 2^127 counts as infinite.
+ * (in a call of one sequence: if max_q is at most 8).  Others go in chunks of 64, where
+ * of states and of the decayed products of queries and keys 16 bits or more enter the
+ * products and of decayed values 22 or more, however small one is beside others (an
+ * element of a state in binary16 that is below 2^-140 of its column's largest counts as
+ * 0): outputs are off by about 2^-17 of their sums' terms before they are rounded, states
+ * by about a rounding of binary32.  Equal run to run.  What a NaN or an infinity reaches
+ * by the formula (its own token's outputs and later ones, the state) is not finite, and
+ * nothing else; a state beyond 2^127 counts as infinite.
  *
  * With FS_VALIDATE=1 lengths, states and decays outside their ranges and states that
  * two sequences share are refused (the call waits for the stream); otherwise lengths

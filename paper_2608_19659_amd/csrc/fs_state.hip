@@ -246,11 +246,14 @@ __global__ __launch_bounds__(kThreads) void k_state_step(StateArgs A) {
 }
 
 // ------------------------------------------------------------------ in chunks --
+using float2v = float __attribute__((ext_vector_type(2)));
+using half2v = _Float16 __attribute__((ext_vector_type(2)));
 using half8v = _Float16 __attribute__((ext_vector_type(8)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using short4v = short __attribute__((ext_vector_type(4)));
 using short8v = short __attribute__((ext_vector_type(8)));
 
+__device__ __forceinline__ float4v multiply(float a, float b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 template <int TYPE>
 __device__ __forceinline__ float4v multiply(short8v a, short8v b, float4v c) {
   if constexpr (TYPE == kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
@@ -260,34 +263,97 @@ __device__ __forceinline__ float4v multiply(short8v a, short8v b, float4v c) {
 // Binary32 values enter a product as sums of PARTS values of its 16-bit type: what
 // one alone loses (2^-9 of a value in bfloat16) an output would be off by as much
 // again as by its own rounding, and a state, which is binary32, by far more.
-// binary16 has no room for any binary32 value, so the values of a row or column of
-// the operand are multiplied by a power of two that brings their largest to 2^14,
-// and the result by its inverse (exactly); what is below 2^-39 of the largest is lost.
+// binary16 has no room for any binary32 value, so the values of a column of the
+// operand are multiplied by a power of two that brings their largest to 2^14,
+// and the result by its inverse (exactly).  Of a value far below the largest the parts
+// hold fewer bits, of one below 2^-39 of it none, though it may be all that a sum has
+// (where a query or a key is 0 beside the others): what they lack of it is multiplied
+// by itself.  That goes by each element alone, so that no column and no token is off by
+// what others hold.  (What is below 2^-140 of a column's largest has no bits behind the
+// factor either and counts as 0.)
 template <int TYPE, int COUNT, int PARTS>
 struct Parts {
   short8v part[COUNT][PARTS];
+  float factor, inverse;
 
   // `most`: bits of the largest magnitude of all that is multiplied by one factor.
-  __device__ __forceinline__ float set(const float (&x)[COUNT][8], uint32_t most) {
-    float factor = 1.0f, inverse = 1.0f;
-    if constexpr (TYPE == kF16) {
-      const uint32_t exponent = max(most >> 23, 15u);  // at most 255
-      factor = __uint_as_float((268 - exponent) << 23);
-      inverse = __uint_as_float((exponent - 14) << 23);
-    }
+  __device__ __forceinline__ void scale(uint32_t most) {
+    const uint32_t exponent = max(most >> 23, 15u);  // at most 255
+    factor = TYPE == kF16 ? __uint_as_float((268 - exponent) << 23) : 1.0f;
+    inverse = TYPE == kF16 ? __uint_as_float((exponent - 14) << 23) : 1.0f;
+  }
+  __device__ __forceinline__ void set(const float (&x)[COUNT][8], uint32_t most) {
+    scale(most);
 #pragma unroll
     for (int t = 0; t < COUNT; ++t)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float rest = TYPE == kF16 ? x[t][e] * factor : x[t][e];
+      for (int e = 0; e < 8; e += 2) {
+        float y[2] = {TYPE == kF16 ? x[t][e] * factor : x[t][e], TYPE == kF16 ? x[t][e + 1] * factor : x[t][e + 1]};
+        uint32_t words[PARTS];
+        split(y, words);
+        put(t, e, words);
+      }
+  }
+  // Two neighbouring values' parts; the values become what these lack of them.
+  __device__ __forceinline__ static void split(float (&x)[2], uint32_t (&words)[PARTS]) {
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-          const uint16_t bits = bits16<TYPE>(rest);
-          part[t][p][e] = (short)bits;
-          if (p + 1 < PARTS) rest -= value16<TYPE>(bits);
+    for (int p = 0; p < PARTS; ++p) {
+      if constexpr (TYPE == kF16) {
+        const half2v h = __builtin_convertvector((float2v{x[0], x[1]}), half2v);
+        words[p] = __builtin_bit_cast(uint32_t, h);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = __builtin_fmaf((float)h[i], -1.0f, x[i]);  // one instruction
+      } else {
+        words[p] = bf16_bits(x[0]) | (uint32_t)bf16_bits(x[1]) << 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] -= bf16_value((uint16_t)(words[p] >> 16 * i));
+      }
+    }
+  }
+  __device__ __forceinline__ void put(int t, int e, const uint32_t (&words)[PARTS]) {
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) part[t][p][e + i] = (short)(words[p] >> 16 * i);
+  }
+  // What the parts lack of x, of any place, behind the factor; 0 if they have all or it is
+  // not small.
+  __device__ __forceinline__ float rest_of_small(float x, float small) const {
+    uint32_t words[PARTS];
+    float rest[2] = {x * factor, 0.0f};
+    const bool is_small = fabsf(rest[0]) < small;
+    split(rest, words);
+    return is_small ? rest[0] : 0.0f;
+  }
+  // x becomes what its parts lack of what is below 2^-3 behind the factor; whether that
+  // is anything.
+  __device__ __forceinline__ bool split_small(float (&x)[COUNT][8]) {
+    bool any = false;
+#pragma unroll
+    for (int t = 0; t < COUNT; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        uint32_t words[PARTS];
+        float y[2] = {x[t][e] * factor, x[t][e + 1] * factor};
+        const bool small[2] = {fabsf(y[0]) < 0x1p-3f, fabsf(y[1]) < 0x1p-3f};
+        split(y, words);
+        put(t, e, words);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[t][e + i] = small[i] ? y[i] : 0.0f;
+          any |= x[t][e + i] != 0.0f;
         }
       }
-    return inverse;
+    return any;
+  }
+  // The least of this lane's values times the factor that is not 0.
+  __device__ __forceinline__ float least(const float (&x)[COUNT][8]) const {
+    uint32_t least = ~0u;  // of the bits less one: those of 0 are last
+#pragma unroll
+    for (int t = 0; t < COUNT; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) least = min(least, (__float_as_uint(x[t][e]) & 0x7fffffffu) - 1u);
+    return least == ~0u ? __builtin_inff() : __uint_as_float(least + 1u) * factor;
   }
 };
 
@@ -335,9 +401,9 @@ struct ChunkShape {
   static constexpr int TILE = kChunk * D;                       // 16-bit words
   // products of queries and keys, as operands in two parts: of 16 query rows with 32
   // keys, six of which are not all of later keys
-  static constexpr int PART = 6 * 512, PRODUCTS = 2 * PART, UNDO = 6 * 16;
+  static constexpr int PART = 6 * 512, PRODUCTS = 2 * PART;
   static constexpr int KEYS = SUMS ? 4 : 2, VALUES = SUMS ? 4 : 1, QUERIES = D == 128 ? 4 : 3;  // tiles; beside them products of two heads
-  static constexpr int BYTES = SUMS ? 8 * TILE * 2 : ((3 + QUERIES) * TILE + 2 * PRODUCTS) * 2 + 2 * UNDO * 4;
+  static constexpr int BYTES = SUMS ? 8 * TILE * 2 : ((3 + QUERIES) * TILE + 2 * PRODUCTS) * 2;
   __device__ static __forceinline__ constexpr int product(int i, int t) { return i < 2 ? i : 2 * i - 2 + t; }
 
   // So that reads meet in no bank.  A transpose takes two neighbouring pieces of
@@ -405,14 +471,14 @@ __device__ __forceinline__ constexpr int token(int t, int e, int g) { return t *
 // (Operands each awaited by itself 72 us, loads through registers 107, four wavefronts
 // of 32 columns 107.)
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
+__global__ __launch_bounds__(S::THREADS, 2) void k_state_chunk(StateArgs A) {
   constexpr int TYPE = S::TYPE, D = S::D, KT = D / 16, KS = D / 32;  // tiles and steps of a key's elements
   constexpr int TASKS = S::WAVES == 8 ? 1 : 2;                       // pairs of key tiles to a wavefront
   constexpr int PARTS = TYPE == kF16 ? 2 : 3;                        // of a decayed value: 22 or 24 bits, as the states have
+  constexpr float SMALL = 0x1p-7f;  // of binary16: 2^-25 is lost of what has this or more, 2^-18 of it
   constexpr uint16_t INFINITE = TYPE == kF16 ? 0x7c00 : 0x7f80;
   extern __shared__ __attribute__((aligned(1024))) short state_lds[];
   short *const lk = state_lds, *const lv = lk + S::KEYS * S::TILE, *const lq = lv + S::VALUES * S::TILE, *const lp = lq + S::QUERIES * S::TILE;
-  float *const undo = (float *)(lp + 2 * S::PRODUCTS);  // of a row of products, what undoes its factor
   const Segment seg = find_segment(A, blockIdx.y);
   const int number = __builtin_amdgcn_readfirstlane(seg.number), before = __builtin_amdgcn_readfirstlane(seg.before);
   if (number < 0) return;
@@ -548,20 +614,49 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
       }
     }
     const bool numbers = !__any(none < kChunk);
+    // The values' operands for the decayed products, which are bfloat16 pairs in either
+    // type: a decay of a few dozen tokens leaves binary16's range.  A binary16 value
+    // is the sum of two bfloat16 ones, and is not held beside them.
+    constexpr bool PAIRS = TYPE == kF16 && !S::SUMS;
+    short8v values[PAIRS ? 2 : 1][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      values[0][t] = v[t];
+      if constexpr (PAIRS)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = value16<kF16>((uint16_t)v[t][e]);
+          const uint16_t upper = bits16<kBF16>(x);
+          values[0][t][e] = (short)upper;
+          values[PAIRS][t][e] = (short)bits16<kBF16>(x - value16<kBF16>(upper));
+        }
+    }
+    const auto value = [&](int t, int e) {
+      if constexpr (PAIRS) return value16<kBF16>((uint16_t)values[0][t][e]) + value16<kBF16>((uint16_t)values[PAIRS][t][e]);
+      else return value16<TYPE>((uint16_t)v[t][e]);
+    };
 
     if constexpr (!S::SUMS) {
-      // the state as an operand
+      // the state as an operand; `small`: which elements [t][e], of any lane, have less
+      // than 16 bits in their parts
       Parts<TYPE, KS, 2> past;
       float past_undo[4];
+      uint32_t small = 0;
       {
         float x[KS][8];
 #pragma unroll
         for (int t = 0; t < KS; ++t)
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[t][e] = s[2 * t + (e >> 2)][e & 3];
-        const float inverse = past.set(x, largest<TYPE, KS>(x));
+        past.set(x, largest<TYPE, KS>(x));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) past_undo[e] = TYPE == kF16 ? __shfl(inverse, 4 * g + e) : 1.0f;
+        for (int e = 0; e < 4; ++e) past_undo[e] = TYPE == kF16 ? __shfl(past.inverse, 4 * g + e) : 1.0f;
+        if (TYPE == kF16 && __any(past.least(x) < SMALL)) {
+#pragma unroll
+          for (int t = 0; t < KS; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) small |= (uint32_t)(__any(x[t][e] != 0.0f && fabsf(x[t][e] * past.factor) < SMALL) != 0) << (8 * t + e);
+        }
       }
       // 16 rows of <q, k>, decayed, by pairs of 16 keys, to LDS as operands
       const auto products = [&](const short *k, const short *lq_of, int to) {
@@ -590,12 +685,102 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)  // later tokens are left out, whatever they are
               x[0][half * 4 + e] = (2 * t + half) * 16 + 4 * g + e > mine_i * 16 + own ? 0.0f : sum[half][e] * fade[task * 2 + half][e];
-          Parts<TYPE, 1, 2> p;
-          const float inverse = p.set(x, largest<TYPE, 1>(x));
+          Parts<kBF16, 1, 2> p;
+          p.set(x, 0);
           short *const out = lp + to * S::PRODUCTS + (S::product(mine_i, t) * 64 + lane) * 8;
           *(short8v *)out = p.part[0][0];
           *(short8v *)(out + S::PART) = p.part[0][1];
-          if (TYPE == kF16 && g == 0) undo[to * S::UNDO + S::product(mine_i, t) * 16 + own] = inverse;
+        }
+      };
+      // A head's outputs.  Two times two tiles of 16 rows, all of their operands on the way
+      // from LDS before the first product: a wavefront that waits for each has one other to
+      // wait behind.
+      const auto outputs = [&](const short *lq_now, const short *lp_now, int head) {
+        uint8_t *const out = (uint8_t *)A.out + (((row0 + c) * A.n_q_heads + h * group + head) * D + dv0) * 2;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (u * 32 >= n) break;
+          float4v o[2] = {};
+          // What the parts lack of small elements, four rows of the state at a time; other
+          // elements add 0.  (Random states have one in a chunk of a hundred: with all of
+          // its column in binary32 instead four prompts of 2048 tokens took 14 us longer.)
+          if (PAIRS && __builtin_expect(small != 0, 0)) {
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+              if (!(small >> 8 * t & 0xff)) continue;
+              short8v y[2];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) y[i] = S::rows(lq_now, at_rows, u * 32 + i * 16, t);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                if (!(small >> (8 * t + e) & 1)) continue;
+                float element = s[2 * t + (e >> 2)][e & 3];
+                asm volatile("" : "+v"(element));  // else the rests are made before the heads, and held
+                const float rest = past.rest_of_small(element, SMALL);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) o[i] = multiply(rest, value16<TYPE>((uint16_t)y[i][e]), o[i]);
+              }
+            }
+          }
+          short8v x[2][KS], w[2][2][2];
+#pragma unroll
+          for (int t = 0; t < KS; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[i][t] = S::rows(lq_now, at_rows, u * 32 + i * 16, t);
+#pragma unroll
+          for (int t = 0; t <= u; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int p = 0; p < 2; ++p) w[i][t][p] = *(const short8v *)(lp_now + p * S::PART + (S::product(u * 2 + i, t) * 64 + lane) * 8);
+          __builtin_amdgcn_sched_barrier(0);
+          float4v near[2] = {};
+          // of this chunk's tokens, without the lower parts of both (2^-18 of a product)
+          const auto products_of_values = [&](float4v (&sum)[2]) {
+#pragma unroll
+            for (int t = 0; t <= u; ++t)
+#pragma unroll
+              for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int d = 0; d < (PAIRS ? 2 - p : 1); ++d)
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) sum[i] = multiply<kBF16>(values[d][t], w[i][t][p], sum[i]);
+          };
+          if constexpr (PAIRS) products_of_values(near);  // beside the state's
+#pragma unroll
+          for (int t = 0; t < KS; ++t)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) o[i] = multiply<TYPE>(past.part[t][p], x[i][t], o[i]);
+          if constexpr (PAIRS) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][e] *= past_undo[e];
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float seen = row_decay * power(l2, (float)(u * 32 + i * 16));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] = PAIRS ? __builtin_fmaf(o[i][e], seen, near[i][e]) : o[i][e] * seen;
+          }
+          if constexpr (!PAIRS) products_of_values(o);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = u * 32 + i * 16 + own;
+            if (!numbers) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (row >= __shfl(none, 4 * g + e)) o[i][e] = __builtin_nanf("");
+            }
+            if (row < n) {
+              uint16_t bits[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) bits[e] = bits16<TYPE>(o[i][e]);
+              __builtin_memcpy(out + (uint32_t)(out_at + (u * 32 + i * 16) * A.n_q_heads * (D * 2)), bits, 8);
+            }
+          }
         }
       };
       // The first head's products, then each head's outputs beside the next one's
@@ -611,78 +796,14 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
       for (int head = 0; head < group; ++head) {
         const short *const lq_now = lq + q_buf * S::TILE, *const lp_now = lp + p_buf * S::PRODUCTS;
         q_buf = q_buf == S::QUERIES - 1 ? 0 : q_buf + 1;
-        const bool values = made && head == 1 && more;
-        if (values) fetch_v(c + kChunk, 0);
+        const bool next_values = made && head == 1 && more;
+        if (next_values) fetch_v(c + kChunk, 0);
         fetched = fetch_next_q();
         // (One wavefront of a SIMD before its outputs, the other behind them.)
         const bool ahead = head + 1 < group || early;
         const short *const k_next = head + 1 < group ? k : lk + (buf ^ 1) * S::TILE;
         if (ahead && wave < 4) products(k_next, lq + q_buf * S::TILE, p_buf ^ 1);
-        // Two times two tiles of 16 rows of outputs, all of their operands on the way from
-        // LDS before the first product: a wavefront that waits for each has one other to
-        // wait behind.
-        {
-          uint8_t *const out = (uint8_t *)A.out + (((row0 + c) * A.n_q_heads + h * group + head) * D + dv0) * 2;
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            if (u * 32 >= n) break;
-            short8v x[2][KS], w[2][2][2];
-#pragma unroll
-            for (int t = 0; t < KS; ++t)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) x[i][t] = S::rows(lq_now, at_rows, u * 32 + i * 16, t);
-#pragma unroll
-            for (int t = 0; t <= u; ++t)
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int p = 0; p < 2; ++p) w[i][t][p] = *(const short8v *)(lp_now + p * S::PART + (S::product(u * 2 + i, t) * 64 + lane) * 8);
-            __builtin_amdgcn_sched_barrier(0);
-            float4v o[2] = {};
-#pragma unroll
-            for (int t = 0; t < KS; ++t)
-#pragma unroll
-              for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) o[i] = multiply<TYPE>(past.part[t][p], x[i][t], o[i]);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float seen = row_decay * power(l2, (float)(u * 32 + i * 16));
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[i][e] = (TYPE == kF16 ? o[i][e] * past_undo[e] : o[i][e]) * seen;
-            }
-#pragma unroll
-            for (int t = 0; t <= u; ++t)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                float4v sum = TYPE == kF16 ? float4v{0, 0, 0, 0} : o[i];
-#pragma unroll
-                for (int p = 0; p < 2; ++p) sum = multiply<TYPE>(v[t], w[i][t][p], sum);
-                if constexpr (TYPE == kF16) {
-                  const float inverse = undo[p_buf * S::UNDO + S::product(u * 2 + i, t) * 16 + own];
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) o[i][e] = __builtin_fmaf(sum[e], inverse, o[i][e]);
-                } else {
-                  o[i] = sum;
-                }
-              }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int row = u * 32 + i * 16 + own;
-              if (!numbers) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (row >= __shfl(none, 4 * g + e)) o[i][e] = __builtin_nanf("");
-              }
-              if (row < n) {
-                uint16_t bits[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bits[e] = bits16<TYPE>(o[i][e]);
-                __builtin_memcpy(out + (uint32_t)(out_at + (u * 32 + i * 16) * A.n_q_heads * (D * 2)), bits, 8);
-              }
-            }
-          }
-        }
+        outputs(lq_now, lp_now, head);
         if (ahead && wave >= 4) products(k_next, lq + q_buf * S::TILE, p_buf ^ 1);
         // The next one's products need the queries after it: behind them what this
         // one has asked for, and its stores.
@@ -690,7 +811,7 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
           if (n < kChunk) arrive<0>();
           else if (S::QUERIES == 3) arrive<4>();
           else if (head == 0 && more && !made) fetched ? arrive<4 + 3 * S::PIECES>() : arrive<4 + 2 * S::PIECES>();
-          else if ((head == 0 && more) || values) fetched ? arrive<4 + 2 * S::PIECES>() : arrive<4 + S::PIECES>();
+          else if ((head == 0 && more) || next_values) fetched ? arrive<4 + 2 * S::PIECES>() : arrive<4 + S::PIECES>();
           else fetched ? arrive<4 + S::PIECES>() : arrive<4>();
         }
         p_buf ^= 1;
@@ -700,61 +821,83 @@ __global__ __launch_bounds__(S::THREADS) void k_state_chunk(StateArgs A) {
     }
     // the state after the chunk
     const float kept = n == kChunk ? chunk_kept : exact_power(A, h, n);
-    Parts<TYPE, 2, PARTS> fading;
-    float inverse;
+    Parts<TYPE, 1, PARTS> fading[2];  // 32 tokens each: a factor for both would be the last ones'
+    float x[2][1][8];
     {
-      float x[2][8];
       const float behind = (float)(n - 1 - 4 * g);  // tokens, of the chunk's behind this lane's first
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          x[t][e] = value16<TYPE>((uint16_t)v[t][e]) * power(l2, behind - (float)token(t, e, 0));
+          x[t][0][e] = value(t, e) * power(l2, behind - (float)token(t, e, 0));
       if (n < kChunk) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (token(t, e, g) >= n) x[t][e] = 0.0f;
+            if (token(t, e, g) >= n) x[t][0][e] = 0.0f;
       }
       if (!numbers) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (token(t, e, g) == none) x[t][e] = __builtin_nanf("");
+            if (token(t, e, g) == none) x[t][0][e] = __builtin_nanf("");
       }
-      inverse = fading.set(x, largest<TYPE, 2>(x));
     }
-    constexpr int AT_ONCE = KT < 8 ? KT : 8;
+    bool some = false;
 #pragma unroll
-    for (int a0 = 0; a0 < KT; a0 += AT_ONCE) {
-      short8v x[AT_ONCE][2];
+    for (int t = 0; t < 2; ++t) {
+      fading[t].scale(largest<TYPE, 1>(x[t]));
+      some |= fading[t].split_small(x[t]);
+    }
+    short8v keys[KT][2];
 #pragma unroll
-      for (int a = 0; a < AT_ONCE; ++a)
+    for (int a = 0; a < KT; ++a)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) x[a][t] = S::keys(k, t * 32, a0 + a);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int t = 0; t < 2; ++t) keys[a][t] = S::keys(k, t * 32, a);
+    __builtin_amdgcn_sched_barrier(0);
+    for (float held = kept;; held = 1.0f) {
 #pragma unroll
-      for (int a = 0; a < AT_ONCE; a += 4) {  // four sums side by side, none waits for itself
-        float4v sum[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = TYPE == kF16 ? float4v{0, 0, 0, 0} : s[a0 + a + i] * kept;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
+      for (int a = 0; a < KT; a += 4) {  // four sums side by side, none waits for itself
+        if constexpr (TYPE == kF16) {
+          float4v sum[2][4] = {};
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = multiply<TYPE>(x[a + i][t], fading.part[t][p], sum[i]);
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (TYPE == kF16) {
+              for (int i = 0; i < 4; ++i) sum[t][i] = multiply<TYPE>(keys[a + i][t], fading[t].part[0][p], sum[t][i]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[a0 + a + i][e] = __builtin_fmaf(sum[i][e], inverse, s[a0 + a + i][e] * kept);
-          } else {
-            s[a0 + a + i] = sum[i];
-          }
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s[a + i][e] = __builtin_fmaf(sum[1][i][e], fading[1].inverse, __builtin_fmaf(sum[0][i][e], fading[0].inverse, s[a + i][e] * held));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[a + i] *= held;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[a + i] = multiply<TYPE>(keys[a + i][t], fading[t].part[0][p], s[a + i]);
         }
+      }
+      // What two binary16 parts lack of values of which they hold less than 22 bits, 2^-25
+      // at most, goes in behind a factor of its own as often as there is any: four times at
+      // most, then no bit of binary32 is left.  (Decays that leave 2^-14 of a value in 32
+      // tokens need none but for a few values, faster ones one or two: 4 prompts of 4096
+      // tokens, 16 heads of 128 from exp(-0.7) to exp(-0.004) a token, 179 us, all at
+      // exp(-0.004) 155, 136 where small values are lost.  With all of the column in binary32
+      // instead the first took 321.)
+      if (TYPE != kF16 || !__any(some)) break;
+      some = false;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        fading[t].factor = 0x1p39f;
+        fading[t].inverse *= 0x1p-39f;
+        some |= fading[t].split_small(x[t]);
       }
     }
   }
