@@ -141,3 +141,28 @@ def state_attend_at_once(q, k, v, state, log_decay, scale):
     held = 1.0 / max(1e-9, 1.0 - float(torch.exp(rate).max()))
     steps = 2 * 2.0 ** -17 + 2.0 ** -24 * (min(n, held) + D)
     return out * scale, S, most * abs(scale) * (steps + 3 * 2.0 ** -17), size * steps
+
+
+def state_norm(n, rate):
+    """How far the state after n tokens of random keys and values may be from the
+    formula's, relative to its norm, where all that is off is off either way: a term's
+    value as parts by 2^-22 of itself at most and its decay as much, 2^-22 / sqrt(3) each
+    in the root mean square; and the terms that count, 1 / (1 - l) of them, are added to
+    a sum of about the state's size, 2^-23 / sqrt(3) each (2^-24 if the matrix units
+    round what they add, twice that if they cut it)."""
+    terms = min(n, 1.0 / -math.expm1(rate))
+    return math.sqrt((2 * 16 + 4 * terms) / 3.0) * 2.0 ** -24
+
+
+def in_parts(x, dtype, count):
+    """x (binary32) as the sum of `count` values of a 16-bit type, each the rest's
+    nearest; for binary16 behind a power of two that brings the largest of a column
+    (along dim 0) to 2^14."""
+    factor = torch.ones_like(x[:1])
+    if dtype is torch.float16:
+        factor = torch.exp2(14.0 - torch.floor(torch.log2(x.abs().amax(dim=0, keepdim=True).clamp(min=2.0 ** -100))))
+    rest, total = x * factor, torch.zeros_like(x)
+    for _ in range(count):
+        part = rest.to(dtype).float()
+        rest, total = rest - part, total + part
+    return total / factor

@@ -138,3 +138,21 @@ def test_no_numbers_beside_elements_far_apart(env, what, bad, dtype):
     got, mine = attend(env, q, k, v, state, decay, 1e-4)
     assert not torch.isfinite(got[hit]).any() and ((got - want).abs() <= room + LEAST)[~hit].all()
     assert not torch.isfinite(mine[lost]).any() and ((mine - end).abs() <= state_room + LEAST)[~lost].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [65, 200, 1000])
+def test_dense_states_to_their_own_norm(env, n, dtype):
+    """Of random keys and values a state's terms add up as their squares do, and so do
+    their errors: ref.state_norm says what is left beside the state's own norm
+    (a part of the values less is beyond it)."""
+    g = gen(n)
+    heads, D = 3, 64
+    q, k, v = (torch.randn(n, heads, D, generator=g).to(TYPES[dtype]) for _ in range(3))
+    state, decay = torch.randn(heads, D, D, generator=g) * 4, torch.tensor([-1.0, -2.0 ** -4, -2.0 ** -8])
+    note(f"dense states, {n} tokens {dtype}")
+    _, mine = attend(env, q, k, v, state, decay, 0.125)
+    end = ref.state_attend(q, k, v, state, decay, 0.125)[1]
+    for h in range(heads):
+        off = float((mine[h] - end[h]).norm() / end[h].norm())
+        assert off < ref.state_norm(n, float(decay[h])), (h, off)
