@@ -560,7 +560,8 @@ typedef enum fs_activation {
  * 2^-20 (1 + |y|) |act(y)| + 2^-22 |y|.  A row with a NaN or an infinity, in x or
  * x * gain, gives NaN; one whose x * gain are all below 2^-100 counts as zeros.
  * Where few tiles would leave CUs idle a product is cut along K and its parts added in
- * the workspace, by the last block of a tile to arrive: equal run to run. */
+ * the workspace, by the last block of a tile to arrive: equal run to run.  A workspace of
+ * the most rows is enough for fewer. */
 fs_status fs_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
 fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
                      const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,

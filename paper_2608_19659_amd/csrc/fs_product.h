@@ -1071,6 +1071,8 @@ int best_tile(int32_t M, int32_t N, int32_t K) {
 // last's, its reading, at 4 TB/s, and what waits for them 3 us.  (N: rows of w.
 // us a call, with the quantisation, weights from memory, best uncut and cut: 64 x 5120 x
 // 20480 44 and 36, 64 x (2 x 20480) x 5120 58.9 and 58.0, 8192 x 5120 x 20480 872 and 852.)
+constexpr int64_t kMostParts = 256, kLeastPart = 1024;  // a block a CU, inner elements of each
+
 struct Choice {
   int tile, parts;
   int64_t whole, rest;  // tiles of an XCD that are whole, and cut into parts
@@ -1091,7 +1093,7 @@ Choice choose(int32_t M, int32_t N, int32_t K) {
       best = {i, 1, per, 0};
       least = time;
     }
-    const int parts = rest ? (int)std::min<int64_t>(32 / rest, K / 1024) : 1;
+    const int parts = rest ? (int)std::min<int64_t>(kMostParts / 8 / rest, K / kLeastPart) : 1;
     if (parts < 2) continue;
     const double moved = 8.0 * rest * (2 * parts - 1) * t.bm * t.bn * 4 / 4e6;
     const double cut = (double)(per / 32) * (1.5 + one) + 1.5 + one / parts + 3.0 + moved;

@@ -35,19 +35,29 @@ bool launch_project_few(const QuantizeArgs &X, const MatmulArgs &A, bool gated, 
   return gated ? few_finished<kGated>(X, A, s, e) : few_finished<kFinished>(X, A, s, e);
 }
 
-ProjectParts plan_project(int64_t M, int64_t w_rows, int64_t K, void *counts, void *sums, QuantizeArgs *rows, MatmulArgs *product) {
-  if (M == 0 || w_rows == 0) return {};
-  const Choice c = choose((int32_t)M, (int32_t)w_rows, (int32_t)K);
-  if (product) {
-    product->tile = c.tile;
-    product->whole = (int32_t)c.whole;  // see project_fits
-    product->parts = c.parts;
-    product->arrived = (int32_t *)counts;
-    product->partials = (int32_t *)sums;
-    rows->zero = (int32_t *)counts;
-    rows->n_zero = (int32_t)c.slots();
+PartsRoom parts_room(int64_t M, int64_t w_rows, int64_t K) {
+  if (M == 0 || w_rows == 0 || K < 2 * kLeastPart) return {};
+  // Which tiles are left over, and so what a cut needs, goes up and down with the rows.
+  // Of a few rows the most that as many or fewer need (all tiles' heights are multiples of
+  // 16), of more what the largest tile could.
+  int64_t sums = 0;
+  if (M > 128) {
+    for (const Tile &t : kTiles) sums = std::max<int64_t>(sums, kMostParts * t.bm * t.bn * 4);
+  } else {
+    for (int64_t m = 16; m - 16 < M; m += 16) sums = std::max(sums, choose((int32_t)m, (int32_t)w_rows, (int32_t)K).bytes());
   }
-  return {(size_t)c.slots() * 4, (size_t)c.bytes()};
+  return {(size_t)kMostParts * 4, (size_t)sums};
+}
+
+void plan_project(int64_t M, int64_t w_rows, int64_t K, void *counts, void *sums, QuantizeArgs *rows, MatmulArgs *product) {
+  const Choice c = choose((int32_t)M, (int32_t)w_rows, (int32_t)K);
+  product->tile = c.tile;
+  product->whole = (int32_t)c.whole;  // see project_fits
+  product->parts = c.parts;
+  product->arrived = (int32_t *)counts;
+  product->partials = (int32_t *)sums;
+  rows->zero = (int32_t *)counts;
+  rows->n_zero = (int32_t)c.slots();
 }
 
 bool project_fits(int64_t M, int64_t w_rows, int64_t K) {

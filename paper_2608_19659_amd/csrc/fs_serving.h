@@ -60,12 +60,14 @@ bool launch_linear_few(const QuantizeArgs &X, const MatmulArgs &A, hipStream_t s
 // The same with an RMS norm before and an activation and a residual behind, or
 // gated: w has 2 N rows, the gates' and then the values'.
 hipError_t launch_quantize_normed(const QuantizeArgs &A, hipStream_t s);
-// Bytes of the counts and of the parts' sums of a product of w_rows weight rows; where
-// `rows` and `product` are given they get these places and how the product is cut.
-struct ProjectParts {
+// Bytes for the counts and the parts' sums of products of w_rows weight rows, of M
+// rows and of fewer.
+struct PartsRoom {
   size_t counts, sums;
 };
-ProjectParts plan_project(int64_t M, int64_t w_rows, int64_t K, void *counts, void *sums, QuantizeArgs *rows, MatmulArgs *product);
+PartsRoom parts_room(int64_t M, int64_t w_rows, int64_t K);
+// Gives `rows` and `product` these places and how the product is cut.
+void plan_project(int64_t M, int64_t w_rows, int64_t K, void *counts, void *sums, QuantizeArgs *rows, MatmulArgs *product);
 bool project_fits(int64_t M, int64_t w_rows, int64_t K);
 hipError_t launch_project(const MatmulArgs &A, bool gated, hipStream_t s);
 bool launch_project_few(const QuantizeArgs &X, const MatmulArgs &A, bool gated, hipStream_t s, hipError_t *e);

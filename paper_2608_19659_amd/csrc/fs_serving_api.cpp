@@ -122,7 +122,7 @@ fs_status matmul(const fs::MatmulArgs &A, hipStream_t stream) {
 fs_status project_workspace_size(int64_t M, int64_t w_rows, int64_t K, size_t *bytes) {
   const fs_status st = fs_linear_workspace_size(M, w_rows, K, bytes);
   if (st != FS_OK) return st;
-  const fs::ProjectParts parts = fs::plan_project(M, w_rows, K, nullptr, nullptr, nullptr, nullptr);
+  const fs::PartsRoom parts = fs::parts_room(M, w_rows, K);
   *bytes += align256(parts.counts) + align256(parts.sums);
   return FS_OK;
 }
@@ -166,8 +166,7 @@ fs_status project(fs_context *ctx, const fs_norm *norm, int64_t w_rows, bool gat
   product.a_scale = rows.scale;
   product.a_padded = 1;
   uint8_t *const counts = (uint8_t *)rows.scale + align256(4 * (size_t)M);
-  const fs::ProjectParts parts = fs::plan_project(M, w_rows, K, nullptr, nullptr, nullptr, nullptr);
-  fs::plan_project(M, w_rows, K, counts, counts + align256(parts.counts), &rows, &product);
+  fs::plan_project(M, w_rows, K, counts, counts + align256(fs::parts_room(M, w_rows, K).counts), &rows, &product);
   if (norm) {
     rows.normed = 1;
     rows.gain = norm->gain;
