@@ -36,7 +36,8 @@ def close(got, want, room, what=""):
     assert (off <= room).all(), (what, float(off.flatten()[worst]), float(room.flatten()[worst]))
 
 
-# every tile of the product, rows and channels that fill none, odd inner sizes
+# rows and channels that fill no tile, odd inner sizes (each tile, by the rule that these calls choose by, cut and
+# whole: test_gpu_cut_products.py)
 SIZES = [(1, 1, 1), (1, 64, 64), (1, 2500, 512), (2, 33, 100), (3, 4100, 528), (4, 9000, 64), (4, 131, 2048), (7, 130, 257),
          (16, 256, 1024), (17, 100, 4097), (33, 512, 384), (64, 320, 5120), (65, 65, 65), (100, 2048, 640), (127, 129, 1040),
          (255, 257, 128), (300, 700, 272), (513, 511, 1024), (777, 1100, 333), (2048, 768, 512), (2500, 3001, 129),
@@ -302,8 +303,8 @@ def test_results_are_the_same_on_every_run(env):
         assert all(torch.equal(bits(plan.run()), first) for _ in range(3))
 
 
-# few enough tiles, or few enough in the last round, and a long inner dimension: the
-# blocks' tiles are cut along it
+# long inner dimensions, along which the tiles of some of these are cut (that they are is
+# seen to in test_gpu_cut_products.py)
 CUT = [(5, 40, 2048), (16, 200, 8192), (9, 515, 5000), (20, 1000, 20480), (33, 2000, 3001), (64, 640, 4096), (64, 5120, 20480),
        (64, 20480, 2560), (100, 2000, 9999), (130, 1300, 4096), (300, 4000, 4096), (700, 2560, 6144), (1500, 5120, 4096),
        (2500, 5121, 3333), (5000, 5120, 4096)]
