@@ -704,7 +704,8 @@ typedef struct fs_state_pool {
  * 0): outputs are off by about 2^-17 of their sums' terms before they are rounded, states
  * by about a rounding of binary32.  Equal run to run.  What a NaN or an infinity reaches
  * by the formula (its own token's outputs and later ones, the state) is not finite, and
- * nothing else; a state beyond 2^127 counts as infinite.
+ * nothing else; a state beyond 2^127 counts as infinite.  A workspace of the most tokens
+ * and sequences is enough for fewer.
  *
  * With FS_VALIDATE=1 lengths, states and decays outside their ranges and states that
  * two sequences share are refused (the call waits for the stream); otherwise lengths

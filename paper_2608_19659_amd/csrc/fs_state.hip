@@ -931,7 +931,7 @@ int64_t blocks_at_once(int32_t head_dim) { return head_dim == 128 ? 256 : 512; }
 // The least tokens of a segment: so many that all tokens make about a segment of a
 // head for each of those.
 int segment_least(int64_t n_tokens, int64_t n_heads, int32_t head_dim) {
-  const int64_t L = (n_tokens * n_heads / blocks_at_once(head_dim) + kChunk - 1) / kChunk * kChunk;
+  const int64_t blocks = blocks_at_once(head_dim), L = ((n_tokens * n_heads + blocks - 1) / blocks + kChunk - 1) / kChunk * kChunk;
   return (int)std::max<int64_t>(kChunk, std::min<int64_t>(L, 1 << 30));
 }
 
@@ -967,10 +967,12 @@ int segment_tokens(const StateArgs &A) {
   return (int)std::min<int64_t>(best, 1 << 30);
 }
 // Places of sequences of more than a segment's L tokens: n of them have less than
-// n / L + 1 segments, and so many sequences n / L at most.
+// n / L + 1 segments, and so many sequences n / L at most.  L is the least length's
+// multiple of kChunk, so n / L goes down where that goes up; it is no more than that of
+// the least length itself and of kChunk, which grow with n.
 int64_t places_at_most(int64_t n_tokens, int64_t n_heads, int32_t head_dim, int64_t n_seqs) {
-  const int64_t L = segment_least(n_tokens, n_heads, head_dim);
-  return n_tokens > L ? n_tokens / L + std::min(n_seqs, n_tokens / L) : 0;
+  const int64_t most = std::min<int64_t>(n_tokens / kChunk, blocks_at_once(head_dim) / n_heads);
+  return n_tokens > kChunk ? most + std::min(n_seqs, most) : 0;
 }
 
 template <class S>

@@ -26,3 +26,15 @@ ROWS = [*range(0, 200), *range(200, 8200, 13), *range(8200, 70000, 997), 1 << 17
 def test_projections_by_rows(name, N, K):
     fn = getattr(fs.load_library(), name)
     grows([(M, size(fn, M, N, K)) for M in ROWS], (name, N, K))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads", [1, 3, 8, 12, 40, 200, 300, 1000])
+def test_states(heads, D):
+    fn = fs.load_library().fs_state_attention_workspace_size
+    pool = ctypes.byref(fs._StatePool(None, 4, heads, D))
+    tokens = [*range(0, 8200, 11), *range(8200, 200000, 997), 1 << 20, (1 << 31) // heads - 1]
+    for S in (1, 2, 64, 4096):
+        grows([(T, size(fn, pool, heads, T, S)) for T in tokens], (heads, D, S))
+    for T in (64, 65, 389, 8192, 179966):
+        grows([(S, size(fn, pool, heads, T, S)) for S in range(0, 4097, 7)], (heads, D, T))
