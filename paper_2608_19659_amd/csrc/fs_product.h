@@ -641,7 +641,7 @@ __device__ __forceinline__ void finish_tile(const MatmulArgs &A, int m, int n, i
 
 // Which operands go from memory to LDS as they are: both where all rows start on
 // multiples of 16 bytes, the codes where those rows do and hold whole pieces of
-// 16 (fs_linear's own do whatever K is), else none.
+// 16 (fs_linear's and fs_project's own do whatever K is), else none.
 enum Direct { kBoth, kCodes, kNone };
 
 template <class S, Direct DIRECT, Finish FINISH>
@@ -1031,8 +1031,8 @@ hipError_t matmul_as(const MatmulArgs &A, hipStream_t s) {
   // (both rows of a gated channel: in 32 bits from the tile's first on)
   const bool a = whole(A.a, A.a_stride), w = whole(A.w, A.w_stride) && (FINISH != kGated || A.N * A.w_stride <= (int64_t)1 << 31);
   if (a && w) k_matmul<S, kBoth, FINISH><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
-  else if (a && (A.a_padded || A.K % 16 == 0)) k_matmul<S, kCodes, FINISH><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
-  else k_matmul<S, kNone, FINISH><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else if (FINISH != kScaled || (a && (A.a_padded || A.K % 16 == 0))) k_matmul<S, kCodes, FINISH><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
+  else if constexpr (FINISH == kScaled) k_matmul<S, kNone, FINISH><<<grid, S::THREADS, 0, s>>>(A, tm, tn);
   return hipGetLastError();
 }
 
