@@ -99,14 +99,14 @@ __device__ __forceinline__ void store_codes8(int8_t *out, int c, int cols, const
 }
 
 // The mean of squares that an RMS norm divides by, of any finite values: two
-// sums, of x^2 and of (2^-72 x)^2, the second where the first may pass what
-// binary32 holds.  (What the first loses below 2^-126 is of no account beside an
+// sums, of x^2 and of (2^-80 x)^2, the second where the first may pass what
+// binary32 holds (131071 of the largest values make 2^113 of it).  (What the first loses below 2^-126 is of no account beside an
 // eps of 2^-80 at least.)
 struct Squares {
   float sum, low;
 
   __device__ __forceinline__ void add(float x) {
-    const float y = x * 0x1p-72f;
+    const float y = x * 0x1p-80f;
     sum = __builtin_fmaf(x, x, sum);
     low = __builtin_fmaf(y, y, low);
   }
@@ -121,7 +121,7 @@ struct Squares {
   // 1 / sqrt(mean + eps), by v_rsq_f32: within a step
   __device__ __forceinline__ float factor(int count, float eps) const {
     if (sum < 0x1p100f) return __builtin_amdgcn_rsqf(sum / (float)max(count, 1) + eps);
-    return 0x1p-72f * __builtin_amdgcn_rsqf(low / (float)count + eps * 0x1p-144f);
+    return 0x1p-80f * __builtin_amdgcn_rsqf(low / (float)count + eps * 0x1p-160f);
   }
 };
 
