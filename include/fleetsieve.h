@@ -556,12 +556,12 @@ typedef enum fs_activation {
  * behind the norm (norm NULL: none), its bias (NULL: none) among it.  residual
  * [M][N] is of out_type (NULL: none); it may be out itself, with out's stride, and
  * may not overlap it otherwise (nor x in any way).  All in binary32, rounded once;
- * without norm, activation and residual the bits of fs_linear.  Activations are off by less than
- * 2^-20 (1 + |y|) |act(y)| + 2^-22 |y|.  A row with a NaN or an infinity, in x or
- * x * gain, gives NaN; one whose x * gain are all below 2^-100 counts as zeros.
- * Where few tiles would leave CUs idle a product is cut along K and its parts added in
- * the workspace, by the last block of a tile to arrive: equal run to run.  A workspace of
- * the most rows is enough for fewer. */
+ * without norm, activation and residual the bits of fs_linear.  Activations are off
+ * by less than 2^-20 (1 + |y|) |act(y)| + 2^-22 |y|, gelu without the last.  A row
+ * with a NaN or an infinity, in x or x * gain, gives NaN; one whose x * gain are all
+ * below 2^-100 counts as zeros.  Where few tiles would leave CUs idle a product is cut
+ * along K and its parts added in the workspace, by the last block of a tile to arrive:
+ * equal run to run.  A workspace of the most rows is enough for fewer. */
 fs_status fs_project_workspace_size(int64_t M, int64_t N, int64_t K, size_t *bytes);
 fs_status fs_project(fs_context *ctx, const void *d_x, fs_dtype type, int64_t x_stride, const fs_norm *norm,
                      const int8_t *d_w, int64_t w_stride, const float *d_w_scale, const float *d_bias,
