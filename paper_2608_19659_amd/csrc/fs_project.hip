@@ -9,12 +9,13 @@
 // values are never stored: a decoder layer of 5120 channels takes 43 us instead of 63
 // for one token on a TP8 shard (of 80 layers, a cache of 1152 tokens).
 //
-// Measured, weights from memory: one row of 5120 x 5120 7.1 us (3.7 TB/s; the chain
-// of a row's loads, its codes and the first weights is most of what is above the
-// weights' bytes' 5.1), normed and gated by 2 x 2560 8.2; 64 rows by 2 x 20480, K =
-// 5120, 57 (3.7 TB/s: a stage's chain of barrier, LDS and products keeps its loads
-// from filling the memory; deeper rings, wider tiles and two blocks a CU took 57 to
-// 61); 4096 rows of the same 747 (2.3 PO/s).
+// Measured, weights from memory: one row of 5120 x 5120 7.1 us (3.7 TB/s, the
+// weights' bytes' time 5.1: a block's chain of the row's loads, its codes and ten stages of
+// weights, in 160 blocks on 256 CUs), normed and gated by 2 x 2560 8.1; 64 rows by 2 x
+// 20480, K = 5120, 57.5 (5 of them the codes' launch, then 4.0 TB/s: a stage's chain of
+// barrier, LDS and products keeps its loads from filling the memory; deeper rings,
+// wider tiles and two blocks a CU took 57 to 61); 4096 rows of the same 735 to 765 by
+// the card (2.3 PO/s).
 #include "fs_product.h"
 
 namespace fs {

@@ -466,7 +466,7 @@ __device__ __forceinline__ constexpr int token(int t, int e, int g) { return t *
 // queries are loaded.  The states' columns make the wavefronts independent but for
 // these products; every wavefront reads all of a head's queries from LDS, and that
 // beside the products' own chain is what bounds it.  Of 4 prompts of 2048 tokens (40
-// query heads over 8) 58 us, 16 of the segments' own sums, 7.6 of joining them; bytes'
+// query heads over 8) 59 us, 16 of the segments' own sums, 7.7 of joining them; bytes'
 // time 40.  Counted there: matrix units 34 % busy, LDS 27 %, a fifteenth of that conflicts.
 // (Operands each awaited by itself 72 us, loads through registers 107, four wavefronts
 // of 32 columns 107.)

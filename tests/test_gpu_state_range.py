@@ -156,3 +156,33 @@ def test_dense_states_to_their_own_norm(env, n, dtype):
     for h in range(heads):
         off = float((mine[h] - end[h]).norm() / end[h].norm())
         assert off < ref.state_norm(n, float(decay[h])), (h, off)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("news", [[100], [70, 1, 300], [900]], ids=str)
+def test_replays_are_the_eager_calls(env, news, dtype):
+    """States of many sizes and fast decays, captured and replayed, each replay from the
+    states of the one before."""
+    fs, ctx = env
+    heads, group, D, S = 2, 2, 64, len(news)
+    note(f"replays of states of many sizes, {news} {dtype}")
+    g = gen(sum(news))
+    cu = [0]
+    for n in news:
+        cu.append(cu[-1] + n)
+    make = lambda h: torch.randn(cu[-1], h, D, generator=g).to(TYPES[dtype]).to("cuda:0")  # noqa: E731
+    q, k, v = make(heads * group), make(heads), make(heads)
+    pools = [spread((S, heads, D, D), gen(1), -6, 3).to("cuda:0") for _ in range(2)]
+    where = (i32(list(range(S))), i32([n + 5 for n in news]), i32(cu), max(news), torch.tensor([-0.7, -0.01], device="cuda:0"))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    ws = torch.empty(16 << 20, dtype=torch.uint8, device="cuda:0")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        out = fs.state_attention(ctx, pools[0], q, k, v, *where, stream=side, workspace=ws)
+    for i in range(4):
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, generator=gen(i)))
+        graph.replay()
+        want = fs.state_attention(ctx, pools[1], q, k, v, *where)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(out), bits(want)) and torch.equal(bits(pools[0]), bits(pools[1])), i
